@@ -39,6 +39,7 @@
  *    outputs are too (no floating-point atomics are used anywhere).
  *  - Supported: d == 128; Hq / Hkv in {1, 2, 4, 8}; cluster counts up to
  *    CK_MAX_CLUSTERS per head-problem.
+ *  - Caches in pages have a layout of their own (ck_paged_kv, below).
  */
 #ifndef CLUSTERKV_H
 #define CLUSTERKV_H
@@ -78,6 +79,19 @@ extern "C" {
 #define CK_WS_CLUSTER_KEYS 0
 #define CK_WS_SPARSE_ATTN 1
 #define CK_WS_OBJECTIVE 2
+#define CK_WS_PAGED_ATTN 3
+#define CK_WS_PROMPT_ATTN 4
+
+/* kind argument of ck_rope_frequencies */
+#define CK_ROPE_PLAIN 0
+#define CK_ROPE_LINEAR 1
+#define CK_ROPE_BASE 2
+#define CK_ROPE_RAMP 3
+#define CK_ROPE_BANDS 4
+
+/* flags of ck_rope_append */
+#define CK_ROPE_HALVES 0u      /* channel j turns with channel j + rot_dim / 2 */
+#define CK_ROPE_ADJACENT 1u    /* channel 2 j turns with channel 2 j + 1 */
 
 typedef struct ck_shape {
   int32_t S;       /* sequences in the batch */
@@ -100,6 +114,8 @@ const char* ck_last_error_detail(void);
  *   CK_WS_OBJECTIVE:    n = tok_count of ck_kmeans_objective, c ignored.
  *   CK_WS_SPARSE_ATTN:  n = upper bound of attended tokens per head-problem
  *                       (budget + n_sink + recent window), c ignored.
+ *   CK_WS_PAGED_ATTN:   n and c ignored: enough for every list, window and lengths.
+ *   CK_WS_PROMPT_ATTN:  n = n_rows of ck_prompt_attn, c ignored.
  * Returns 0 for an invalid request.
  */
 size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c);
@@ -477,6 +493,149 @@ int ck_cached_decode_step(const ck_shape* sh, const void* q, const void* K_home,
                           float softmax_scale, float* scores, int32_t* sel_clusters,
                           int32_t* n_sel_clusters, int32_t* n_sel_tokens, int32_t* miss_tokens,
                           void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A cache in pages: what stands before and beside the clustered path.  Prompts and
+ * generated tokens get their rotary positions and their rows in the cache
+ * (ck_rope_append); prompts attend causally (ck_prompt_attn), single tokens over
+ * caches of different lengths, in full, with a window and sinks, or over a recalled
+ * list (ck_paged_decode_attn); rows move between caches (ck_copy_rows).
+ *
+ * Row r of sequence s and KV head h is
+ *   K[page_table[s][r / page_size]][h][r % page_size]        (and V likewise).
+ * The contiguous caches of the calls above, [S, Hkv, N_cap, d], are the same thing
+ * with page_size = N_cap, pages_per_seq = 1 and page_table = 0, 1, .., S - 1.
+ *
+ *   K, V          [n_pages, Hkv, page_size, d] in sh->dtype
+ *   page_table    int32 [n_seqs, pages_per_seq]; several sequences may name one page.
+ *                 A number outside [0, n_pages) is no page: its rows are not attended,
+ *                 nothing is written to them and nothing is copied from them.  So the
+ *                 pages that a window has left behind can be taken away (entry -1).
+ *   page_size     rows of a page, any number >= 1
+ *   n_pages * Hkv * page_size has to stay below 2^31.
+ *
+ * lengths [dev] int32 [S] is the number of rows of every sequence, the new tokens'
+ * included.  The attention calls take it as at least 0 and at most pages_per_seq *
+ * page_size.
+ * sh->N_cap and sh->C_cap are not used by these calls (they have to be positive).
+ *
+ * Ragged batches: q_starts [dev] int32 [S + 1] ascending; the new tokens of sequence s
+ * are rows [q_starts[s], q_starts[s + 1]) of q, k, v and out, token i of them is row
+ *   lengths[s] - (q_starts[s + 1] - q_starts[s]) + i   of its cache.
+ * A sequence may have none.  Rows of q, k, v and out before q_starts[0], from q_starts[S]
+ * on or from n_rows on are neither read nor written.
+ * ---------------------------------------------------------------------- */
+typedef struct ck_paged_kv {
+  void* K;
+  void* V;
+  const int32_t* page_table;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_seqs;
+  int32_t pages_per_seq;
+} ck_paged_kv;
+
+/*
+ * Turning rates of rotary positions: freqs [host out] rot_dim / 2 floats, radians per
+ * position, of pair j = 0, 1, ..; *attn_factor [host out] what cosines and sines are
+ * multiplied by (1 except for CK_ROPE_RAMP).  With w_j = base^(-2 j / rot_dim):
+ *   CK_ROPE_PLAIN   w_j
+ *   CK_ROPE_LINEAR  w_j / factor
+ *   CK_ROPE_BASE    as plain with base * factor^(rot_dim / (rot_dim - 2))
+ *   CK_ROPE_RAMP    pairs that make more than `fast` turns within trained_len positions keep
+ *                   w_j, those that make fewer than `slow` get w_j / factor, a ramp over j
+ *                   between; attn_factor = 0.1 ln(factor) + 1 (arXiv 2309.00071)
+ *   CK_ROPE_BANDS   the same ends, by trained_len against the wavelength 2 pi / w_j: more
+ *                   than `fast` wavelengths keep w_j, fewer than `slow` get w_j / factor, between
+ *                   them the share of w_j grows linearly with the number of wavelengths
+ * factor >= 1; trained_len, fast and slow (fast > slow > 0) are read by the last two only.
+ * Host only: nothing is enqueued.
+ * Errors: CK_EINVALID (null, unknown kind, odd rot_dim or outside [2, d], base <= 1, ...).
+ */
+int ck_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double factor,
+                        double trained_len, double fast, double slow, float* freqs,
+                        float* attn_factor);
+
+/*
+ * Rotary positions and cache rows of new tokens.  Of every query and key head the first
+ * rot_dim channels turn in pairs (x1, x2), by the angle a = position * freqs[j]:
+ *   x1' = attn_factor (x1 cos a - x2 sin a),  x2' = attn_factor (x2 cos a + x1 sin a);
+ * the other channels stay as they are.  Queries go to q_out, keys and values (as they
+ * are) to the tokens' rows of the cache; no other row is touched.
+ * q, k, v    [dev] token rows of [Hq, d], [Hkv, d], [Hkv, d]; the row of token t starts at
+ *            t * q_stride (k_stride, v_stride) elements, strides are multiples of 16 bytes
+ *            (views of one projection's output can be given as they are).  q and q_out may
+ *            be NULL together: only the cache is written.
+ * n_rows     token rows there are; q_starts NULL: n_rows == S, one new token per sequence.
+ * positions  [dev] int32 [n_rows], NULL: the row of the cache.
+ * freqs      [dev] float [rot_dim / 2].
+ * q_out      [dev] [n_rows, Hq, d]; may be q itself where q_stride == Hq * d.
+ * A token whose row lies outside the table or on no page is not stored.  Angles are exact
+ * to 2^-50 turns at any position (64-bit product and reduction), the rest is 32-bit, rounded
+ * once.  Pages that two sequences share must not get rows in the same call.
+ */
+int ck_rope_append(const ck_shape* sh, const void* q, const void* k, const void* v,
+                   int64_t q_stride, int64_t k_stride, int64_t v_stride, int64_t n_rows,
+                   const int32_t* q_starts, const int32_t* lengths, const int32_t* positions,
+                   const float* freqs, int32_t rot_dim, float attn_factor, uint32_t flags,
+                   void* q_out, const ck_paged_kv* kv, void* stream);
+
+/*
+ * GQA decode attention of one token per sequence over a paged cache: q, out [S, Hq, d], and
+ * with n = lengths[s] (the new token is row n - 1) over the rows
+ *   window < 0:   [0, n)
+ *   window >= 0:  [0, min(n_sink, n)), the list, [max(n_sink, n - window), n).
+ * No row at all gives zeros.
+ * token_idx [dev] int32 [S, Hkv, idx_stride], n_tokens [dev] int32 [S, Hkv]: recalled rows, as
+ *           ck_gather_indices writes them; both NULL: no list.  Needs window >= 0.  Entries
+ *           outside [0, n) are not attended; one that is a sink, in the window or listed
+ *           twice counts twice.  max_tokens: upper bound of n_tokens, <= idx_stride.
+ * workspace ck_workspace_bytes(sh, CK_WS_PAGED_ATTN, 0, 0); calls that share one must be
+ *           ordered (its contents on entry do not matter).
+ * The split of the rows over workgroups follows the lengths, which are read on the device:
+ * a captured call may be replayed with other lengths, lists and tables.  Softmax and sums
+ * in fp32; the order of the sums depends on the lengths of the whole batch.
+ */
+int ck_paged_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* kv,
+                         const int32_t* lengths, int64_t n_sink, int64_t window,
+                         const int32_t* token_idx, const int32_t* n_tokens, int32_t idx_stride,
+                         int32_t max_tokens, float softmax_scale, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Causal GQA attention of new tokens over a paged cache that holds their rows already: the
+ * query at row p of its sequence attends to the rows r <= p with
+ *   window < 0, or r < n_sink, or r > p - window
+ * (window counts the token itself; 0 leaves the sinks).  No row at all gives zeros.
+ * q, out    [dev] [n_rows, Hq, d], CK_BF16 only; not the same buffer.
+ * q_starts, lengths  see above (q_starts is needed here).
+ * workspace ck_workspace_bytes(sh, CK_WS_PROMPT_ATTN, n_rows, 0); calls that share one must
+ *           be ordered (its contents on entry do not matter).
+ * Products take bf16 operands (probabilities rounded to bf16), maximum, sum and accumulators
+ * are fp32.
+ */
+int ck_prompt_attn(const ck_shape* sh, const void* q, int64_t n_rows, const int32_t* q_starts,
+                   const ck_paged_kv* kv, const int32_t* lengths, int64_t n_sink, int64_t window,
+                   float softmax_scale, void* out, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
+/*
+ * Rows of one cache to another: for every sequence s < S, KV head h and j < n_copy[s]
+ *   dst row (s, h, begin[s] + j) := src row (src_seq[s], h, row_idx[s, h, j] or begin[s] + j),
+ * keys and values, as they are.  Copies a shared page before it is written (fork), keeps
+ * the listed rows of a cache in fresh pages (compaction), and moves rows between paged and
+ * contiguous caches.
+ * n_copy    [dev] int32 [S], taken as at least 0 and at most max_rows.
+ * row_idx   [dev] int32 [S, Hkv, idx_stride], idx_stride >= max_rows, NULL: rows keep their number.
+ * begin     [dev] int32 [S], NULL: 0.
+ * src_seq   [dev] int32 [S], NULL: s itself (then src->n_seqs >= S).
+ * Rows that either cache does not have (negative, behind the table, on no page, a src_seq that
+ * is none) are left out: what stands in dst stays.  src and dst may share the pool; a row that
+ * the call writes must not be one that it reads, nor be written twice.
+ */
+int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* dst,
+                 const int32_t* n_copy, int32_t max_rows, const int32_t* row_idx,
+                 int32_t idx_stride, const int32_t* begin, const int32_t* src_seq, void* stream);
 
 /*
  * Measurement aid, not part of the method: a register-only loop of

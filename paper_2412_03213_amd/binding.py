@@ -18,7 +18,9 @@ CK_BF16, CK_F32 = 0, 1
 CK_SEL_WHOLE, CK_SEL_TRIM_LAST = 0, 1
 CK_MAX_CLUSTERS = 2048
 CK_METRIC_COSINE, CK_METRIC_L2, CK_METRIC_IP, CK_KM_UNTIL_CONVERGED = 0, 1, 2, 4
-CK_WS_CLUSTER_KEYS, CK_WS_SPARSE_ATTN, CK_WS_OBJECTIVE = 0, 1, 2
+CK_WS_CLUSTER_KEYS, CK_WS_SPARSE_ATTN, CK_WS_OBJECTIVE, CK_WS_PAGED_ATTN, CK_WS_PROMPT_ATTN = 0, 1, 2, 3, 4
+CK_ROPE_PLAIN, CK_ROPE_LINEAR, CK_ROPE_BASE, CK_ROPE_RAMP, CK_ROPE_BANDS = 0, 1, 2, 3, 4
+CK_ROPE_HALVES, CK_ROPE_ADJACENT = 0, 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libclusterkv.so")
@@ -28,7 +30,8 @@ EXPORTS = ("ck_version", "ck_strerror", "ck_last_error_detail", "ck_workspace_by
            "ck_select_clusters", "ck_gather_indices", "ck_sparse_decode_attn", "ck_sparse_decode_attn_static", "ck_sparse_decode_attn_two_pass", "ck_decode_step",
            "ck_full_decode_attn", "ck_token_scores", "ck_topk_select", "ck_recall_hits",
            "ck_page_keys", "ck_expand_pages", "ck_host_device_ptr", "ck_cache_reset",
-           "ck_cached_decode_step", "ck_probe_mfma_bf16")
+           "ck_cached_decode_step", "ck_rope_frequencies", "ck_rope_append", "ck_paged_decode_attn",
+           "ck_prompt_attn", "ck_copy_rows", "ck_probe_mfma_bf16")
 
 
 class ClusterKVError(RuntimeError):
@@ -48,6 +51,12 @@ class _CkClusterCache(ctypes.Structure):
                 ("clusters", ctypes.c_void_p * 2), ("starts", ctypes.c_void_p * 2),
                 ("n_held", ctypes.c_void_p * 2), ("cap_tokens", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class _CkPagedKV(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("pages_per_seq", ctypes.c_int32)]
 
 
 @dataclass(frozen=True)
@@ -151,6 +160,19 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.ck_cached_decode_step.restype = ctypes.c_int
     lib.ck_cached_decode_step.argtypes = [SH, P, P, P, P, P, P, P, I32, I32, CC, I32, F, P, P, P,
                                           P, P, P, P, SZ, P]
+    KV = ctypes.POINTER(_CkPagedKV)
+    DBL = ctypes.c_double
+    lib.ck_rope_frequencies.restype = ctypes.c_int
+    lib.ck_rope_frequencies.argtypes = [I32, I32, DBL, DBL, DBL, DBL, DBL, ctypes.POINTER(F),
+                                        ctypes.POINTER(F)]
+    lib.ck_rope_append.restype = ctypes.c_int
+    lib.ck_rope_append.argtypes = [SH, P, P, P, I64, I64, I64, I64, P, P, P, P, I32, F, U32, P, KV, P]
+    lib.ck_paged_decode_attn.restype = ctypes.c_int
+    lib.ck_paged_decode_attn.argtypes = [SH, P, KV, P, I64, I64, P, P, I32, I32, F, P, P, SZ, P]
+    lib.ck_prompt_attn.restype = ctypes.c_int
+    lib.ck_prompt_attn.argtypes = [SH, P, I64, P, KV, P, I64, I64, F, P, P, SZ, P]
+    lib.ck_copy_rows.restype = ctypes.c_int
+    lib.ck_copy_rows.argtypes = [SH, KV, KV, P, I32, P, I32, P, P, P]
     lib.ck_probe_mfma_bf16.restype = ctypes.c_int
     lib.ck_probe_mfma_bf16.argtypes = [I32, I32, P, P, P, ctypes.POINTER(ctypes.c_double), P]
     lib.host_decode_step = _host_decode_step()
@@ -467,6 +489,163 @@ def cached_decode_step(st, cache: ClusterCache, q, K_home, V_home):
                           cache.miss_tokens, st.out, workspace=st.attn_ws)
     cache.step += 1
     return st.out
+
+
+class PagedKV:
+    """Keys and values of a batch in pages: K, V [n_pages, Hkv, page_size, d], page_table int32
+    [n_seqs, pages_per_seq].  Without a table K and V are a contiguous cache [S, Hkv, N_cap, d],
+    one page for each sequence.  The tensors may be written in place, not replaced."""
+
+    def __init__(self, K, V, page_table=None):
+        if page_table is None:
+            page_table = torch.arange(K.shape[0], dtype=torch.int32, device=K.device)[:, None]
+        if K.dim() != 4 or K.shape != V.shape or K.dtype != V.dtype:
+            raise ValueError("K and V must be [n_pages, Hkv, page_size, d], of one type")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32:
+            raise ValueError("page_table must be int32 [n_seqs, pages_per_seq]")
+        self.K, self.V, self.page_table = K, V, page_table
+        self.dtype, self.Hkv, self.page_size = K.dtype, K.shape[1], K.shape[2]
+        self._c = _CkPagedKV(_ptr(K), _ptr(V), _ptr(page_table), K.shape[0], K.shape[2],
+                             page_table.shape[0], page_table.shape[1])
+        self._d = K.shape[3]
+
+    def c(self, sh: Shape) -> _CkPagedKV:
+        if self.Hkv != sh.Hkv or self._d != sh.d or self.dtype != sh.torch_dtype:
+            raise ValueError("the cache has other heads or another type than the shape says")
+        return self._c
+
+
+def _kv(sh: Shape, kv):
+    if isinstance(kv, PagedKV):
+        return ctypes.byref(kv.c(sh))
+    return ctypes.byref(kv) if kv is not None else None      # a structure of raw addresses
+
+
+def _ints(t, name, *shape):
+    """Address of an int32 tensor of this shape (None: any), of an address, or None."""
+    if not isinstance(t, torch.Tensor):
+        return t
+    if t.dtype is not torch.int32 or t.dim() != len(shape) or any(
+            want is not None and have != want for have, want in zip(t.shape, shape)):
+        raise ValueError(f"{name} must be int32 {list(shape)}")
+    return _ptr(t)
+
+
+def _rows(t, name, heads: int, sh: Shape):
+    """Address and row stride of token rows [n, heads, d] whose rows may lie apart."""
+    if not isinstance(t, torch.Tensor):
+        return t, heads * sh.d
+    if t.dtype is not sh.torch_dtype or t.dim() != 3 or t.shape[1:] != (heads, sh.d) or (
+            t.stride()[1:] != (sh.d, 1) and t.shape[1] > 1) or t.stride(2) != 1:
+        raise ValueError(f"{name} must be token rows [n, {heads}, {sh.d}] of the shape's type")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * sh.d
+
+
+def _dense(t, name, n, sh: Shape):
+    if isinstance(t, torch.Tensor) and (t.dtype is not sh.torch_dtype or
+                                        tuple(t.shape) != (n, sh.Hq, sh.d)):
+        raise ValueError(f"{name} must be [{n}, {sh.Hq}, {sh.d}] of the shape's type")
+    return _ptr(t)
+
+
+def _bytes(workspace) -> int:
+    return workspace.numel() * workspace.element_size() if isinstance(workspace, torch.Tensor) else 0
+
+
+def ck_rope_frequencies(kind: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0,
+                        trained_len: float = 0.0, fast: float = 0.0, slow: float = 0.0):
+    """Turning rates as a host tensor, float32 [rot_dim / 2], and the factor on cosines and sines."""
+    lib = load_library()
+    freqs = torch.zeros(max(1, rot_dim // 2), dtype=torch.float32)
+    af = ctypes.c_float(0.0)
+    _check(lib.ck_rope_frequencies(kind, rot_dim, base, factor, trained_len, fast, slow,
+                                   ctypes.cast(freqs.data_ptr(), ctypes.POINTER(ctypes.c_float)),
+                                   ctypes.byref(af)))
+    return freqs, af.value
+
+
+def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None, positions=None,
+                   attn_factor: float = 1.0, interleaved: bool = False):
+    """q, k, v: token rows [n, heads, d], views of one projection's output among them; freqs: device
+    float32 [rot_dim / 2]; q and q_out may both be None.  interleaved: adjacent channels turn."""
+    lib = load_library()
+    n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
+    qp, qs = _rows(q, "q", sh.Hq, sh)
+    kp, ks = _rows(k, "k", sh.Hkv, sh)
+    vp, vs = _rows(v, "v", sh.Hkv, sh)
+    for t in (q, v):
+        if isinstance(t, torch.Tensor) and t.shape[0] != n:
+            raise ValueError("q, k and v must have the same number of rows")
+    if isinstance(freqs, torch.Tensor) and (freqs.dtype is not torch.float32 or freqs.dim() != 1):
+        raise ValueError("freqs must be float32 [rot_dim / 2]")
+    rot = 2 * freqs.shape[0] if isinstance(freqs, torch.Tensor) else sh.d
+    s = sh.c()
+    _check(lib.ck_rope_append(ctypes.byref(s), qp, kp, vp, qs, ks, vs, n,
+                              _ints(q_starts, "q_starts", sh.S + 1),
+                              _ints(lengths, "lengths", sh.S), _ints(positions, "positions", n),
+                              _ptr(freqs), rot, attn_factor,
+                              CK_ROPE_ADJACENT if interleaved else CK_ROPE_HALVES,
+                              _dense(q_out, "q_out", n, sh), _kv(sh, kv), _stream(k)))
+
+
+def paged_decode_workspace(sh: Shape, device) -> torch.Tensor:
+    """Scratch of ck_paged_decode_attn, whatever its lists, window and lengths."""
+    return torch.empty(max(256, ck_workspace_bytes(sh, CK_WS_PAGED_ATTN, 0)), dtype=torch.uint8,
+                       device=device)
+
+
+def prompt_workspace(sh: Shape, n_rows: int, device) -> torch.Tensor:
+    """Scratch of ck_prompt_attn for up to n_rows token rows."""
+    return torch.empty(max(256, ck_workspace_bytes(sh, CK_WS_PROMPT_ATTN, n_rows)),
+                       dtype=torch.uint8, device=device)
+
+
+def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window: int = -1,
+                         token_idx=None, n_tokens=None, max_tokens=None, softmax_scale=None,
+                         workspace=None):
+    lib = load_library()
+    if softmax_scale is None:
+        softmax_scale = sh.d ** -0.5
+    if workspace is None:
+        workspace = paged_decode_workspace(sh, q.device)
+    stride = token_idx.shape[-1] if isinstance(token_idx, torch.Tensor) else 0
+    if max_tokens is None:
+        max_tokens = stride
+    s = sh.c()
+    _check(lib.ck_paged_decode_attn(ctypes.byref(s), _dense(q, "q", sh.S, sh), _kv(sh, kv),
+                                    _ints(lengths, "lengths", sh.S), n_sink, window,
+                                    _ints(token_idx, "token_idx", sh.S, sh.Hkv, None),
+                                    _ints(n_tokens, "n_tokens", sh.S, sh.Hkv), stride, max_tokens,
+                                    softmax_scale, _dense(out, "out", sh.S, sh), _ptr(workspace),
+                                    _bytes(workspace), _stream(q)))
+    return workspace
+
+
+def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, window: int = -1,
+                   softmax_scale=None, workspace=None):
+    lib = load_library()
+    if softmax_scale is None:
+        softmax_scale = sh.d ** -0.5
+    n = q.shape[0] if isinstance(q, torch.Tensor) else 1
+    if workspace is None:
+        workspace = prompt_workspace(sh, n, q.device)
+    s = sh.c()
+    _check(lib.ck_prompt_attn(ctypes.byref(s), _dense(q, "q", n, sh), n,
+                              _ints(q_starts, "q_starts", sh.S + 1), _kv(sh, kv),
+                              _ints(lengths, "lengths", sh.S), n_sink, window, softmax_scale,
+                              _dense(out, "out", n, sh), _ptr(workspace), _bytes(workspace),
+                              _stream(q)))
+    return workspace
+
+
+def ck_copy_rows(sh: Shape, src, dst, n_copy, max_rows: int, row_idx=None, begin=None, src_seq=None):
+    lib = load_library()
+    stride = row_idx.shape[-1] if isinstance(row_idx, torch.Tensor) else max_rows
+    s = sh.c()
+    _check(lib.ck_copy_rows(ctypes.byref(s), _kv(sh, src), _kv(sh, dst), _ints(n_copy, "n_copy", sh.S),
+                            max_rows, _ints(row_idx, "row_idx", sh.S, sh.Hkv, None), stride,
+                            _ints(begin, "begin", sh.S), _ints(src_seq, "src_seq", sh.S),
+                            _stream(n_copy)))
 
 
 def _probe_operands(t):

@@ -1,5 +1,6 @@
 // C ABI of the ClusterKV library: argument validation (host only, before anything
 // is enqueued) and the sequence of kernel launches behind every entry point.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 
@@ -112,6 +113,11 @@ size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c) {
   if (which == CK_WS_OBJECTIVE) {
     if (n < 1) return 0;
     return ck::objective_workspace_bytes(dm, n);
+  }
+  if (which == CK_WS_PAGED_ATTN) return ck::paged_workspace_bytes(dm);
+  if (which == CK_WS_PROMPT_ATTN) {
+    if (n < 1 || n > ck::MAX_NEW_ROWS) return 0;
+    return ck::prompt_workspace_bytes(dm, n);
   }
   return 0;
 }
@@ -795,6 +801,206 @@ int ck_cached_decode_step(const ck_shape* sh, const void* q, const void* K_home,
                                            0, budget, 0, 0, 0, softmax_scale, out, workspace, false,
                                            st),
                     "attention launch");
+}
+
+namespace {
+// K and V are looked at last, as in the other calls: K [dev], then V
+int check_paged(const ck_paged_kv* kv, const char* what, const ck::Dims& dm, int64_t n_seqs) {
+  if (!kv) return fail(CK_EINVALID, "%s is NULL", what);
+  if (kv->n_pages < 1 || kv->page_size < 1 || kv->n_seqs < 1 || kv->pages_per_seq < 1)
+    return fail(CK_EINVALID, "%s: n_pages, page_size, n_seqs and pages_per_seq must be positive", what);
+  if (kv->n_seqs < n_seqs)
+    return fail(CK_EINVALID, "%s: a table of %d sequences, %lld needed", what, kv->n_seqs, (long long)n_seqs);
+  const double rows = (double)kv->n_pages * dm.Hkv * kv->page_size;
+  if (rows > (double)0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "%s: more than 2^31 - 1 rows in the pool", what);
+  if ((int64_t)kv->page_size * kv->pages_per_seq > (int64_t)1 << 30)
+    return fail(CK_EUNSUPPORTED, "%s: more than 2^30 rows of a sequence", what);
+  const void* all[3] = {kv->K, kv->V, kv->page_table};
+  const char* name[3] = {"K", "V", "page_table"};
+  for (int i = 0; i < 3; ++i) {
+    if (!all[i]) return fail(CK_EINVALID, "%s: %s is NULL", what, name[i]);
+    if (!aligned16(all[i])) return fail(CK_EMISALIGNED, "%s: %s is not 16-byte aligned", what, name[i]);
+  }
+  return CK_OK;
+}
+
+int check_rows(int64_t n_rows) {
+  if (n_rows < 1) return fail(CK_EINVALID, "n_rows=%lld must be positive", (long long)n_rows);
+  if (n_rows > ck::MAX_NEW_ROWS)
+    return fail(CK_EUNSUPPORTED, "n_rows=%lld (at most %lld)", (long long)n_rows, (long long)ck::MAX_NEW_ROWS);
+  return CK_OK;
+}
+
+int check_token_rows(const char* what, const void* p, int64_t stride, int heads, const ck::Dims& dm) {
+  if (!p) return fail(CK_EINVALID, "%s is NULL", what);
+  if (!aligned16(p)) return fail(CK_EMISALIGNED, "%s is not 16-byte aligned", what);
+  if (stride < (int64_t)heads * ck::D)
+    return fail(CK_EINVALID, "%s_stride=%lld smaller than a row of %d", what, (long long)stride, heads * ck::D);
+  if (stride % (dm.dtype == CK_BF16 ? 8 : 4) != 0)
+    return fail(CK_EMISALIGNED, "%s_stride=%lld is no multiple of 16 bytes", what, (long long)stride);
+  if (stride > (int64_t)1 << 40) return fail(CK_EUNSUPPORTED, "%s_stride=%lld", what, (long long)stride);
+  return CK_OK;
+}
+}  // namespace
+
+int ck_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double factor,
+                        double trained_len, double fast, double slow, float* freqs,
+                        float* attn_factor) {
+  if (kind < CK_ROPE_PLAIN || kind > CK_ROPE_BANDS) return fail(CK_EINVALID, "unknown kind %d", kind);
+  if (rot_dim < 2 || rot_dim > ck::D || rot_dim % 2 != 0)
+    return fail(CK_EINVALID, "rot_dim=%d must be even and in [2, %d]", rot_dim, ck::D);
+  if (!(base > 1.0) || !isfinite(base)) return fail(CK_EINVALID, "base must be greater than 1");
+  if (kind != CK_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor)))
+    return fail(CK_EINVALID, "factor must be at least 1");
+  if (kind == CK_ROPE_BASE && rot_dim == 2)
+    return fail(CK_EINVALID, "one pair has no base to raise: its rate is 1");
+  const bool by_turns = kind == CK_ROPE_RAMP || kind == CK_ROPE_BANDS;
+  if (by_turns && (!(trained_len > 0.0) || !isfinite(trained_len) || !(slow > 0.0) || !(fast > slow) || !isfinite(fast)))
+    return fail(CK_EINVALID, "trained_len must be positive and fast > slow > 0");
+  if (!freqs || !attn_factor) return fail(CK_EINVALID, "freqs or attn_factor is NULL");
+  const double two_pi = 6.283185307179586477;
+  if (kind == CK_ROPE_BASE) base *= pow(factor, rot_dim / (rot_dim - 2.0));
+  // the pair that makes a number of turns within trained_len positions
+  auto pair_of = [&](double turns) { return rot_dim * log(trained_len / (turns * two_pi)) / (2.0 * log(base)); };
+  double lo = 0.0, hi = 1.0;
+  if (kind == CK_ROPE_RAMP) {
+    lo = fmax(floor(pair_of(fast)), 0.0);
+    hi = fmin(ceil(pair_of(slow)), rot_dim - 1.0);
+  }
+  for (int j = 0; j < rot_dim / 2; ++j) {
+    const double w = pow(base, -2.0 * j / rot_dim);
+    double f = w;
+    if (kind == CK_ROPE_LINEAR) f = w / factor;
+    if (kind == CK_ROPE_RAMP) {
+      const double ramp = fmin(fmax((j - lo) / fmax(hi - lo, 1e-3), 0.0), 1.0);
+      f = w / factor * ramp + w * (1.0 - ramp);
+    }
+    if (kind == CK_ROPE_BANDS) {
+      const double keep = fmin(fmax((trained_len * w / two_pi - slow) / (fast - slow), 0.0), 1.0);
+      f = (1.0 - keep) * w / factor + keep * w;
+    }
+    freqs[j] = (float)f;
+  }
+  *attn_factor = kind == CK_ROPE_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  return CK_OK;
+}
+
+int ck_rope_append(const ck_shape* sh, const void* q, const void* k, const void* v,
+                   int64_t q_stride, int64_t k_stride, int64_t v_stride, int64_t n_rows,
+                   const int32_t* q_starts, const int32_t* lengths, const int32_t* positions,
+                   const float* freqs, int32_t rot_dim, float attn_factor, uint32_t flags,
+                   void* q_out, const ck_paged_kv* kv, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if ((rc = check_rows(n_rows))) return rc;
+  if (!q_starts && n_rows != sh->S)
+    return fail(CK_EINVALID, "n_rows=%lld without q_starts: one token for each of the %d sequences",
+                (long long)n_rows, sh->S);
+  if (rot_dim < 2 || rot_dim > ck::D || rot_dim % 2 != 0)
+    return fail(CK_EINVALID, "rot_dim=%d must be even and in [2, %d]", rot_dim, ck::D);
+  if (flags > CK_ROPE_ADJACENT) return fail(CK_EINVALID, "unknown flags 0x%x", flags);
+  if (!isfinite(attn_factor)) return fail(CK_EINVALID, "attn_factor is not finite");
+  if (!q != !q_out) return fail(CK_EINVALID, "q and q_out must be given together");
+  if (q) {
+    if ((rc = check_token_rows("q", q, q_stride, dm.Hq, dm))) return rc;
+    CK_REQUIRE_PTR(q_out);
+    if (q == q_out && q_stride != (int64_t)dm.Hq * ck::D)
+      return fail(CK_EINVALID, "q_out is q, whose rows are not dense");
+  }
+  if ((rc = check_token_rows("k", k, k_stride, dm.Hkv, dm))) return rc;
+  if ((rc = check_token_rows("v", v, v_stride, dm.Hkv, dm))) return rc;
+  CK_OPTIONAL_PTR(q_starts);
+  CK_REQUIRE_PTR(lengths);
+  CK_OPTIONAL_PTR(positions);
+  CK_REQUIRE_PTR(freqs);
+  if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
+  return hip_result(ck::launch_rope_append(dm, q, k, v, q_stride, k_stride, v_stride, n_rows, q_starts,
+                                           lengths, positions, freqs, rot_dim, attn_factor,
+                                           flags == CK_ROPE_ADJACENT, q_out, *kv, (hipStream_t)stream),
+                    "rotary append launch");
+}
+
+int ck_paged_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* kv,
+                         const int32_t* lengths, int64_t n_sink, int64_t window,
+                         const int32_t* token_idx, const int32_t* n_tokens, int32_t idx_stride,
+                         int32_t max_tokens, float softmax_scale, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (n_sink < 0) return fail(CK_EINVALID, "n_sink=%lld is negative", (long long)n_sink);
+  if (!token_idx != !n_tokens) return fail(CK_EINVALID, "token_idx and n_tokens must be given together");
+  if (n_tokens) {
+    if (window < 0) return fail(CK_EINVALID, "a list needs a window: without one every row is attended already");
+    if (max_tokens < 0 || idx_stride < max_tokens)
+      return fail(CK_EINVALID, "max_tokens=%d outside [0, idx_stride=%d]", max_tokens, idx_stride);
+    if (max_tokens > 1 << 30) return fail(CK_EUNSUPPORTED, "attended set too large");
+  }
+  if (!(softmax_scale > 0.f)) return fail(CK_EINVALID, "softmax_scale must be positive");
+  CK_REQUIRE_PTR(q);
+  CK_REQUIRE_PTR(lengths);
+  CK_REQUIRE_PTR(out);
+  CK_OPTIONAL_PTR(token_idx);
+  CK_OPTIONAL_PTR(n_tokens);
+  if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
+  const size_t need = ck::paged_workspace_bytes(dm);
+  if (!workspace) return fail(CK_EWORKSPACE, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(CK_EMISALIGNED, "workspace is not 16-byte aligned");
+  if (workspace_bytes < need)
+    return fail(CK_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  return hip_result(ck::launch_paged_attn(dm, q, *kv, lengths, n_sink, window, token_idx, n_tokens, idx_stride,
+                                          max_tokens, softmax_scale, out, workspace, (hipStream_t)stream),
+                    "paged attention launch");
+}
+
+int ck_prompt_attn(const ck_shape* sh, const void* q, int64_t n_rows, const int32_t* q_starts,
+                   const ck_paged_kv* kv, const int32_t* lengths, int64_t n_sink, int64_t window,
+                   float softmax_scale, void* out, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (dm.dtype != CK_BF16) return fail(CK_EUNSUPPORTED, "prompt attention runs on bf16 only");
+  if ((rc = check_rows(n_rows))) return rc;
+  if (n_rows * dm.Hq > (int64_t)1 << 30) return fail(CK_EUNSUPPORTED, "more than 2^30 query rows in one call");
+  if (n_sink < 0) return fail(CK_EINVALID, "n_sink=%lld is negative", (long long)n_sink);
+  if (!(softmax_scale > 0.f)) return fail(CK_EINVALID, "softmax_scale must be positive");
+  CK_REQUIRE_PTR(q);
+  CK_REQUIRE_PTR(q_starts);
+  CK_REQUIRE_PTR(lengths);
+  CK_REQUIRE_PTR(out);
+  if (q == out) return fail(CK_EINVALID, "out is q");
+  if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
+  const size_t need = ck::prompt_workspace_bytes(dm, n_rows);
+  if (!workspace) return fail(CK_EWORKSPACE, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(CK_EMISALIGNED, "workspace is not 16-byte aligned");
+  if (workspace_bytes < need)
+    return fail(CK_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  return hip_result(ck::launch_prompt_attn(dm, q, n_rows, q_starts, *kv, lengths, n_sink, window, softmax_scale,
+                                           out, workspace, (hipStream_t)stream),
+                    "prompt attention launch");
+}
+
+int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* dst,
+                 const int32_t* n_copy, int32_t max_rows, const int32_t* row_idx,
+                 int32_t idx_stride, const int32_t* begin, const int32_t* src_seq, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (max_rows < 1) return fail(CK_EINVALID, "max_rows=%d must be positive", max_rows);
+  if (max_rows > 1 << 28) return fail(CK_EUNSUPPORTED, "max_rows=%d (at most %d)", max_rows, 1 << 28);
+  if (row_idx && idx_stride < max_rows)
+    return fail(CK_EINVALID, "idx_stride=%d smaller than max_rows=%d", idx_stride, max_rows);
+  CK_REQUIRE_PTR(n_copy);
+  CK_OPTIONAL_PTR(row_idx);
+  CK_OPTIONAL_PTR(begin);
+  CK_OPTIONAL_PTR(src_seq);
+  if ((rc = check_paged(src, "src", dm, src_seq ? 1 : dm.S))) return rc;
+  if ((rc = check_paged(dst, "dst", dm, dm.S))) return rc;
+  return hip_result(ck::launch_copy_rows(dm, *src, *dst, n_copy, max_rows, row_idx, idx_stride, begin, src_seq,
+                                         (hipStream_t)stream),
+                    "row copy launch");
 }
 
 int ck_probe_mfma_bf16(int32_t n_workgroups, int32_t iters, const void* operands,

@@ -238,6 +238,7 @@ struct Dims {
 };
 
 
+constexpr int64_t MAX_NEW_ROWS = 1 << 24;    // token rows of one call on a ragged batch
 constexpr int CHUNK_RUNS_MAX = 512;         // chunks per head-problem the update walks (LDS: 2 words each)
 constexpr int KM_SMALL_MAX_TOKENS = 384;    // token ranges up to this size (and up to
 constexpr int KM_SMALL_MAX_CLUSTERS = 8;    // this many clusters) are clustered by one kernel
@@ -380,6 +381,24 @@ hipError_t launch_cached_step(const Dims& dm, const void* q, const void* centroi
                               int32_t* sel_clusters, int32_t* n_sel_clusters,
                               int32_t* n_sel_tokens, const CacheArgs& cache, void* out,
                               void* workspace, hipStream_t st);
+// caches in pages
+hipError_t launch_rope_append(const Dims& dm, const void* q, const void* k, const void* v, int64_t q_stride,
+                              int64_t k_stride, int64_t v_stride, int64_t n_rows, const int32_t* q_starts,
+                              const int32_t* lengths, const int32_t* positions, const float* freqs, int rot_dim,
+                              float attn_factor, bool adjacent, void* q_out, const ck_paged_kv& kv,
+                              hipStream_t st);
+hipError_t launch_copy_rows(const Dims& dm, const ck_paged_kv& src, const ck_paged_kv& dst, const int32_t* n_copy,
+                            int max_rows, const int32_t* row_idx, int idx_stride, const int32_t* begin,
+                            const int32_t* src_seq, hipStream_t st);
+size_t paged_workspace_bytes(const Dims& dm);
+hipError_t launch_paged_attn(const Dims& dm, const void* q, const ck_paged_kv& kv, const int32_t* lengths,
+                             int64_t n_sink, int64_t window, const int32_t* token_idx, const int32_t* n_tokens,
+                             int idx_stride, int max_tokens, float softmax_scale, void* out, void* workspace,
+                             hipStream_t st);
+size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows);
+hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
+                              const ck_paged_kv& kv, const int32_t* lengths, int64_t n_sink, int64_t window,
+                              float softmax_scale, void* out, void* workspace, hipStream_t st);
 // evaluation helpers
 hipError_t launch_row_scores(const Dims& dm, const void* q, const void* table,
                              int64_t table_stride, int64_t row_begin, int n_rows, float* scores,

@@ -1,0 +1,97 @@
+// Rows of K and V from one cache to another: paged or contiguous, whole or by a list per KV head.
+// Bound by memory: every row is read and written once.  A row of 256 (bf16) or 512 (fp32) bytes goes
+// through 16 or 32 lanes; a wavefront has several rows of K and of V under way.
+#include "paged.hpp"
+
+namespace ck {
+
+namespace {
+
+struct CopyArgs {
+  const void *K, *V;
+  void *K2, *V2;
+  Pages src, dst;
+  const int32_t *n_copy, *row_idx, *begin, *src_seq;
+  int Hkv, max_rows, idx_stride;
+};
+
+constexpr int COPY_ROWS = 64;                           // of a workgroup: 16 of each wavefront
+
+template <int LANES>                                    // of 16 bytes for a row
+__global__ __launch_bounds__(256) void k_copy_rows(const CopyArgs a) {
+  const int hp = blockIdx.y, s = hp / a.Hkv, h = hp % a.Hkv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int n = a.n_copy[s];
+  n = n < a.max_rows ? n : a.max_rows;
+  const int j0 = blockIdx.x * COPY_ROWS + wave * 16;
+  if (j0 >= n) return;
+  const int from_seq = a.src_seq ? a.src_seq[s] : s;
+  if ((uint32_t)from_seq >= (uint32_t)a.src.n_seqs) return;
+  const int begin = a.begin ? a.begin[s] : 0;
+  // lane x < 16 finds out where row j0 + x comes from and goes to
+  const int j = j0 + (lane & 15);
+  int from = -1, to = -1;
+  if (j < n) {
+    const int64_t r = (int64_t)begin + j;
+    const int rd = r >= 0 && r < 0x7FFFFFFF ? (int)r : -1;
+    const int rs = a.row_idx ? a.row_idx[(int64_t)hp * a.idx_stride + j] : rd;
+    to = a.dst.row(s, h, rd);
+    from = a.src.row(from_seq, h, rs);
+    if (to < 0 || from < 0) from = to = -1;
+  }
+  constexpr int PER = 64 / LANES;                       // rows a wavefront moves with one instruction
+  constexpr int U = 16 / PER;
+  const int part = lane % LANES, sub = lane / LANES;
+  const uint4 *K = static_cast<const uint4*>(a.K), *V = static_cast<const uint4*>(a.V);
+  uint4 *K2 = static_cast<uint4*>(a.K2), *V2 = static_cast<uint4*>(a.V2);
+  constexpr int B = U < 4 ? U : 4;
+#pragma unroll
+  for (int u0 = 0; u0 < U; u0 += B) {
+    uint4 k[B], v[B];
+    int t[B];
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int x = (u0 + u) * PER + sub;
+      const int f = __shfl(from, x);
+      t[u] = __shfl(to, x);
+      if (t[u] < 0) continue;
+      k[u] = K[(int64_t)f * LANES + part];
+      v[u] = V[(int64_t)f * LANES + part];
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      if (t[u] < 0) continue;
+      K2[(int64_t)t[u] * LANES + part] = k[u];
+      V2[(int64_t)t[u] * LANES + part] = v[u];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_copy_rows(const Dims& dm, const ck_paged_kv& src, const ck_paged_kv& dst, const int32_t* n_copy,
+                            int max_rows, const int32_t* row_idx, int idx_stride, const int32_t* begin,
+                            const int32_t* src_seq, hipStream_t st) {
+  CopyArgs a = {};
+  a.K = src.K;
+  a.V = src.V;
+  a.K2 = dst.K;
+  a.V2 = dst.V;
+  a.src = Pages(src, dm.Hkv);
+  a.dst = Pages(dst, dm.Hkv);
+  a.n_copy = n_copy;
+  a.row_idx = row_idx;
+  a.begin = begin;
+  a.src_seq = src_seq;
+  a.Hkv = dm.Hkv;
+  a.max_rows = max_rows;
+  a.idx_stride = idx_stride;
+  const dim3 grid((unsigned)((max_rows + COPY_ROWS - 1) / COPY_ROWS), (unsigned)dm.HP);
+  if (dm.dtype == CK_BF16)
+    hipLaunchKernelGGL(k_copy_rows<16>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(k_copy_rows<32>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace ck
