@@ -18,7 +18,7 @@ namespace ck {
 namespace {
 
 constexpr float PR_NEG_BIG = -1.0e30f;
-constexpr int PR_WAVES = 4;
+constexpr int PR_WAVES = 8;
 constexpr int PR_ROWS = PR_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int PR_TILE = 64;                             // cache rows of a tile
 
@@ -74,13 +74,36 @@ struct QueryBlock {
 // one of the two bf16 of a word is infinite or not a number
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
-template <int G>
-__global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_attn(const PromptArgs a) {
-  __shared__ __attribute__((aligned(16))) uint4 k_lds[PR_TILE * 16], v_lds[PR_TILE * 16];
-  __shared__ __attribute__((aligned(8))) uint16_t hole_lds[4];
+// 16 bytes for every lane from base + offset to LDS at `to` + 16 * lane, on their way when this returns:
+// they are counted with the vector loads (wait_for_tiles).
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void group_barrier() {       // LDS writes of this wavefront are done before it
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page.
+template <int G, bool EIGHTS>
+__global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
+  constexpr int TILE_BYTES = PR_TILE * D * 2;           // of K; V follows
+  __shared__ __attribute__((aligned(1024))) char tiles[2][2 * TILE_BYTES];
+  __shared__ __attribute__((aligned(8))) uint8_t hole_lds[2][8];   // bit r: row r of the tile is not there
   __shared__ int odd_lds[PR_WAVES];                     // a value of the wavefront's rows is not finite
+  static_assert(PR_WAVES == 8 && PR_TILE == 64, "eight rows of a tile for each wavefront");
   constexpr int TOKENS = PR_ROWS / G;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.x % a.Hkv;
   QueryBlock qb;
   if (!qb.find(a, blockIdx.x / a.Hkv, TOKENS)) return;
@@ -99,7 +122,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_attn(const PromptArgs 
   for (int sl = 0; sl < 8; ++sl)
     q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.q + q_at + sl * 16 + half * 8));
   const int p = there ? p0 + my_tok : -1;               // last row that the lane's query sees
-  const int p_lo = p0 + wave * 32 / G;                  // first query of the wavefront
+  const int p_lo = p0 + wave * 32 / G, p_hi = min(p0 + (wave * 32 + 31) / G, p_last);   // of the wavefront
 
   // ---- the tiles: those of the sinks, then from the first row of the first window on ----
   const int end = p_last + 1 < 0 ? 0 : p_last + 1;      // <= length
@@ -110,88 +133,140 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_attn(const PromptArgs 
   if (a.window >= 0) first_tile = a.window == 0 ? last_tile : max(0, p0 - a.window + 1) / PR_TILE;
   first_tile = max(first_tile, sink_tiles);
   const int n_tiles = sink_tiles + max(0, last_tile - first_tile);
+  auto first_row = [&](int nth) { return (nth < sink_tiles ? nth : first_tile + (nth - sink_tiles)) * PR_TILE; };
 
   floatx16 acc[4];
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-  float m = PR_NEG_BIG, l = 0.f;                        // l: of this lane's rows
+  float m = PR_NEG_BIG, l = 0.f;                        // of the unscaled scores; l: of this lane's rows
 
-  // what this lane brings of a tile: pieces lane % 16 of rows 16 wave + 4 i + lane / 16
-  uint4 kr[4], vr[4];
-  uint32_t holes = 0;                                   // of the wavefront's 16 rows
-  auto load = [&](int nth) {
-    const int tile = nth < sink_tiles ? nth : first_tile + (nth - sink_tiles);
-    holes = 0;
+  // ---- bringing tiles: this wavefront rows 8 wave + 4 i + lane / 16, pieces lane % 16 ----
+  constexpr int LOOKUPS = EIGHTS ? 1 : 2;
+  int page[LOOKUPS], slot[LOOKUPS];                     // of the tile after the next
+  auto look_up = [&](int nth) {
+    const int r0 = first_row(nth) + wave * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = tile * PR_TILE + wave * 16 + i * 4 + (lane >> 4);
-      const int at = r < end ? a.pages.row(qb.s, h, r) : -1;
-      const uint64_t none = __ballot(at < 0);
-      holes |= (uint32_t)((none & 1) | ((none >> 16) & 1) << 1 | ((none >> 32) & 1) << 2 | ((none >> 48) & 1) << 3) << (4 * i);
-      kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-      if (at >= 0) {
-        kr[i] = *reinterpret_cast<const uint4*>(a.K + (int64_t)at * D + (lane & 15) * 8);
-        vr[i] = *reinterpret_cast<const uint4*>(a.V + (int64_t)at * D + (lane & 15) * 8);
+    for (int i = 0; i < LOOKUPS; ++i) {
+      const int r = EIGHTS ? r0 : r0 + 4 * i + (lane >> 4);
+      page[i] = -1;
+      slot[i] = 0;
+      if (nth < n_tiles && r < end) {
+        const int e = a.pages.size.quotient(r);
+        page[i] = a.pages.table[(int64_t)qb.s * a.pages.per_seq + e];
+        slot[i] = r - e * (int)a.pages.size.d;
       }
     }
   };
-  if (n_tiles > 0) load(0);
-  for (int nth = 0; nth < n_tiles; ++nth) {
-    const int tile = nth < sink_tiles ? nth : first_tile + (nth - sink_tiles);
-    const int r0 = tile * PR_TILE;
-    __syncthreads();                                    // the tile before has been read
-    uint32_t odd = 0;
+  uint32_t piece[2];                                    // where in 4 rows the lane's piece stands
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = wave * 16 + i * 4 + (lane >> 4), at = r * 16 + ((lane & 15) ^ swizzle(r));
-      k_lds[at] = kr[i];
-      v_lds[at] = vr[i];
-      odd |= not_finite(vr[i].x) | not_finite(vr[i].y) | not_finite(vr[i].z) | not_finite(vr[i].w);
+  for (int i = 0; i < 2; ++i) {
+    const int sub = lane >> 4, r = wave * 8 + 4 * i + sub;
+    piece[i] = (EIGHTS ? (4 * i + sub) * 256 : 0) + ((lane & 15) ^ swizzle(r)) * 16;
+  }
+  const uint32_t lds0 = lds_address(tiles) + wave * 8 * 256;
+  auto bring = [&](int buf) {
+    const uint32_t to = lds0 + buf * 2 * TILE_BYTES;
+    uint32_t holes;
+    if constexpr (EIGHTS) {
+      const int at = __builtin_amdgcn_readfirstlane(a.pages.place(page[0], h, slot[0]));
+      holes = at < 0 ? 0xFFu : 0u;
+      const char* K = reinterpret_cast<const char*>(a.K) + (int64_t)max(at, 0) * (D * 2);
+      const char* V = reinterpret_cast<const char*>(a.V) + (int64_t)max(at, 0) * (D * 2);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        load_to_lds(K, piece[i], to + i * 1024);
+        load_to_lds(V, piece[i], to + i * 1024 + TILE_BYTES);
+      }
+    } else {
+      holes = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = a.pages.place(page[i], h, slot[i]);
+        const uint64_t none = __ballot(at < 0);
+        holes |= (uint32_t)((none & 1) | ((none >> 16) & 1) << 1 | ((none >> 32) & 1) << 2 | ((none >> 48) & 1) << 3) << (4 * i);
+        const int64_t from = (int64_t)max(at, 0) * (D * 2) + piece[i];
+        load_to_lds(reinterpret_cast<const char*>(a.K) + from, to + i * 1024);
+        load_to_lds(reinterpret_cast<const char*>(a.V) + from, to + i * 1024 + TILE_BYTES);
+      }
     }
-    const bool odd_rows = __ballot(odd != 0) != 0;
-    if (lane == 0) {
-      hole_lds[wave] = (uint16_t)holes;
-      odd_lds[wave] = odd_rows;
+    if (lane == 0) hole_lds[buf][wave] = (uint8_t)holes;
+  };
+
+  // where this lane reads: K row `col`, pieces 2 sl + half; V rows 4 half + (lane / 4) % 4, see below
+  const int rr = (lane >> 2) & 3;
+  const uint32_t k_at = lds_address(tiles) + col * 256 + (half ^ swizzle(col)) * 16;
+  const uint32_t v_at = lds_address(tiles) + TILE_BYTES + (4 * half + rr) * 256 + (lane & 1) * 8 + (rr << 6) +
+                        (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) << 4);
+
+  if (n_tiles > 0) {
+    look_up(0);
+    bring(0);
+    look_up(1);
+  }
+  for (int nth = 0; nth < n_tiles; ++nth) {
+    const int buf = nth & 1, r0 = first_row(nth);
+    wait_for_tiles();
+    group_barrier();
+    if (nth + 1 < n_tiles) {
+      bring(buf ^ 1);
+      look_up(nth + 2);
     }
-    __syncthreads();
-    if (nth + 1 < n_tiles) load(nth + 1);
-    const uint64_t gone = *reinterpret_cast<const uint64_t*>(hole_lds);
-    const bool whole = gone == 0 && r0 + PR_TILE <= p_lo + 1 &&
-                       (a.window < 0 || r0 + PR_TILE <= n_sink || r0 > p_last - a.window);
+    const uint64_t gone = *reinterpret_cast<const uint64_t*>(hole_lds[buf]);
+    const bool open = gone == 0 && (a.window < 0 || r0 + PR_TILE <= n_sink || r0 > p_last - a.window);
+    bool odd = false;
+    if (!(open && r0 + PR_TILE <= p0 + 1)) {            // some row is masked for some query of the workgroup
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 w = *reinterpret_cast<const uint4*>(tiles[buf] + TILE_BYTES + wave * 8 * 256 + i * 1024 + lane * 16);
+        bad |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
+      }
+      const bool any = __ballot(bad != 0) != 0;
+      if (lane == 0) odd_lds[wave] = any;
+      group_barrier();
+#pragma unroll
+      for (int w = 0; w < PR_WAVES; ++w) odd |= odd_lds[w] != 0;
+    }
+    const bool whole = open && r0 + PR_TILE <= p_lo + 1;
+    if (r0 > p_hi || (a.window >= 0 && r0 >= n_sink && r0 + PR_TILE <= p_lo - a.window + 1)) continue;
 
     // ---- S^T ----
     floatx16 sc[2];
+    const uint32_t kb = k_at + buf * 2 * TILE_BYTES;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
-      const int r = b * 32 + col;
 #pragma unroll
       for (int sl = 0; sl < 8; ++sl) {
-        const bf16x8 k = __builtin_bit_cast(bf16x8, k_lds[r * 16 + ((2 * sl + half) ^ swizzle(r))]);
+        const bf16x8 k = *(lds_bf16x8*)(uintptr_t)((kb ^ (sl << 5)) + b * 32 * 256);
         sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[sl], sc[b], 0, 0, 0);
       }
     }
     // ---- softmax ----
+    if (!whole) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int rt = b * 32 + 8 * (i >> 2) + 4 * half + (i & 3), r = r0 + rt;
+          const bool seen = r <= p && (a.window < 0 || r < n_sink || r > p - a.window) && !((gone >> rt) & 1);
+          sc[b][i] = seen ? sc[b][i] : -INFINITY;
+        }
+    }
     float mx = PR_NEG_BIG;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float x = sc[b][i] * a.scale_log2e;
-        if (!whole) {
-          const int rt = b * 32 + 8 * (i >> 2) + 4 * half + (i & 3), r = r0 + rt;
-          const bool seen = r <= p && (a.window < 0 || r < n_sink || r > p - a.window) && !((gone >> rt) & 1);
-          x = seen ? x : -INFINITY;
-        }
-        sc[b][i] = x;
-        mx = fmaxf(mx, x);
-      }
-    mx = fmaxf(xor32(mx, OpMax()), m);
-    const float corr = __builtin_amdgcn_exp2f(m - mx);
-    if (__ballot(corr != 1.f)) {
+      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[b][i]), sc[b][i + 1]);
+    mx = xor32(mx, OpMax());
+    // The maximum in use may be smaller than the true one by 8 powers of two: probabilities are relative to
+    // each other, and up to 256 they are as exact as up to 1.
+    if (__ballot((mx - m) * a.scale_log2e > 8.f)) {
+      mx = fmaxf(mx, m);
+      const float corr = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -199,57 +274,61 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_attn(const PromptArgs 
       l *= corr;
       m = mx;
     }
-    bf16x8 pb[4];                                       // slab s of 16 rows
+    const float mc = m * a.scale_log2e;
+    uint4 pb[4];                                        // slab s of 16 rows
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = __builtin_amdgcn_exp2f(sc[b][i] - m);
-        l += e;
-        pb[2 * b + (i >> 3)][i & 7] = (bf16)e;
+      for (int i = 0; i < 16; i += 2) {
+        bf16x2 e;
+        e[0] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale_log2e, -mc));
+        e[1] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[b][i + 1], a.scale_log2e, -mc));
+        const bf16x2 one = {(bf16)1.f, (bf16)1.f};
+        l = __builtin_amdgcn_fdot2_f32_bf16(e, one, l, false);   // what the product takes is what is summed
+        reinterpret_cast<uint32_t*>(&pb[2 * b + (i >> 3)])[(i & 7) >> 1] = __builtin_bit_cast(uint32_t, e);
       }
     // ---- O^T ----
-    const bool careful = !whole && (odd_lds[0] | odd_lds[1] | odd_lds[2] | odd_lds[3]);
+    const uint32_t vb = v_at + buf * 2 * TILE_BYTES;
+    auto values = [&](int c, int s) {
+      // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6)) + s * 4096));
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6) ^ 32) + s * 4096 + 2048));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    typedef short shortx8 __attribute__((ext_vector_type(8)));
+    if (whole || !odd) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+      for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
-        shortx4 part[2];
+        for (int c = 0; c < 4; ++c)
+          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(c, s)),
+                                                           __builtin_bit_cast(bf16x8, pb[s]), acc[c], 0, 0, 0);
+      continue;
+    }
+    // A value that is not finite reaches only the queries that see its row: it is taken out of the product
+    // (zero times it would be a NaN for the others) and added where its probability is not zero.
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int r = 16 * s + 8 * u + 4 * half + ((lane >> 2) & 3);
-          const int piece = (4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swizzle(r);
-          char* at = reinterpret_cast<char*>(v_lds) + r * 256 + piece * 16 + (lane & 1) * 8;
-          part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)at);
-        }
-        typedef short shortx8 __attribute__((ext_vector_type(8)));
-        shortx8 v = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-        if (careful) {
-          // A value that is not finite reaches only the queries that see its row: it is taken out of the
-          // product (zero times it would be a NaN for the others) and added where its probability is not zero.
-          shortx8 kind[3];
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const shortx8 v = values(c, s);
+        const float what[4] = {0.f, INFINITY, -INFINITY, NAN};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          shortx8 x;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const uint16_t w = (uint16_t)v[e];
-            const bool odd_value = (w & 0x7F80u) == 0x7F80u, inf = (w & 0x7FFFu) == 0x7F80u;
-            kind[0][e] = inf && !(w >> 15) ? 0x3F80 : 0;
-            kind[1][e] = inf && (w >> 15) ? 0x3F80 : 0;
-            kind[2][e] = odd_value && !inf ? 0x3F80 : 0;
-            v[e] = odd_value ? 0 : v[e];
+            const int kind = (w & 0x7F80u) != 0x7F80u ? 0 : ((w & 0x7Fu) ? 3 : 1 + (w >> 15));
+            x[e] = k == 0 ? (kind == 0 ? (short)w : 0) : (kind == k ? 0x3F80 : 0);
           }
-          const float what[3] = {INFINITY, -INFINITY, NAN};
+          floatx16 z;
 #pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            floatx16 z;
+          for (int i = 0; i < 16; ++i) z[i] = k == 0 ? acc[c][i] : 0.f;
+          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, pb[s]), z, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[i] = 0.f;
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kind[k]), pb[s], z, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c][i] = z[i] > 0.f ? acc[c][i] + what[k] : acc[c][i];
-          }
+          for (int i = 0; i < 16; ++i) acc[c][i] = k == 0 ? z[i] : (z[i] > 0.f ? acc[c][i] + what[k] : acc[c][i]);
         }
-        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pb[s], acc[c], 0, 0, 0);
       }
   }
 
@@ -264,12 +343,23 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_attn(const PromptArgs 
       uint32_t w[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t lo = __builtin_bit_cast(uint16_t, (bf16)(acc[c][4 * j + 2 * e] * inv));
-        const uint32_t hi = __builtin_bit_cast(uint16_t, (bf16)(acc[c][4 * j + 2 * e + 1] * inv));
-        w[e] = lo | hi << 16;
+        bf16x2 o;
+        o[0] = (bf16)(acc[c][4 * j + 2 * e] * inv);
+        o[1] = (bf16)(acc[c][4 * j + 2 * e + 1] * inv);
+        w[e] = __builtin_bit_cast(uint32_t, o);
       }
       *reinterpret_cast<uint2*>(a.out + q_at + 32 * c + 8 * j + 4 * half) = make_uint2(w[0], w[1]);
     }
+}
+
+template <bool EIGHTS>
+void launch_prompt_g(int G, dim3 grid, dim3 block, const PromptArgs& a, hipStream_t st) {
+  switch (G) {
+    case 1: hipLaunchKernelGGL((k_prompt_attn<1, EIGHTS>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_prompt_attn<2, EIGHTS>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_prompt_attn<4, EIGHTS>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_prompt_attn<8, EIGHTS>), grid, block, 0, st, a); break;
+  }
 }
 
 }  // namespace
@@ -304,12 +394,10 @@ hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, con
   // a block of each sequence may be short
   const int64_t blocks = n_rows / tokens + (n_rows < dm.S ? n_rows : dm.S);
   const dim3 grid((unsigned)(blocks * dm.Hkv)), block(PR_WAVES * 64);
-  switch (dm.G) {
-    case 1: hipLaunchKernelGGL(k_prompt_attn<1>, grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL(k_prompt_attn<2>, grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL(k_prompt_attn<4>, grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL(k_prompt_attn<8>, grid, block, 0, st, a); break;
-  }
+  if (kv.page_size % 8 == 0)
+    launch_prompt_g<true>(dm.G, grid, block, a, st);
+  else
+    launch_prompt_g<false>(dm.G, grid, block, a, st);
   return hipGetLastError();
 }
 
