@@ -11,6 +11,8 @@
 //                 the transposing reads (ds_read_b64_tr_b16) in the same order.  The accumulator has the
 //                 queries in its lanes again, so scaling it is in-lane too.
 // Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
+#include <type_traits>
+
 #include "paged.hpp"
 
 namespace ck {
@@ -93,13 +95,19 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
+// all bits of the halves that are finite
+__device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
+  const uint32_t bad = not_finite(w);
+  return ~(bad | (bad - (bad >> 15)));
+}
+
 // EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page.
 template <int G, bool EIGHTS>
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
   constexpr int TILE_BYTES = PR_TILE * D * 2;           // of K; V follows
   __shared__ __attribute__((aligned(1024))) char tiles[2][2 * TILE_BYTES];
   __shared__ __attribute__((aligned(8))) uint8_t hole_lds[2][8];   // bit r: row r of the tile is not there
-  __shared__ int odd_lds[PR_WAVES];                     // a value of the wavefront's rows is not finite
+  __shared__ __attribute__((aligned(8))) uint8_t odd_lds[8];       // bit r: row r has a value that is not finite
   static_assert(PR_WAVES == 8 && PR_TILE == 64, "eight rows of a tile for each wavefront");
   constexpr int TOKENS = PR_ROWS / G;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
@@ -200,60 +208,68 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   const uint32_t v_at = lds_address(tiles) + TILE_BYTES + (4 * half + rr) * 256 + (lane & 1) * 8 + (rr << 6) +
                         (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) << 4);
 
-  if (n_tiles > 0) {
-    look_up(0);
-    bring(0);
-    look_up(1);
-  }
-  for (int nth = 0; nth < n_tiles; ++nth) {
-    const int buf = nth & 1, r0 = first_row(nth);
-    wait_for_tiles();
-    group_barrier();
-    if (nth + 1 < n_tiles) {
-      bring(buf ^ 1);
-      look_up(nth + 2);
-    }
-    const uint64_t gone = *reinterpret_cast<const uint64_t*>(hole_lds[buf]);
-    const bool open = gone == 0 && (a.window < 0 || r0 + PR_TILE <= n_sink || r0 > p_last - a.window);
-    bool odd = false;
-    if (!(open && r0 + PR_TILE <= p0 + 1)) {            // some row is masked for some query of the workgroup
-      uint32_t bad = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint4 w = *reinterpret_cast<const uint4*>(tiles[buf] + TILE_BYTES + wave * 8 * 256 + i * 1024 + lane * 16);
-        bad |= not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w);
-      }
-      const bool any = __ballot(bad != 0) != 0;
-      if (lane == 0) odd_lds[wave] = any;
-      group_barrier();
-#pragma unroll
-      for (int w = 0; w < PR_WAVES; ++w) odd |= odd_lds[w] != 0;
-    }
-    const bool whole = open && r0 + PR_TILE <= p_lo + 1;
-    if (r0 > p_hi || (a.window >= 0 && r0 >= n_sink && r0 + PR_TILE <= p_lo - a.window + 1)) continue;
-
+  typedef short shortx8 __attribute__((ext_vector_type(8)));
+  // whole: every query of the wavefront sees every row of the tile.  Else gone: rows that are not there, odd: rows
+  // that had a value that is not finite.
+  auto use_tile = [&](bool whole, int buf, int r0, uint64_t gone, uint64_t odd) {
     // ---- S^T ----
     floatx16 sc[2];
-    const uint32_t kb = k_at + buf * 2 * TILE_BYTES;
+    const uint32_t kb = k_at + buf * 2 * TILE_BYTES, vb = v_at + buf * 2 * TILE_BYTES;
+    // four pieces of a K operand, and of V operands, are on their way while four products run
+    auto keys = [&](int g, bf16x8 (&k)[4]) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+      for (int i = 0; i < 4; ++i) k[i] = *(lds_bf16x8*)(uintptr_t)((kb ^ (((g & 1) * 4 + i) << 5)) + (g >> 1) * 32 * 256);
+    };
+    auto values = [&](int s, shortx8 (&v)[4]) {
+      // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
-#pragma unroll
-      for (int sl = 0; sl < 8; ++sl) {
-        const bf16x8 k = *(lds_bf16x8*)(uintptr_t)((kb ^ (sl << 5)) + b * 32 * 256);
-        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[sl], sc[b], 0, 0, 0);
+      for (int c = 0; c < 4; ++c) {
+        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6)) + s * 4096));
+        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6) ^ 32) + s * 4096 + 2048));
+        v[c] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
+    };
+    bf16x8 k[2][4];
+    shortx8 v[2][4];
+    keys(0, k[0]);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g < 3) keys(g + 1, k[(g + 1) & 1]);
+      else values(0, v[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int sl = (g & 1) * 4 + i;
+        if (sl == 0) {
+          floatx16 z;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e] = 0.f;
+          sc[g >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[g & 1][i], q[sl], z, 0, 0, 0);
+        } else {
+          sc[g >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[g & 1][i], q[sl], sc[g >> 1], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
     // ---- softmax ----
+    uint64_t seen = ~0ull;
     if (!whole) {
+      // rows of the tile that the query sees, as bits
+      const int last = p - r0;
+      seen = last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1);
+      if (a.window >= 0) {
+        const int first = p - a.window + 1 - r0, sinks = n_sink - r0;
+        uint64_t near = first <= 0 ? ~0ull : (first > 63 ? 0 : ~0ull << first);
+        near |= sinks <= 0 ? 0 : (sinks > 63 ? ~0ull : (1ull << sinks) - 1);
+        seen &= near;
+      }
+      seen &= ~gone;
+      const uint64_t mine = seen >> (4 * half);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int rt = b * 32 + 8 * (i >> 2) + 4 * half + (i & 3), r = r0 + rt;
-          const bool seen = r <= p && (a.window < 0 || r < n_sink || r > p - a.window) && !((gone >> rt) & 1);
-          sc[b][i] = seen ? sc[b][i] : -INFINITY;
+          const uint32_t bit = 1u << (8 * (i >> 2) + (i & 3));
+          sc[b][i] = ((uint32_t)(mine >> (32 * b)) & bit) ? sc[b][i] : -INFINITY;
         }
     }
     float mx = PR_NEG_BIG;
@@ -275,7 +291,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       m = mx;
     }
     const float mc = m * a.scale_log2e;
-    uint4 pb[4];                                        // slab s of 16 rows
+    uint32_t pb[4][4];                                  // slab s of 16 rows
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -285,51 +301,83 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
         e[1] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[b][i + 1], a.scale_log2e, -mc));
         const bf16x2 one = {(bf16)1.f, (bf16)1.f};
         l = __builtin_amdgcn_fdot2_f32_bf16(e, one, l, false);   // what the product takes is what is summed
-        reinterpret_cast<uint32_t*>(&pb[2 * b + (i >> 3)])[(i & 7) >> 1] = __builtin_bit_cast(uint32_t, e);
+        pb[2 * b + (i >> 3)][(i & 7) >> 1] = __builtin_bit_cast(uint32_t, e);
       }
     // ---- O^T ----
-    const uint32_t vb = v_at + buf * 2 * TILE_BYTES;
-    auto values = [&](int c, int s) {
-      // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
-      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6)) + s * 4096));
-      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6) ^ 32) + s * 4096 + 2048));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    typedef short shortx8 __attribute__((ext_vector_type(8)));
-    if (whole || !odd) {
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) values(s + 1, v[(s + 1) & 1]);
+      const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(pb[s][0], pb[s][1], pb[s][2], pb[s][3]));
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(c, s)),
-                                                           __builtin_bit_cast(bf16x8, pb[s]), acc[c], 0, 0, 0);
-      continue;
+      for (int c = 0; c < 4; ++c)
+        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[s & 1][c]), pr, acc[c], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // A value that is not finite reaches only the queries that see its row: it is taken out of the product
-    // (zero times it would be a NaN for the others) and added where its probability is not zero.
+    // The values that have been taken out of the tile reach the queries that see their rows.
+    for (uint64_t rows = odd; rows; rows &= rows - 1) { // uniform
+      const int r = __builtin_ctzll(rows);
+      const bool here = (seen >> r) & 1;
+      const int at = a.pages.row(qb.s, h, r0 + r);
+      if (at < 0 || !here) continue;
+      const uint2* from = reinterpret_cast<const uint2*>(a.V + (int64_t)at * D) + half;
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const shortx8 v = values(c, s);
-        const float what[4] = {0.f, INFINITY, -INFINITY, NAN};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          shortx8 x;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const uint16_t w = (uint16_t)v[e];
-            const int kind = (w & 0x7F80u) != 0x7F80u ? 0 : ((w & 0x7Fu) ? 3 : 1 + (w >> 15));
-            x[e] = k == 0 ? (kind == 0 ? (short)w : 0) : (kind == k ? 0x3F80 : 0);
-          }
-          floatx16 z;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[i] = k == 0 ? acc[c][i] : 0.f;
-          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, pb[s]), z, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c][i] = k == 0 ? z[i] : (z[i] > 0.f ? acc[c][i] + what[k] : acc[c][i]);
+        for (int j = 0; j < 4; ++j) {                   // channels 32 c + 8 j + 4 half + (0..3)
+          const uint2 w = from[8 * c + 2 * j];
+          const uint32_t x = w.x & ~finite_mask(w.x), y = w.y & ~finite_mask(w.y);   // the others: 0
+          acc[c][4 * j] += lo_bf16(x);
+          acc[c][4 * j + 1] += hi_bf16(x);
+          acc[c][4 * j + 2] += lo_bf16(y);
+          acc[c][4 * j + 3] += hi_bf16(y);
         }
+    }
+  };
+
+  __builtin_amdgcn_s_waitcnt(0);                        // the queries: no wait for them inside the loop
+  if (n_tiles > 0) {
+    look_up(0);
+    bring(0);
+    look_up(1);
+  }
+  for (int nth = 0; nth < n_tiles; ++nth) {
+    const int buf = nth & 1, r0 = first_row(nth);
+    wait_for_tiles();
+    group_barrier();
+    if (nth + 1 < n_tiles) {
+      bring(buf ^ 1);
+      look_up(nth + 2);
+    }
+    uint64_t gone = *reinterpret_cast<const uint64_t*>(hole_lds[buf]);
+    gone = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)gone) |
+           (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(gone >> 32)) << 32;
+    const bool open = gone == 0 && (a.window < 0 || r0 + PR_TILE <= n_sink || r0 > p_last - a.window);
+    uint64_t odd = 0;
+    if (!(open && r0 + PR_TILE <= p0 + 1)) {
+      // Some row is masked for some query of the workgroup.  A value that is not finite may reach only the queries
+      // that see its row, and zero times it would be a NaN for the others: it leaves the tile.
+      uint32_t rows = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint4* at = reinterpret_cast<uint4*>(tiles[buf] + TILE_BYTES + wave * 8 * 256 + i * 1024 + lane * 16);
+        const uint4 w = *at;
+        const bool bad = (not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w)) != 0;
+        const uint64_t some = __ballot(bad);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) rows |= ((some >> (16 * u)) & 0xFFFF ? 1u : 0u) << (4 * i + u);
+        if (bad) *at = make_uint4(w.x & finite_mask(w.x), w.y & finite_mask(w.y), w.z & finite_mask(w.z), w.w & finite_mask(w.w));
       }
+      if (lane == 0) odd_lds[wave] = (uint8_t)rows;
+      group_barrier();
+      odd = *reinterpret_cast<const uint64_t*>(odd_lds);
+      odd = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)odd) |
+            (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(odd >> 32)) << 32;
+    }
+    const bool whole = open && r0 + PR_TILE <= p_lo + 1;
+    if (r0 > p_hi || (a.window >= 0 && r0 >= n_sink && r0 + PR_TILE <= p_lo - a.window + 1)) continue;
+
+    use_tile(whole, buf, r0, gone, odd & ~gone);
   }
 
   // ---- out: channels 32 c + 8 (i / 4) + 4 half + i % 4 of row `col` ----
