@@ -1,6 +1,6 @@
 // Causal attention of many new tokens over a paged cache, in full or over sinks and a window.
 //
-// Bound by the matrix cores: 4 d operations for every pair of query and row.  A workgroup takes 128 query
+// Bound by the matrix cores: 4 d operations for every pair of query and row.  A workgroup takes 256 query
 // rows of one KV head: token by token, the G heads of the group beside each other, so that they share the
 // K and V tiles and few tokens still fill it.  A wavefront has 32 of these rows.  Per tile of 64 cache rows:
 //   S^T = K Q^T   (v_mfma_f32_32x32x16_bf16, K from LDS as A, the queries in registers as B):
@@ -11,8 +11,6 @@
 //                 the transposing reads (ds_read_b64_tr_b16) in the same order.  The accumulator has the
 //                 queries in its lanes again, so scaling it is in-lane too.
 // Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
-#include <type_traits>
-
 #include "paged.hpp"
 
 namespace ck {
@@ -23,26 +21,36 @@ constexpr float PR_NEG_BIG = -1.0e30f;
 constexpr int PR_WAVES = 8;
 constexpr int PR_ROWS = PR_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int PR_TILE = 64;                             // cache rows of a tile
+constexpr int PR_MIN_TILES = 4;                         // of a piece
+constexpr int PR_CUS = 256;
+constexpr int PR_BUFFERS = 3;                           // tiles of keys, and of values, in LDS
 
 struct PromptArgs {
   const bf16 *q, *K, *V;
   bf16* out;
+  float* part;                                          // [blocks, Hkv, n_split] partials, see Partial
   const int32_t *starts, *lengths;
   Pages pages;
-  int S, Hq, Hkv, n_rows, n_sink, window;               // window < 0: every row
+  int S, Hq, Hkv, n_rows, n_sink, window, n_split;      // window < 0: every row
   float scale_log2e;
 };
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 
 // 16-byte piece c of row r of a tile stands at piece c ^ swizzle(r) of its 256 bytes: the 32 rows that a K
 // operand reads a piece of, and the 4 rows of 64 bytes that a transposing read takes, are in different banks.
 __device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 
-// Which block of which sequence; the last block of a sequence, which sees most rows, comes first.
+// The block of queries of a workgroup: which sequence, which of its new tokens, which tiles of the cache they see.
+// The last block of a sequence, which sees most rows, comes first.
 struct QueryBlock {
-  int s, block, begin, n_new;
+  int s, begin, tok0, n_tok;                            // rows [begin + tok0, + n_tok) of q
+  int p0, p_last, end;                                  // cache rows of the first and last token; rows seen < end
+  int n_sink, sink_tiles, gap, n_tiles;                 // tile j < sink_tiles is tile j of the cache, else j + gap
   __device__ __forceinline__ static int bound(const PromptArgs& a, int s) {
     const int t = a.starts[s];
     return t < 0 ? 0 : (t < a.n_rows ? t : a.n_rows);
@@ -63,18 +71,82 @@ struct QueryBlock {
         const int l = __builtin_ctzll(beyond);
         s = s0 + l;
         begin = __builtin_amdgcn_readlane(b, l);
-        n_new = __builtin_amdgcn_readlane(m, l);
-        block = __builtin_amdgcn_readlane(upto, l) - 1 - w;
+        const int n_new = __builtin_amdgcn_readlane(m, l);
+        tok0 = (__builtin_amdgcn_readlane(upto, l) - 1 - w) * tokens;
+        n_tok = min(tokens, n_new - tok0);
+        const int length = __builtin_amdgcn_readfirstlane(a.pages.clamp_length(a.lengths[s]));
+        p0 = length - n_new + tok0;                     // negative: sees nothing
+        p_last = p0 + n_tok - 1;
+        end = max(p_last + 1, 0);                       // <= length
+        n_sink = a.window < 0 ? 0 : a.n_sink;
+        const int last_tile = (end + PR_TILE - 1) / PR_TILE;
+        sink_tiles = (min(n_sink, end) + PR_TILE - 1) / PR_TILE;
+        int first_tile = 0;
+        if (a.window >= 0) first_tile = a.window == 0 ? last_tile : max(0, p0 - a.window + 1) / PR_TILE;
+        first_tile = max(first_tile, sink_tiles);
+        gap = first_tile - sink_tiles;
+        n_tiles = sink_tiles + max(0, last_tile - first_tile);
         return true;
       }
       before = __builtin_amdgcn_readlane(upto, WAVE - 1);
     }
     return false;
   }
+  __device__ __forceinline__ int first_row(int tile) const { return (tile < sink_tiles ? tile : tile + gap) * PR_TILE; }
+  // Few blocks: their tiles are cut into pieces for n_split workgroups, short ones into fewer.
+  __device__ __forceinline__ int piece_tiles(int n_split) const {
+    return n_split == 1 ? n_tiles : max(PR_MIN_TILES, (n_tiles + n_split - 1) / n_split);
+  }
+  __device__ __forceinline__ int pieces(int n_split) const {
+    return n_split == 1 || n_tiles == 0 ? 1 : (n_tiles + piece_tiles(n_split) - 1) / piece_tiles(n_split);
+  }
 };
+
+// Where a lane's query and its part of the output are: row `wave * 32 + lane % 32` of the block.
+struct QueryRow {
+  int token, head;
+  bool there;
+  int64_t at;                                           // element of q and out
+  template <int G>
+  __device__ __forceinline__ static QueryRow of(const PromptArgs& a, const QueryBlock& b, int h, int row) {
+    QueryRow r;
+    r.token = row / G;
+    r.head = row % G;
+    r.there = r.token < b.n_tok;
+    r.at = ((int64_t)(b.begin + b.tok0 + (r.there ? r.token : 0)) * a.Hq + h * G + r.head) * D;
+    return r;
+  }
+};
+
+// What a workgroup leaves of a piece: maximum and sum of every lane, then its accumulators four by four.
+struct Partial {
+  static constexpr int FLOATS = PR_WAVES * WAVE * (2 + 64);
+  float* base;
+  __device__ __forceinline__ Partial(float* part, int64_t index) : base(part + index * FLOATS) {}
+  __device__ __forceinline__ float2* stats(int tid) const { return reinterpret_cast<float2*>(base) + tid; }
+  __device__ __forceinline__ float4* four(int i, int tid) const {
+    return reinterpret_cast<float4*>(base + PR_WAVES * WAVE * 2) + i * PR_WAVES * WAVE + tid;
+  }
+};
+
+// channels 32 c + 8 j + 4 half + (0..3) of a query
+__device__ __forceinline__ void store_four(bf16* out, int c, int j, int half, const float (&x)[4]) {
+  bf16x2 lo, hi;
+  lo[0] = (bf16)x[0];
+  lo[1] = (bf16)x[1];
+  hi[0] = (bf16)x[2];
+  hi[1] = (bf16)x[3];
+  *reinterpret_cast<uint2*>(out + 32 * c + 8 * j + 4 * half) =
+      make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
 
 // one of the two bf16 of a word is infinite or not a number
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+// all bits of the halves that are finite
+__device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
+  const uint32_t bad = not_finite(w);
+  return ~(bad | (bad - (bad >> 15)));
+}
 
 // 16 bytes for every lane from base + offset to LDS at `to` + 16 * lane, on their way when this returns:
 // they are counted with the vector loads (wait_for_tiles).
@@ -84,64 +156,54 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
-__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ void group_barrier() {       // LDS writes of this wavefront are done before it
+template <int LEFT>                                     // loads that may still be on their way
+__device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void group_barrier() {       // LDS reads and writes of this wavefront are done before it
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// all bits of the halves that are finite
-__device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
-  const uint32_t bad = not_finite(w);
-  return ~(bad | (bad - (bad >> 15)));
-}
+// A run of tiles [lo, lo + n), as what one comparison tells.
+struct Tiles {
+  int lo;
+  uint32_t n;
+  __device__ __forceinline__ Tiles(int lo_, int hi) : lo(lo_), n((uint32_t)max(hi - lo_, 0)) {}
+  __device__ __forceinline__ bool has(int t) const { return (uint32_t)(t - lo) < n; }
+};
 
 // EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page.
 template <int G, bool EIGHTS>
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
-  constexpr int TILE_BYTES = PR_TILE * D * 2;           // of K; V follows
-  __shared__ __attribute__((aligned(1024))) char tiles[2][2 * TILE_BYTES];
-  __shared__ __attribute__((aligned(8))) uint8_t hole_lds[2][8];   // bit r: row r of the tile is not there
-  __shared__ __attribute__((aligned(8))) uint8_t odd_lds[8];       // bit r: row r has a value that is not finite
-  static_assert(PR_WAVES == 8 && PR_TILE == 64, "eight rows of a tile for each wavefront");
-  constexpr int TOKENS = PR_ROWS / G;
+  constexpr int TILE_BYTES = PR_TILE * D * 2;
+  __shared__ __attribute__((aligned(1024))) char k_tiles[PR_BUFFERS][TILE_BYTES];
+  __shared__ __attribute__((aligned(1024))) char v_tiles[PR_BUFFERS][TILE_BYTES];
+  __shared__ __attribute__((aligned(8))) uint8_t odd_lds[4][8];    // of tile t % 4; bit r: row r had a value not finite
+  static_assert(PR_WAVES == 8 && PR_TILE == 64 && PR_BUFFERS == 3, "eight rows of a tile for each wavefront");
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % a.Hkv;
+  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv, block = w / a.n_split, piece = w % a.n_split;
   QueryBlock qb;
-  if (!qb.find(a, blockIdx.x / a.Hkv, TOKENS)) return;
-  const int length = a.pages.clamp_length(a.lengths[qb.s]);
-  const int tok0 = qb.block * TOKENS;                   // of the sequence's new tokens
-  const int n_tok = min(TOKENS, qb.n_new - tok0);
-  const int p0 = length - qb.n_new + tok0;              // cache row of the first; negative: sees nothing
-  const int p_last = p0 + n_tok - 1;
+  if (!qb.find(a, block, PR_ROWS / G)) return;
+  const int tile0 = piece * qb.piece_tiles(a.n_split), n_pieces = qb.pieces(a.n_split);
+  if (piece >= n_pieces) return;
+  const int n_tiles = min(qb.piece_tiles(a.n_split), qb.n_tiles - tile0);
 
   // ---- queries: lane holds channels 16 sl + 8 half + (0..7) of row `col` ----
-  const int m_row = wave * 32 + col, my_tok = m_row / G, my_head = m_row % G;
-  const bool there = my_tok < n_tok;
-  const int64_t q_at = ((int64_t)(qb.begin + tok0 + (there ? my_tok : 0)) * a.Hq + h * G + my_head) * D;
+  const QueryRow mine = QueryRow::of<G>(a, qb, h, wave * 32 + col);
   bf16x8 q[8];
 #pragma unroll
   for (int sl = 0; sl < 8; ++sl)
-    q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.q + q_at + sl * 16 + half * 8));
-  const int p = there ? p0 + my_tok : -1;               // last row that the lane's query sees
-  const int p_lo = p0 + wave * 32 / G, p_hi = min(p0 + (wave * 32 + 31) / G, p_last);   // of the wavefront
+    q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.q + mine.at + sl * 16 + half * 8));
+  const int p = mine.there ? qb.p0 + mine.token : -1;   // last row that the lane's query sees
+  const int p_lo = qb.p0 + wave * 32 / G;               // of the wavefront's first query
 
-  // ---- the tiles: those of the sinks, then from the first row of the first window on ----
-  const int end = p_last + 1 < 0 ? 0 : p_last + 1;      // <= length
-  const int n_sink = a.window < 0 ? 0 : a.n_sink;
-  const int last_tile = (end + PR_TILE - 1) / PR_TILE;
-  const int sink_tiles = (min(n_sink, end) + PR_TILE - 1) / PR_TILE;
-  int first_tile = 0;
-  if (a.window >= 0) first_tile = a.window == 0 ? last_tile : max(0, p0 - a.window + 1) / PR_TILE;
-  first_tile = max(first_tile, sink_tiles);
-  const int n_tiles = sink_tiles + max(0, last_tile - first_tile);
-  auto first_row = [&](int nth) { return (nth < sink_tiles ? nth : first_tile + (nth - sink_tiles)) * PR_TILE; };
+  // Tiles of which every query sees every row, for the workgroup and for the wavefront.  (Those of the sinks are few.)
+  const int window_in = a.window < 0 ? 0 : (max(0, qb.p_last - a.window + 1) + PR_TILE - 1) / PR_TILE - qb.gap;
+  const int from_whole = max(window_in, qb.sink_tiles) - tile0;
+  const Tiles all_whole(from_whole, max(0, qb.p0 + 1) / PR_TILE - qb.gap - tile0);
+  const Tiles whole(from_whole, max(0, p_lo + 1) / PR_TILE - qb.gap - tile0);
 
   floatx16 acc[4];
 #pragma unroll
@@ -150,136 +212,169 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
   float m = PR_NEG_BIG, l = 0.f;                        // of the unscaled scores; l: of this lane's rows
 
-  // ---- bringing tiles: this wavefront rows 8 wave + 4 i + lane / 16, pieces lane % 16 ----
-  constexpr int LOOKUPS = EIGHTS ? 1 : 2;
-  int page[LOOKUPS], slot[LOOKUPS];                     // of the tile after the next
-  auto look_up = [&](int nth) {
-    const int r0 = first_row(nth) + wave * 8;
-#pragma unroll
-    for (int i = 0; i < LOOKUPS; ++i) {
-      const int r = EIGHTS ? r0 : r0 + 4 * i + (lane >> 4);
-      page[i] = -1;
-      slot[i] = 0;
-      if (nth < n_tiles && r < end) {
-        const int e = a.pages.size.quotient(r);
-        page[i] = a.pages.table[(int64_t)qb.s * a.pages.per_seq + e];
-        slot[i] = r - e * (int)a.pages.size.d;
-      }
-    }
+  // ---- where rows are ----
+  // Page numbers are looked up by whole wavefronts: EIGHTS: lane 8 i + j for rows 8 j of tile i of the next eight
+  // tiles; else lane r for row r of the next tile.  Every wavefront has them all: its own rows, and what is missing.
+  constexpr int AT_ONCE = EIGHTS ? 8 : 1;
+  int next_page, next_slot, place = -1;
+  auto look_up = [&](int t) {                           // t: a multiple of AT_ONCE; tiles behind the last have no rows
+    const int tile = EIGHTS ? t + (lane >> 3) : t;
+    const int r = qb.first_row(tile0 + tile) + (EIGHTS ? (lane & 7) * 8 : lane);
+    const bool is = tile < n_tiles && r < qb.end;
+    const int e = a.pages.size.quotient(is ? r : 0);
+    next_page = a.pages.table[(int64_t)qb.s * a.pages.per_seq + e];
+    next_slot = is ? r - e * (int)a.pages.size.d : -1;
   };
-  uint32_t piece[2];                                    // where in 4 rows the lane's piece stands
+  // Rows of a tile that are not there, as bits, of the last four tiles asked for (the newest first).
+  uint64_t gone[4] = {0, 0, 0, 0};
+  uint32_t own[2];                                      // where in the source the lane's 16 bytes of 4 rows stand
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int sub = lane >> 4, r = wave * 8 + 4 * i + sub;
-    piece[i] = (EIGHTS ? (4 * i + sub) * 256 : 0) + ((lane & 15) ^ swizzle(r)) * 16;
+    own[i] = (EIGHTS ? (4 * i + sub) * 256 : 0) + ((lane & 15) ^ swizzle(r)) * 16;
   }
-  const uint32_t lds0 = lds_address(tiles) + wave * 8 * 256;
-  auto bring = [&](int buf) {
-    const uint32_t to = lds0 + buf * 2 * TILE_BYTES;
-    uint32_t holes;
-    if constexpr (EIGHTS) {
-      const int at = __builtin_amdgcn_readfirstlane(a.pages.place(page[0], h, slot[0]));
-      holes = at < 0 ? 0xFFu : 0u;
-      const char* K = reinterpret_cast<const char*>(a.K) + (int64_t)max(at, 0) * (D * 2);
-      const char* V = reinterpret_cast<const char*>(a.V) + (int64_t)max(at, 0) * (D * 2);
+  const uint32_t own_k = lds_address(k_tiles) + wave * 8 * 256, own_v = lds_address(v_tiles) + wave * 8 * 256;
+  struct Rows { int at[EIGHTS ? 1 : 2]; };              // pool rows of this wavefront's part of a tile
+  auto bring = [&](const bf16* pool, const Rows& r, uint32_t to) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        load_to_lds(K, piece[i], to + i * 1024);
-        load_to_lds(V, piece[i], to + i * 1024 + TILE_BYTES);
-      }
-    } else {
-      holes = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = a.pages.place(page[i], h, slot[i]);
-        const uint64_t none = __ballot(at < 0);
-        holes |= (uint32_t)((none & 1) | ((none >> 16) & 1) << 1 | ((none >> 32) & 1) << 2 | ((none >> 48) & 1) << 3) << (4 * i);
-        const int64_t from = (int64_t)max(at, 0) * (D * 2) + piece[i];
-        load_to_lds(reinterpret_cast<const char*>(a.K) + from, to + i * 1024);
-        load_to_lds(reinterpret_cast<const char*>(a.V) + from, to + i * 1024 + TILE_BYTES);
-      }
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (EIGHTS)
+        load_to_lds(reinterpret_cast<const char*>(pool) + (int64_t)r.at[0] * (D * 2), own[i], to + i * 1024);
+      else
+        load_to_lds(reinterpret_cast<const char*>(pool) + ((int64_t)r.at[i] * (D * 2) + own[i]), to + i * 1024);
     }
-    if (lane == 0) hole_lds[buf][wave] = (uint8_t)holes;
+  };
+  auto rows_of = [&](int t) {                           // in turn: t = 0, 1, 2, ..
+    if ((t & (AT_ONCE - 1)) == 0) {
+      place = next_slot < 0 ? -1 : a.pages.place(next_page, h, next_slot);
+      look_up(t + AT_ONCE);
+    }
+    Rows r;
+    gone[3] = gone[2];
+    gone[2] = gone[1];
+    gone[1] = gone[0];
+    if constexpr (EIGHTS) {
+      const uint32_t none = (uint32_t)(__ballot(place < 0) >> ((t & 7) * 8)) & 0xFFu;
+      gone[0] = __ballot((none >> (lane >> 3)) & 1);    // bit j of none is rows 8 j .. 8 j + 7
+      r.at[0] = max(__builtin_amdgcn_readlane(place, (t & 7) * 8 + wave), 0);
+    } else {
+      gone[0] = __ballot(place < 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) r.at[i] = max(__shfl(place, wave * 8 + 4 * i + (lane >> 4)), 0);
+    }
+    return r;
   };
 
-  // where this lane reads: K row `col`, pieces 2 sl + half; V rows 4 half + (lane / 4) % 4, see below
-  const int rr = (lane >> 2) & 3;
-  const uint32_t k_at = lds_address(tiles) + col * 256 + (half ^ swizzle(col)) * 16;
-  const uint32_t v_at = lds_address(tiles) + TILE_BYTES + (4 * half + rr) * 256 + (lane & 1) * 8 + (rr << 6) +
-                        (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) << 4);
+  // ---- values that are not finite ----
+  // Where some query does not see some row, such a value may reach only the queries that see its row, and zero times it
+  // would be a NaN for the others: it leaves the tile.  Each wavefront looks at the rows that it has brought.
+  auto check_values = [&](int t, uint64_t missing, uint32_t buffer) {
+    if (all_whole.has(t) && missing == 0) return;
+    uint32_t rows = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint4* at = reinterpret_cast<uint4*>(v_tiles[0] + buffer + wave * 8 * 256 + i * 1024 + lane * 16);
+      const uint4 x = *at;
+      const bool bad = (not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w)) != 0;
+      const uint64_t some = __ballot(bad);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) rows |= ((some >> (16 * u)) & 0xFFFF ? 1u : 0u) << (4 * i + u);
+      if (bad) *at = make_uint4(x.x & finite_mask(x.x), x.y & finite_mask(x.y), x.z & finite_mask(x.z), x.w & finite_mask(x.w));
+    }
+    if (lane == 0) odd_lds[t & 3][wave] = (uint8_t)rows;
+  };
+  // ... and what has left the tile is added to the queries that see it
+  uint64_t seen = 0;                                    // rows of the tile that the query sees
+  auto add_odd_values = [&](int t, uint64_t missing) {
+    if (all_whole.has(t) && missing == 0) return;
+    const uint64_t in_lds = *reinterpret_cast<const uint64_t*>(odd_lds[t & 3]);
+    uint64_t rows = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)in_lds) |
+                    (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(in_lds >> 32)) << 32;
+    for (; rows; rows &= rows - 1) {
+      const int r = __builtin_ctzll(rows);
+      const int at = a.pages.row(qb.s, h, qb.first_row(tile0 + t) + r);
+      if (at < 0 || !((seen >> r) & 1)) continue;
+      const uint2* from = reinterpret_cast<const uint2*>(a.V + (int64_t)at * D) + half;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {                   // channels 32 c + 8 j + 4 half + (0..3)
+          const uint2 x = from[8 * c + 2 * j];
+          const uint32_t lo = x.x & ~finite_mask(x.x), hi = x.y & ~finite_mask(x.y);   // the others: 0
+          acc[c][4 * j] += lo_bf16(lo);
+          acc[c][4 * j + 1] += hi_bf16(lo);
+          acc[c][4 * j + 2] += lo_bf16(hi);
+          acc[c][4 * j + 3] += hi_bf16(hi);
+        }
+    }
+  };
 
-  typedef short shortx8 __attribute__((ext_vector_type(8)));
-  // whole: every query of the wavefront sees every row of the tile.  Else gone: rows that are not there, odd: rows
-  // that had a value that is not finite.
-  auto use_tile = [&](bool whole, int buf, int r0, uint64_t gone, uint64_t odd) {
-    // ---- S^T ----
-    floatx16 sc[2];
-    const uint32_t kb = k_at + buf * 2 * TILE_BYTES, vb = v_at + buf * 2 * TILE_BYTES;
-    // four pieces of a K operand, and of V operands, are on their way while four products run
-    auto keys = [&](int g, bf16x8 (&k)[4]) {
+  // ---- the products ----
+  // A lane reads K row `col`, pieces 2 sl + half, and V rows 4 half + (lane / 4) % 4 of groups of 8.
+  const int rr = (lane >> 2) & 3;
+  const uint32_t k_at = lds_address(k_tiles) + col * 256 + (half ^ swizzle(col)) * 16;
+  const uint32_t v_at = lds_address(v_tiles) + (4 * half + rr) * 256 + (lane & 1) * 8 + (rr << 6) +
+                        (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ half) << 4);
+  struct Group { bf16x8 f[4]; };                        // operands of four products
+  auto read_values = [&](uint32_t buffer, int s) {
+    // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
+    const uint32_t vb = v_at + buffer;
+    Group r;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) k[i] = *(lds_bf16x8*)(uintptr_t)((kb ^ (((g & 1) * 4 + i) << 5)) + (g >> 1) * 32 * 256);
-    };
-    auto values = [&](int s, shortx8 (&v)[4]) {
-      // rows 16 s + 8 u + 4 half + (0..3), channels 32 c + 16 ((lane / 16) % 2) + (0..15) of the 16 lanes
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6)) + s * 4096));
-        const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6) ^ 32) + s * 4096 + 2048));
-        v[c] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    };
-    bf16x8 k[2][4];
-    shortx8 v[2][4];
-    keys(0, k[0]);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g < 3) keys(g + 1, k[(g + 1) & 1]);
-      else values(0, v[0]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int sl = (g & 1) * 4 + i;
-        if (sl == 0) {
-          floatx16 z;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) z[e] = 0.f;
-          sc[g >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[g & 1][i], q[sl], z, 0, 0, 0);
-        } else {
-          sc[g >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[g & 1][i], q[sl], sc[g >> 1], 0, 0, 0);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < 4; ++c) {
+      const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6)) + s * 4096));
+      const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(uintptr_t)((vb ^ (c << 6) ^ 32) + s * 4096 + 2048));
+      const shortx8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      r.f[c] = __builtin_bit_cast(bf16x8, both);
     }
-    // ---- softmax ----
-    uint64_t seen = ~0ull;
-    if (!whole) {
-      // rows of the tile that the query sees, as bits
-      const int last = p - r0;
-      seen = last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1);
-      if (a.window >= 0) {
-        const int first = p - a.window + 1 - r0, sinks = n_sink - r0;
-        uint64_t near = first <= 0 ? ~0ull : (first > 63 ? 0 : ~0ull << first);
-        near |= sinks <= 0 ? 0 : (sinks > 63 ? ~0ull : (1ull << sinks) - 1);
-        seen &= near;
-      }
-      seen &= ~gone;
-      const uint64_t mine = seen >> (4 * half);
+    return r;
+  };
+  auto read_keys = [&](uint32_t buffer, int g) {        // slabs 2 g and 2 g + 1 of both halves of the tile
+    const uint32_t kb = k_at + buffer;
+    Group r;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+    for (int i = 0; i < 4; ++i) r.f[i] = *(lds_bf16x8*)(uintptr_t)((kb ^ ((2 * g + (i >> 1)) << 5)) + (i & 1) * 32 * 256);
+    return r;
+  };
+  typedef floatx16 Scores[2];
+  auto score = [&](const Group& k, int g, int i, Scores& sc) {
+    const int b = i & 1, sl = 2 * g + (i >> 1);
+    floatx16 z;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t bit = 1u << (8 * (i >> 2) + (i & 3));
-          sc[b][i] = ((uint32_t)(mine >> (32 * b)) & bit) ? sc[b][i] : -INFINITY;
-        }
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.f[i], q[sl], sl == 0 ? z : sc[b], 0, 0, 0);
+  };
+  uint32_t pb[4][4];                                    // probabilities: slab s of 16 rows
+  auto weigh = [&](const Group& v, int s, int c) {
+    const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(pb[s][0], pb[s][1], pb[s][2], pb[s][3]));
+    acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.f[c], pr, acc[c], 0, 0, 0);
+  };
+  // Scores of rows that the query does not see become -infinity.
+  auto mask = [&](int t, uint64_t missing, Scores& sc) -> uint64_t {
+    if (whole.has(t) && missing == 0) return ~0ull;
+    const int r0 = qb.first_row(tile0 + t), last = p - r0;
+    uint64_t sees = last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1);
+    if (a.window >= 0) {
+      const int first = p - a.window + 1 - r0, sinks = qb.n_sink - r0;
+      uint64_t near = first <= 0 ? ~0ull : (first > 63 ? 0 : ~0ull << first);
+      near |= sinks <= 0 ? 0 : (sinks > 63 ? ~0ull : (1ull << sinks) - 1);
+      sees &= near;
     }
-    float mx = PR_NEG_BIG;
+    sees &= ~missing;
+    const uint64_t rows = sees >> (4 * half);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, sc[b][i]), sc[b][i + 1]);
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t bit = 1u << (8 * (i >> 2) + (i & 3));
+        sc[b][i] = ((uint32_t)(rows >> (32 * b)) & bit) ? sc[b][i] : -INFINITY;
+      }
+    return sees;
+  };
+  // The maximum in use may be smaller than the true one by 8 powers of two: probabilities are relative to
+  // each other, and up to 256 they are as exact as up to 1.
+  auto raise = [&](float mx) {
     mx = xor32(mx, OpMax());
-    // The maximum in use may be smaller than the true one by 8 powers of two: probabilities are relative to
-    // each other, and up to 256 they are as exact as up to 1.
     if (__ballot((mx - m) * a.scale_log2e > 8.f)) {
       mx = fmaxf(mx, m);
       const float corr = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e);
@@ -290,118 +385,183 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       l *= corr;
       m = mx;
     }
-    const float mc = m * a.scale_log2e;
-    uint32_t pb[4][4];                                  // slab s of 16 rows
+  };
+  auto max_of = [&](float mx, const Scores& sc, int quarter) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        bf16x2 e;
-        e[0] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale_log2e, -mc));
-        e[1] = (bf16)__builtin_amdgcn_exp2f(fmaf(sc[b][i + 1], a.scale_log2e, -mc));
-        const bf16x2 one = {(bf16)1.f, (bf16)1.f};
-        l = __builtin_amdgcn_fdot2_f32_bf16(e, one, l, false);   // what the product takes is what is summed
-        pb[2 * b + (i >> 3)][(i & 7) >> 1] = __builtin_bit_cast(uint32_t, e);
-      }
-    // ---- O^T ----
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s < 3) values(s + 1, v[(s + 1) & 1]);
-      const bf16x8 pr = __builtin_bit_cast(bf16x8, make_uint4(pb[s][0], pb[s][1], pb[s][2], pb[s][3]));
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[s & 1][c]), pr, acc[c], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < 8; i += 2) {
+      const int e = 8 * (quarter & 1) + i;
+      mx = fmaxf(fmaxf(mx, sc[quarter >> 1][e]), sc[quarter >> 1][e + 1]);
     }
-    // The values that have been taken out of the tile reach the queries that see their rows.
-    for (uint64_t rows = odd; rows; rows &= rows - 1) { // uniform
-      const int r = __builtin_ctzll(rows);
-      const bool here = (seen >> r) & 1;
-      const int at = a.pages.row(qb.s, h, r0 + r);
-      if (at < 0 || !here) continue;
-      const uint2* from = reinterpret_cast<const uint2*>(a.V + (int64_t)at * D) + half;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {                   // channels 32 c + 8 j + 4 half + (0..3)
-          const uint2 w = from[8 * c + 2 * j];
-          const uint32_t x = w.x & ~finite_mask(w.x), y = w.y & ~finite_mask(w.y);   // the others: 0
-          acc[c][4 * j] += lo_bf16(x);
-          acc[c][4 * j + 1] += hi_bf16(x);
-          acc[c][4 * j + 2] += lo_bf16(y);
-          acc[c][4 * j + 3] += hi_bf16(y);
-        }
-    }
+    return mx;
   };
 
-  __builtin_amdgcn_s_waitcnt(0);                        // the queries: no wait for them inside the loop
+  // A tile in two parts, so that there is something for the matrix cores and something for the vector ALUs in both:
+  //   the scores of the next tile, while the probabilities of this one are taken;
+  //   the products of this one's probabilities and values, while the maximum of the next scores is found.
+  // Vector instructions are laid between the products by hand; operands are read two groups of four products ahead
+  // (LDS answers later than one group takes).  At the begin of tile t all wavefronts ask for the keys of t + 3 and the
+  // values of t + 2, whose buffers were read for tile t - 1; what was asked for before that has to be there at its end.
+  // Tiles behind the last one are asked for and scored too (rows that the pool has, all masked): no conditions.
   if (n_tiles > 0) {
+    __builtin_amdgcn_s_waitcnt(0);                      // the queries: no wait for them inside the loop
     look_up(0);
-    bring(0);
-    look_up(1);
-  }
-  for (int nth = 0; nth < n_tiles; ++nth) {
-    const int buf = nth & 1, r0 = first_row(nth);
-    wait_for_tiles();
+    Rows v_rows, k_rows = rows_of(0);
+    bring(a.K, k_rows, own_k);
+    auto request = [&](int t, uint32_t v_buffer, uint32_t k_buffer) {   // keys of tile t, values of t - 1
+      v_rows = k_rows;
+      k_rows = rows_of(t);
+      bring(a.V, v_rows, own_v + v_buffer);
+      bring(a.K, k_rows, own_k + k_buffer);
+    };
+    request(1, 0, TILE_BYTES);
+    request(2, TILE_BYTES, 2 * TILE_BYTES);
+    wait_for_tiles<0>();
+    check_values(0, gone[2], 0);
     group_barrier();
-    if (nth + 1 < n_tiles) {
-      bring(buf ^ 1);
-      look_up(nth + 2);
+    Scores sa, sb;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const Group k = read_keys(0, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) score(k, g, i, sa);
     }
-    uint64_t gone = *reinterpret_cast<const uint64_t*>(hole_lds[buf]);
-    gone = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)gone) |
-           (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(gone >> 32)) << 32;
-    const bool open = gone == 0 && (a.window < 0 || r0 + PR_TILE <= n_sink || r0 > p_last - a.window);
-    uint64_t odd = 0;
-    if (!(open && r0 + PR_TILE <= p0 + 1)) {
-      // Some row is masked for some query of the workgroup.  A value that is not finite may reach only the queries
-      // that see its row, and zero times it would be a NaN for the others: it leaves the tile.
-      uint32_t rows = 0;
+    seen = mask(0, gone[2], sa);
+    {
+      float mx = PR_NEG_BIG;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint4* at = reinterpret_cast<uint4*>(tiles[buf] + TILE_BYTES + wave * 8 * 256 + i * 1024 + lane * 16);
-        const uint4 w = *at;
-        const bool bad = (not_finite(w.x) | not_finite(w.y) | not_finite(w.z) | not_finite(w.w)) != 0;
-        const uint64_t some = __ballot(bad);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) rows |= ((some >> (16 * u)) & 0xFFFF ? 1u : 0u) << (4 * i + u);
-        if (bad) *at = make_uint4(w.x & finite_mask(w.x), w.y & finite_mask(w.y), w.z & finite_mask(w.z), w.w & finite_mask(w.w));
-      }
-      if (lane == 0) odd_lds[wave] = (uint8_t)rows;
+      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
+      raise(mx);
+    }
+    // buffers of tiles t, t + 1 and t + 2
+    uint32_t b0 = 0, b1 = TILE_BYTES, b2 = 2 * TILE_BYTES;
+    auto use_tile = [&](int t, Scores& sc, Scores& next) {
       group_barrier();
-      odd = *reinterpret_cast<const uint64_t*>(odd_lds);
-      odd = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)odd) |
-            (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(odd >> 32)) << 32;
+      request(t + 3, b2, b0);
+      // gone: of tiles t + 3, t + 2, t + 1, t
+      const float mc = m * a.scale_log2e;
+      Group k0 = read_keys(b1, 0), k1, k2, k3, v0, v1;
+      float x[17][2], e[17][2];
+      auto scaled = [&](int j) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) x[j][u] = fmaf(sc[j >> 3][2 * (j & 7) + u], a.scale_log2e, -mc);
+        asm volatile("" : "+v"(x[j][0]), "+v"(x[j][1]));
+      };
+      auto powers = [&](int j) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) e[j][u] = __builtin_amdgcn_exp2f(x[j][u]);
+        asm volatile("" : "+v"(e[j][0]), "+v"(e[j][1]));
+      };
+      auto packed = [&](int j) {
+        bf16x2 two;
+        two[0] = (bf16)e[j][0];
+        two[1] = (bf16)e[j][1];
+        l += e[j][0] + e[j][1];
+        pb[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, two);
+        asm volatile("" : "+v"(pb[j >> 2][j & 3]), "+v"(l));
+      };
+      __builtin_amdgcn_s_setprio(1);
+      scaled(0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {                    // one product, and one step of each of three pairs
+        const int g = j >> 2;
+        if (j == 0) k1 = read_keys(b1, 1);
+        if (j == 4) k2 = read_keys(b1, 2);
+        if (j == 8) k3 = read_keys(b1, 3);
+        if (j == 12) v0 = read_values(b0, 0);
+        score(g == 0 ? k0 : (g == 1 ? k1 : (g == 2 ? k2 : k3)), g, j & 3, next);
+        if (j + 1 < 16) scaled(j + 1);
+        powers(j);
+        if (j > 0) packed(j - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      packed(15);
+      __builtin_amdgcn_s_setprio(0);
+      const uint64_t next_seen = mask(t + 1, gone[2], next);
+      float mx = PR_NEG_BIG;
+      v1 = read_values(b0, 1);
+      Group v2, v3;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int s = j >> 2;
+        if (j == 0) v2 = read_values(b0, 2);
+        if (j == 4) v3 = read_values(b0, 3);
+        weigh(s == 0 ? v0 : (s == 1 ? v1 : (s == 2 ? v2 : v3)), s, j & 3);
+        if (j & 3) continue;
+        if (s > 0) mx = max_of(mx, next, s - 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mx = max_of(mx, next, 3);
+      add_odd_values(t, gone[3]);
+      seen = next_seen;
+      raise(mx);
+      wait_for_tiles<4>();                              // all but the last four that have been asked for
+      check_values(t + 1, gone[2], b1);
+      const uint32_t b = b0;
+      b0 = b1;
+      b1 = b2;
+      b2 = b;
+    };
+    for (int t = 0; t < n_tiles; t += 2) {
+      use_tile(t, sa, sb);
+      use_tile(t + 1, sb, sa);
     }
-    const bool whole = open && r0 + PR_TILE <= p_lo + 1;
-    if (r0 > p_hi || (a.window >= 0 && r0 >= n_sink && r0 + PR_TILE <= p_lo - a.window + 1)) continue;
-
-    use_tile(whole, buf, r0, gone, odd & ~gone);
+    wait_for_tiles<0>();                                // nothing is on its way to LDS behind the end
   }
 
-  // ---- out: channels 32 c + 8 (i / 4) + 4 half + i % 4 of row `col` ----
   l = xor32(l, OpSum());
+  if (!mine.there) return;
+  if (n_pieces > 1) {
+    const Partial to(a.part, ((int64_t)block * a.Hkv + h) * a.n_split + piece);
+    *to.stats(tid) = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      *to.four(i, tid) = make_float4(acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2],
+                                     acc[i >> 2][4 * (i & 3) + 3]);
+    return;
+  }
   const float inv = l > 0.f ? 1.0f / l : 0.f;
-  if (!there) return;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      uint32_t w[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        bf16x2 o;
-        o[0] = (bf16)(acc[c][4 * j + 2 * e] * inv);
-        o[1] = (bf16)(acc[c][4 * j + 2 * e + 1] * inv);
-        w[e] = __builtin_bit_cast(uint32_t, o);
-      }
-      *reinterpret_cast<uint2*>(a.out + q_at + 32 * c + 8 * j + 4 * half) = make_uint2(w[0], w[1]);
+      const float x[4] = {acc[c][4 * j] * inv, acc[c][4 * j + 1] * inv, acc[c][4 * j + 2] * inv, acc[c][4 * j + 3] * inv};
+      store_four(a.out + mine.at, c, j, half, x);
     }
 }
 
+// The pieces of a block joined, in their order: blockIdx.y has four of the 64 accumulators of every lane.
+template <int G>
+__global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs a) {
+  const int h = blockIdx.x % a.Hkv, block = blockIdx.x / a.Hkv, i = blockIdx.y;
+  QueryBlock qb;
+  if (!qb.find(a, block, PR_ROWS / G)) return;
+  const int n = qb.pieces(a.n_split), tid = threadIdx.x, lane = tid & 63;
+  const QueryRow mine = QueryRow::of<G>(a, qb, h, (tid >> 6) * 32 + (lane & 31));
+  if (n == 1 || !mine.there) return;
+  const int64_t first = ((int64_t)block * a.Hkv + h) * a.n_split;
+  float m = PR_NEG_BIG, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < n; ++k) {
+    const Partial from(a.part, first + k);
+    const float2 st = *from.stats(tid);
+    const float4 f = *from.four(i, tid);
+    const float mx = fmaxf(m, st.x);
+    const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e), add = __builtin_amdgcn_exp2f((st.x - mx) * a.scale_log2e);
+    m = mx;
+    l = l * old + st.y * add;
+    x[0] = x[0] * old + f.x * add;
+    x[1] = x[1] * old + f.y * add;
+    x[2] = x[2] * old + f.z * add;
+    x[3] = x[3] * old + f.w * add;
+  }
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
+  store_four(a.out + mine.at, i >> 2, i & 3, lane >> 5, x);
+}
+
 template <bool EIGHTS>
-void launch_prompt_g(int G, dim3 grid, dim3 block, const PromptArgs& a, hipStream_t st) {
+void launch_prompt_g(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
+  const dim3 grid(blocks * a.Hkv * a.n_split), block(PR_WAVES * 64);
   switch (G) {
     case 1: hipLaunchKernelGGL((k_prompt_attn<1, EIGHTS>), grid, block, 0, st, a); break;
     case 2: hipLaunchKernelGGL((k_prompt_attn<2, EIGHTS>), grid, block, 0, st, a); break;
@@ -409,24 +569,44 @@ void launch_prompt_g(int G, dim3 grid, dim3 block, const PromptArgs& a, hipStrea
     default: hipLaunchKernelGGL((k_prompt_attn<8, EIGHTS>), grid, block, 0, st, a); break;
   }
 }
+void launch_join(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
+  const dim3 grid(blocks * a.Hkv, 16), block(PR_WAVES * 64);
+  switch (G) {
+    case 1: hipLaunchKernelGGL(k_prompt_join<1>, grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL(k_prompt_join<2>, grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL(k_prompt_join<4>, grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL(k_prompt_join<8>, grid, block, 0, st, a); break;
+  }
+}
+
+// Blocks there can be: one of each sequence may be short.
+int64_t prompt_blocks(const Dims& dm, int64_t n_rows) {
+  return n_rows / (PR_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S);
+}
+// Workgroups that share the tiles of a block.  One workgroup fills a compute unit; what does not fill half of the
+// chip is cut.
+int prompt_split(const Dims& dm, int64_t n_rows) {
+  const int64_t groups = prompt_blocks(dm, n_rows) * dm.Hkv;
+  return groups >= PR_CUS ? 1 : (int)(PR_CUS / groups);
+}
 
 }  // namespace
 
 size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows) {
-  (void)dm;
-  (void)n_rows;
-  return 256;
+  const int n_split = prompt_split(dm, n_rows);
+  if (n_split == 1) return 256;
+  return (size_t)prompt_blocks(dm, n_rows) * dm.Hkv * n_split * Partial::FLOATS * sizeof(float);
 }
 
 hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
                               const ck_paged_kv& kv, const int32_t* lengths, int64_t n_sink, int64_t window,
                               float softmax_scale, void* out, void* workspace, hipStream_t st) {
-  (void)workspace;
   PromptArgs a = {};
   a.q = static_cast<const bf16*>(q);
   a.K = static_cast<const bf16*>(kv.K);
   a.V = static_cast<const bf16*>(kv.V);
   a.out = static_cast<bf16*>(out);
+  a.part = static_cast<float*>(workspace);
   a.starts = q_starts;
   a.lengths = lengths;
   a.pages = Pages(kv, dm.Hkv);
@@ -437,15 +617,14 @@ hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, con
   const int64_t rows = a.pages.rows;
   a.n_sink = (int)(n_sink < rows ? n_sink : rows);
   a.window = window < 0 || window >= rows ? -1 : (int)window;
+  a.n_split = prompt_split(dm, n_rows);
   a.scale_log2e = softmax_scale * 1.4426950408889634f;
-  const int tokens = PR_ROWS / dm.G;
-  // a block of each sequence may be short
-  const int64_t blocks = n_rows / tokens + (n_rows < dm.S ? n_rows : dm.S);
-  const dim3 grid((unsigned)(blocks * dm.Hkv)), block(PR_WAVES * 64);
+  const unsigned blocks = (unsigned)prompt_blocks(dm, n_rows);
   if (kv.page_size % 8 == 0)
-    launch_prompt_g<true>(dm.G, grid, block, a, st);
+    launch_prompt_g<true>(dm.G, blocks, a, st);
   else
-    launch_prompt_g<false>(dm.G, grid, block, a, st);
+    launch_prompt_g<false>(dm.G, blocks, a, st);
+  if (a.n_split > 1) launch_join(dm.G, blocks, a, st);
   return hipGetLastError();
 }
 
