@@ -521,31 +521,33 @@ def _kv(sh: Shape, kv):
     return ctypes.byref(kv) if kv is not None else None      # a structure of raw addresses
 
 
-def _ints(t, name, *shape):
-    """Address of an int32 tensor of this shape (None: any), of an address, or None."""
-    if not isinstance(t, torch.Tensor):
+# The next three check what the kernels take for granted; they are on the path of every generated token.
+def _ints(t, name, shape):
+    """Address of an int32 tensor of this shape, of an address, or None."""
+    if t is None or isinstance(t, int):
         return t
-    if t.dtype is not torch.int32 or t.dim() != len(shape) or any(
-            want is not None and have != want for have, want in zip(t.shape, shape)):
-        raise ValueError(f"{name} must be int32 {list(shape)}")
-    return _ptr(t)
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be int32 {list(shape)}, contiguous")
+    return t.data_ptr()
 
 
-def _rows(t, name, heads: int, sh: Shape):
-    """Address and row stride of token rows [n, heads, d] whose rows may lie apart."""
-    if not isinstance(t, torch.Tensor):
+def _rows(t, name, n, heads: int, sh: Shape):
+    """Address and row stride of n token rows [heads, d] that may lie apart."""
+    if t is None or isinstance(t, int):
         return t, heads * sh.d
-    if t.dtype is not sh.torch_dtype or t.dim() != 3 or t.shape[1:] != (heads, sh.d) or (
-            t.stride()[1:] != (sh.d, 1) and t.shape[1] > 1) or t.stride(2) != 1:
-        raise ValueError(f"{name} must be token rows [n, {heads}, {sh.d}] of the shape's type")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * sh.d
+    st = t.stride()
+    if (t.dtype is not sh.torch_dtype or t.shape != (n, heads, sh.d) or st[2] != 1
+            or (st[1] != sh.d and heads > 1)):
+        raise ValueError(f"{name} must be token rows [{n}, {heads}, {sh.d}] of the shape's type")
+    return t.data_ptr(), st[0] if n > 1 else heads * sh.d
 
 
 def _dense(t, name, n, sh: Shape):
-    if isinstance(t, torch.Tensor) and (t.dtype is not sh.torch_dtype or
-                                        tuple(t.shape) != (n, sh.Hq, sh.d)):
-        raise ValueError(f"{name} must be [{n}, {sh.Hq}, {sh.d}] of the shape's type")
-    return _ptr(t)
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not sh.torch_dtype or t.shape != (n, sh.Hq, sh.d) or not t.is_contiguous():
+        raise ValueError(f"{name} must be [{n}, {sh.Hq}, {sh.d}] of the shape's type, contiguous")
+    return t.data_ptr()
 
 
 def _bytes(workspace) -> int:
@@ -570,19 +572,17 @@ def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None,
     float32 [rot_dim / 2]; q and q_out may both be None.  interleaved: adjacent channels turn."""
     lib = load_library()
     n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
-    qp, qs = _rows(q, "q", sh.Hq, sh)
-    kp, ks = _rows(k, "k", sh.Hkv, sh)
-    vp, vs = _rows(v, "v", sh.Hkv, sh)
-    for t in (q, v):
-        if isinstance(t, torch.Tensor) and t.shape[0] != n:
-            raise ValueError("q, k and v must have the same number of rows")
-    if isinstance(freqs, torch.Tensor) and (freqs.dtype is not torch.float32 or freqs.dim() != 1):
-        raise ValueError("freqs must be float32 [rot_dim / 2]")
-    rot = 2 * freqs.shape[0] if isinstance(freqs, torch.Tensor) else sh.d
-    s = sh.c()
-    _check(lib.ck_rope_append(ctypes.byref(s), qp, kp, vp, qs, ks, vs, n,
-                              _ints(q_starts, "q_starts", sh.S + 1),
-                              _ints(lengths, "lengths", sh.S), _ints(positions, "positions", n),
+    qp, qs = _rows(q, "q", n, sh.Hq, sh)
+    kp, ks = _rows(k, "k", n, sh.Hkv, sh)
+    vp, vs = _rows(v, "v", n, sh.Hkv, sh)
+    rot = sh.d
+    if isinstance(freqs, torch.Tensor):
+        if freqs.dtype is not torch.float32 or freqs.dim() != 1:
+            raise ValueError("freqs must be float32 [rot_dim / 2]")
+        rot = 2 * freqs.shape[0]
+    _check(lib.ck_rope_append(ctypes.byref(sh.c()), qp, kp, vp, qs, ks, vs, n,
+                              _ints(q_starts, "q_starts", (sh.S + 1,)),
+                              _ints(lengths, "lengths", (sh.S,)), _ints(positions, "positions", (n,)),
                               _ptr(freqs), rot, attn_factor,
                               CK_ROPE_ADJACENT if interleaved else CK_ROPE_HALVES,
                               _dense(q_out, "q_out", n, sh), _kv(sh, kv), _stream(k)))
@@ -611,11 +611,10 @@ def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window
     stride = token_idx.shape[-1] if isinstance(token_idx, torch.Tensor) else 0
     if max_tokens is None:
         max_tokens = stride
-    s = sh.c()
-    _check(lib.ck_paged_decode_attn(ctypes.byref(s), _dense(q, "q", sh.S, sh), _kv(sh, kv),
-                                    _ints(lengths, "lengths", sh.S), n_sink, window,
-                                    _ints(token_idx, "token_idx", sh.S, sh.Hkv, None),
-                                    _ints(n_tokens, "n_tokens", sh.S, sh.Hkv), stride, max_tokens,
+    _check(lib.ck_paged_decode_attn(ctypes.byref(sh.c()), _dense(q, "q", sh.S, sh), _kv(sh, kv),
+                                    _ints(lengths, "lengths", (sh.S,)), n_sink, window,
+                                    _ints(token_idx, "token_idx", (sh.S, sh.Hkv, stride)),
+                                    _ints(n_tokens, "n_tokens", (sh.S, sh.Hkv)), stride, max_tokens,
                                     softmax_scale, _dense(out, "out", sh.S, sh), _ptr(workspace),
                                     _bytes(workspace), _stream(q)))
     return workspace
@@ -629,10 +628,9 @@ def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, wi
     n = q.shape[0] if isinstance(q, torch.Tensor) else 1
     if workspace is None:
         workspace = prompt_workspace(sh, n, q.device)
-    s = sh.c()
-    _check(lib.ck_prompt_attn(ctypes.byref(s), _dense(q, "q", n, sh), n,
-                              _ints(q_starts, "q_starts", sh.S + 1), _kv(sh, kv),
-                              _ints(lengths, "lengths", sh.S), n_sink, window, softmax_scale,
+    _check(lib.ck_prompt_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh), n,
+                              _ints(q_starts, "q_starts", (sh.S + 1,)), _kv(sh, kv),
+                              _ints(lengths, "lengths", (sh.S,)), n_sink, window, softmax_scale,
                               _dense(out, "out", n, sh), _ptr(workspace), _bytes(workspace),
                               _stream(q)))
     return workspace
@@ -641,10 +639,11 @@ def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, wi
 def ck_copy_rows(sh: Shape, src, dst, n_copy, max_rows: int, row_idx=None, begin=None, src_seq=None):
     lib = load_library()
     stride = row_idx.shape[-1] if isinstance(row_idx, torch.Tensor) else max_rows
-    s = sh.c()
-    _check(lib.ck_copy_rows(ctypes.byref(s), _kv(sh, src), _kv(sh, dst), _ints(n_copy, "n_copy", sh.S),
-                            max_rows, _ints(row_idx, "row_idx", sh.S, sh.Hkv, None), stride,
-                            _ints(begin, "begin", sh.S), _ints(src_seq, "src_seq", sh.S),
+    per_seq = (sh.S,)
+    _check(lib.ck_copy_rows(ctypes.byref(sh.c()), _kv(sh, src), _kv(sh, dst),
+                            _ints(n_copy, "n_copy", per_seq), max_rows,
+                            _ints(row_idx, "row_idx", (sh.S, sh.Hkv, stride)), stride,
+                            _ints(begin, "begin", per_seq), _ints(src_seq, "src_seq", per_seq),
                             _stream(n_copy)))
 
 

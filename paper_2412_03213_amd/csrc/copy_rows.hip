@@ -21,24 +21,21 @@ template <int LANES>                                    // of 16 bytes for a row
 __global__ __launch_bounds__(256) void k_copy_rows(const CopyArgs a) {
   const int hp = blockIdx.y, s = hp / a.Hkv, h = hp % a.Hkv;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int n = a.n_copy[s];
-  n = n < a.max_rows ? n : a.max_rows;
+  // three loads under way together, then two for every row
+  const int n_copy = a.n_copy[s], from_seq = a.src_seq ? a.src_seq[s] : s, begin = a.begin ? a.begin[s] : 0;
+  const int n = n_copy < a.max_rows ? n_copy : a.max_rows;
   const int j0 = blockIdx.x * COPY_ROWS + wave * 16;
-  if (j0 >= n) return;
-  const int from_seq = a.src_seq ? a.src_seq[s] : s;
-  if ((uint32_t)from_seq >= (uint32_t)a.src.n_seqs) return;
-  const int begin = a.begin ? a.begin[s] : 0;
   // lane x < 16 finds out where row j0 + x comes from and goes to
   const int j = j0 + (lane & 15);
-  int from = -1, to = -1;
-  if (j < n) {
-    const int64_t r = (int64_t)begin + j;
-    const int rd = r >= 0 && r < 0x7FFFFFFF ? (int)r : -1;
-    const int rs = a.row_idx ? a.row_idx[(int64_t)hp * a.idx_stride + j] : rd;
-    to = a.dst.row(s, h, rd);
-    from = a.src.row(from_seq, h, rs);
-    if (to < 0 || from < 0) from = to = -1;
-  }
+  const int64_t r = (int64_t)begin + j;
+  const int rd = j < n && r >= 0 && r < 0x7FFFFFFF ? (int)r : -1;
+  const int rs = a.row_idx ? a.row_idx[(int64_t)hp * a.idx_stride + min(j, a.max_rows - 1)] : rd;
+  const bool known = (uint32_t)from_seq < (uint32_t)a.src.n_seqs;
+  const Pages::Entry es = a.src.entry(known ? from_seq : 0, known ? rs : -1), ed = a.dst.entry(s, rd);
+  const int page_s = a.src.table[es.at], page_d = a.dst.table[ed.at];
+  int from = a.src.place(page_s, h, es.slot), to = a.dst.place(page_d, h, ed.slot);
+  if (to < 0 || from < 0) from = to = -1;
+  if (j0 >= n) return;
   constexpr int PER = 64 / LANES;                       // rows a wavefront moves with one instruction
   constexpr int U = 16 / PER;
   const int part = lane % LANES, sub = lane / LANES;

@@ -5,15 +5,14 @@
 
 namespace ck {
 
-// n / d for 0 <= n < 2^31, d >= 1: the product with a rounded-up reciprocal is the quotient or one more.
+// n / d for 0 <= n < 2^31, d >= 1: the product with a rounded-down reciprocal is the quotient or one less.
 struct Divider {
   uint32_t d, magic;
-  Divider() : d(1), magic(0) {}
-  explicit Divider(uint32_t d_) : d(d_), magic(d_ > 1 ? (uint32_t)((1ull << 32) / d_ + 1) : 0) {}
+  Divider() : d(1), magic(0xFFFFFFFFu) {}
+  explicit Divider(uint32_t d_) : d(d_), magic(d_ > 1 ? (uint32_t)((1ull << 32) / d_) : 0xFFFFFFFFu) {}
   __device__ __forceinline__ int quotient(int n) const {
-    if (d == 1) return n;                               // uniform
     const uint32_t q = __umulhi((uint32_t)n, magic);
-    return (int)(q - (q * (uint64_t)d > (uint32_t)n ? 1 : 0));
+    return (int)((uint32_t)n - q * d >= d ? q + 1 : q);
   }
 };
 
@@ -27,14 +26,21 @@ struct Pages {
       : table(kv.page_table), n_pages(kv.n_pages), n_seqs(kv.n_seqs), per_seq(kv.pages_per_seq), Hkv(Hkv_),
         rows(kv.page_size * kv.pages_per_seq), size((uint32_t)kv.page_size) {}
   __device__ __forceinline__ int clamp_length(int n) const { return n < 0 ? 0 : (n < rows ? n : rows); }
-  // pool row (of d channels) of row r of sequence s, head h; -1 where there is none
+  // Where a row's page number stands (some number that the table has, for a row that it does not have), and
+  // from the number the pool row (of d channels) of the row; -1 where there is none.  In two steps and without a
+  // branch, so that loads of several rows are under way together.
+  struct Entry { int64_t at; int slot; };               // slot < 0: no such row
+  __device__ __forceinline__ Entry entry(int s, int r) const {
+    const bool is = (uint32_t)r < (uint32_t)rows;
+    const int e = size.quotient(is ? r : 0);
+    return {(int64_t)s * per_seq + e, is ? r - e * (int)size.d : -1};
+  }
   __device__ __forceinline__ int place(int page, int h, int slot) const {
-    return (uint32_t)page < (uint32_t)n_pages ? (page * Hkv + h) * (int)size.d + slot : -1;
+    return slot >= 0 && (uint32_t)page < (uint32_t)n_pages ? (page * Hkv + h) * (int)size.d + slot : -1;
   }
   __device__ __forceinline__ int row(int s, int h, int r) const {
-    if ((uint32_t)r >= (uint32_t)rows) return -1;
-    const int e = size.quotient(r);
-    return place(table[(int64_t)s * per_seq + e], h, r - e * (int)size.d);
+    const Entry e = entry(s, r);
+    return place(table[e.at], h, e.slot);
   }
 };
 

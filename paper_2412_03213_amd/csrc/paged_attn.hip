@@ -23,7 +23,7 @@ namespace {
 constexpr float PA_NEG_BIG = -1.0e30f;                  // "no row yet": finite so that differences stay finite
 constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
-constexpr int PA_MIN_PIECE = PA_WAVES * PA_STEP;
+constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;   // two steps of each wavefront
 constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
 constexpr int PA_PART = D + 2;                          // floats of a (piece, query head): max, sum, acc[128]
 constexpr unsigned long long PA_TICKET = 0x434B5061676Eull;   // marks a ticket word as ours
@@ -42,8 +42,8 @@ struct PagedArgs {
 // What a sequence attends to: [0, sinks), the list, [recent, length).
 struct Span {
   int length, sinks, recent;
-  __device__ __forceinline__ Span(const PagedArgs& a, int s) {
-    length = a.pages.clamp_length(a.lengths[s]);
+  __device__ __forceinline__ Span(const PagedArgs& a, int n) {
+    length = a.pages.clamp_length(n);
     sinks = a.n_sink < length ? a.n_sink : length;
     recent = a.window < 0 ? sinks : max(sinks, length - a.window);
   }
@@ -62,22 +62,27 @@ __device__ __forceinline__ int64_t wave_sum_l(int64_t v) {
 // Which piece of which sequence and head this workgroup has; by every wavefront for itself.
 struct Piece {
   int s, h, split, n_split, first, length;              // first: piece 0 of (s, head 0)
+  int n_rows;                                           // lengths[s]
   __device__ __forceinline__ bool find(const PagedArgs& a, int w) {
     const int lane = threadIdx.x & 63;
-    const int listed = a.n_tokens ? a.max_tokens : 0;
+    const int listed = a.max_tokens;                    // 0 without a list
     int64_t total = 0;
-    int mine = 0;
+    int len = 0, mine = 0;
     for (int s0 = 0; s0 < a.S; s0 += WAVE) {
-      mine = s0 + lane < a.S ? Span(a, s0 + lane).rows(listed) : 0;
+      len = a.lengths[min(s0 + lane, a.S - 1)];
+      mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
       total += mine;
     }
     total = wave_sum_l(total) * a.Hkv;
-    int64_t len = (total + PA_PIECES - 1) / PA_PIECES;
-    len = (len + PA_MIN_PIECE - 1) / PA_MIN_PIECE * PA_MIN_PIECE;
-    length = len < PA_MIN_PIECE ? PA_MIN_PIECE : (int)len;
+    const int64_t even = (total + PA_PIECES - 1) / PA_PIECES;
+    length = (int)((even + PA_MIN_PIECE - 1) / PA_MIN_PIECE * PA_MIN_PIECE);
+    length = __builtin_amdgcn_readfirstlane(length < PA_MIN_PIECE ? PA_MIN_PIECE : length);
     int before = 0;
     for (int s0 = 0; s0 < a.S; s0 += WAVE) {
-      if (a.S > WAVE) mine = s0 + lane < a.S ? Span(a, s0 + lane).rows(listed) : 0;
+      if (a.S > WAVE) {
+        len = a.lengths[min(s0 + lane, a.S - 1)];
+        mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
+      }
       int n = (mine + length - 1) / length;
       n = s0 + lane < a.S ? (n < 1 ? 1 : n) : 0;
       const int upto = wave_inclusive_scan(n);
@@ -90,6 +95,7 @@ struct Piece {
         first = (before + __builtin_amdgcn_readlane(upto, l) - n_split) * a.Hkv;
         split = (w - first) / a.Hkv;
         h = (w - first) - split * a.Hkv;
+        n_rows = __builtin_amdgcn_readlane(len, l);
         return true;
       }
       before = group;
@@ -299,7 +305,7 @@ struct StateF32 {
   }
 };
 
-template <typename T, int G>
+template <typename T, int G, bool LIST>
 __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void k_paged_attn(const PagedArgs a) {
   constexpr bool BF16 = std::is_same<T, bf16>::value;
@@ -311,14 +317,15 @@ void k_paged_attn(const PagedArgs a) {
   CK_FETCH_ARG(a.q);
   CK_FETCH_ARG(a.lengths);
   CK_FETCH_ARG(a.S);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, kg = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Piece pc;
   if (!pc.find(a, blockIdx.x)) return;
   const int s = pc.s, h = pc.h, hp = s * a.Hkv + h;
-  const Span span(a, s);
+  const Span span(a, pc.n_rows);
   int listed = 0;
-  if (a.n_tokens) {
-    listed = a.n_tokens[hp];
+  if constexpr (LIST) {
+    listed = __builtin_amdgcn_readfirstlane(a.n_tokens[hp]);
     listed = listed < 0 ? 0 : (listed < a.max_tokens ? listed : a.max_tokens);
   }
   const int n_total = span.rows(listed);
@@ -346,21 +353,18 @@ void k_paged_attn(const PagedArgs a) {
 
   // Pool rows of 64 positions, lane by lane; four steps.  -1 where there is no row.
   auto logical = [&](int p) -> int {
-    if (p >= w_end) return -1;
-    if (p < span.sinks) return p;
     const int i = p - span.sinks;
-    if (i < listed) {
-      const int r = a.token_idx[(int64_t)hp * a.idx_stride + i];
-      return (uint32_t)r < (uint32_t)span.length ? r : -1;
+    int r = i < 0 ? p : span.recent + (i - listed);
+    if constexpr (LIST) {                               // the load is made for every position: no branch
+      const int x = a.token_idx[(int64_t)hp * a.idx_stride + max(0, min(i, a.max_tokens - 1))];
+      if (i >= 0 && i < listed) r = (uint32_t)x < (uint32_t)span.length ? x : -1;
     }
-    return span.recent + (i - listed);
+    return p < w_end ? r : -1;
   };
-  struct Found { int page, slot; };                     // page number as the table holds it, -1: none
+  struct Found { int page, slot; };                     // page number as the table holds it
   auto look_up = [&](int group) -> Found {
-    const int r = logical(w_begin + group * WAVE + lane);
-    if ((uint32_t)r >= (uint32_t)a.pages.rows) return {-1, 0};
-    const int e = a.pages.size.quotient(r);
-    return {a.pages.table[(int64_t)s * a.pages.per_seq + e], r - e * (int)a.pages.size.d};
+    const Pages::Entry e = a.pages.entry(s, logical(w_begin + group * WAVE + lane));
+    return {a.pages.table[e.at], e.slot};
   };
   int(*rows)[WAVE] = rows_lds[wave];
   auto put_rows = [&](int group, const Found& f) { rows[group & 1][lane] = a.pages.place(f.page, h, f.slot); };
@@ -388,27 +392,36 @@ void k_paged_attn(const PagedArgs a) {
       }
     }
   };
+  // Register sets in rotation: the loads of the next steps (three in bf16, one in fp32) are under way while one is
+  // reduced.  They go on behind the end (tokens that are not there read row 0), so that every step is followed by as
+  // many loads and waits for its own only.
+  constexpr int NS = BF16 ? 4 : 2;
   if (n_steps > 0) {                                    // wave-uniform
     put_rows(0, look_up(0));
     Found next = look_up(1);
     wave_lds_order();
-    Step cur, ahead;
-    fetch(0, cur);
-    for (int t = 0; t < n_steps; ++t) {
-      if ((t & 3) == 0) {                               // the rows of the next four steps, and those behind them
-        wave_lds_order();
-        put_rows((t >> 2) + 1, next);
-        wave_lds_order();
-        next = look_up((t >> 2) + 2);
+    Step sets[NS];
+#pragma unroll
+    for (int j = 0; j < NS - 1; ++j) fetch(j, sets[j]);
+    for (int group = 0;; ++group) {
+      wave_lds_order();
+      put_rows(group + 1, next);
+      wave_lds_order();
+      next = look_up(group + 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = group * 4 + j;
+        fetch(t + NS - 1, sets[(j + NS - 1) % NS]);
+        const int4 tr = step_rows(t);
+        if constexpr (BF16)
+          state.add(sets[j % NS], tr, qb, stage, a.scale_log2e);
+        else
+          state.add(sets[j % NS], tr, qv);
+        if (t + 1 >= n_steps) goto reduced;             // out of both loops: no path back without all of the loads
       }
-      if (t + 1 < n_steps) fetch(t + 1, ahead);
-      if constexpr (BF16)
-        state.add(cur, step_rows(t), qb, stage, a.scale_log2e);
-      else
-        state.add(cur, step_rows(t), qv);
-      cur = ahead;
     }
   }
+reduced:
   state.leave(red + wave * G * PA_PART);
   __syncthreads();
 
@@ -510,14 +523,14 @@ void k_paged_attn(const PagedArgs a) {
 
 size_t ticket_bytes(const Dims& dm) { return ((size_t)dm.HP * 8 + 255) & ~(size_t)255; }
 
-template <typename T>
+template <typename T, bool LIST>
 void launch_paged_t(int G, dim3 grid, const PagedArgs& a, hipStream_t st) {
   const dim3 block(PA_WAVES * 64);
   switch (G) {
-    case 1: hipLaunchKernelGGL((k_paged_attn<T, 1>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_paged_attn<T, 2>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_paged_attn<T, 4>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_paged_attn<T, 8>), grid, block, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_paged_attn<T, 1, LIST>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_paged_attn<T, 2, LIST>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_paged_attn<T, 4, LIST>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_paged_attn<T, 8, LIST>), grid, block, 0, st, a); break;
   }
 }
 
@@ -557,10 +570,12 @@ hipError_t launch_paged_attn(const Dims& dm, const void* q, const ck_paged_kv& k
   if (!n_tokens && most > rows) most = rows;
   const int64_t each = most > 0 ? (most + PA_MIN_PIECE - 1) / PA_MIN_PIECE : 1;
   const int64_t pieces = dm.HP * each < PA_PIECES + dm.HP ? dm.HP * each : PA_PIECES + dm.HP;
+  const dim3 grid((unsigned)pieces);
+  const bool list = a.max_tokens > 0;
   if (dm.dtype == CK_BF16)
-    launch_paged_t<bf16>(dm.G, dim3((unsigned)pieces), a, st);
+    list ? launch_paged_t<bf16, true>(dm.G, grid, a, st) : launch_paged_t<bf16, false>(dm.G, grid, a, st);
   else
-    launch_paged_t<float>(dm.G, dim3((unsigned)pieces), a, st);
+    list ? launch_paged_t<float, true>(dm.G, grid, a, st) : launch_paged_t<float, false>(dm.G, grid, a, st);
   return hipGetLastError();
 }
 

@@ -220,10 +220,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   auto look_up = [&](int t) {                           // t: a multiple of AT_ONCE; tiles behind the last have no rows
     const int tile = EIGHTS ? t + (lane >> 3) : t;
     const int r = qb.first_row(tile0 + tile) + (EIGHTS ? (lane & 7) * 8 : lane);
-    const bool is = tile < n_tiles && r < qb.end;
-    const int e = a.pages.size.quotient(is ? r : 0);
-    next_page = a.pages.table[(int64_t)qb.s * a.pages.per_seq + e];
-    next_slot = is ? r - e * (int)a.pages.size.d : -1;
+    const Pages::Entry e = a.pages.entry(qb.s, tile < n_tiles && r < qb.end ? r : -1);
+    next_page = a.pages.table[e.at];
+    next_slot = e.slot;
   };
   // Rows of a tile that are not there, as bits, of the last four tiles asked for (the newest first).
   uint64_t gone[4] = {0, 0, 0, 0};
@@ -246,7 +245,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   };
   auto rows_of = [&](int t) {                           // in turn: t = 0, 1, 2, ..
     if ((t & (AT_ONCE - 1)) == 0) {
-      place = next_slot < 0 ? -1 : a.pages.place(next_page, h, next_slot);
+      place = a.pages.place(next_page, h, next_slot);
       look_up(t + AT_ONCE);
     }
     Rows r;
