@@ -52,14 +52,14 @@ __global__ __launch_bounds__(256) void k_copy_rows(const CopyArgs a) {
       const int f = __shfl(from, x);
       t[u] = __shfl(to, x);
       if (t[u] < 0) continue;
-      k[u] = K[(int64_t)f * LANES + part];
-      v[u] = V[(int64_t)f * LANES + part];
+      k[u] = load_once(K + (int64_t)f * LANES + part);
+      v[u] = load_once(V + (int64_t)f * LANES + part);
     }
 #pragma unroll
     for (int u = 0; u < B; ++u) {
       if (t[u] < 0) continue;
-      K2[(int64_t)t[u] * LANES + part] = k[u];
-      V2[(int64_t)t[u] * LANES + part] = v[u];
+      store_once(K2 + (int64_t)t[u] * LANES + part, k[u]);
+      store_once(V2 + (int64_t)t[u] * LANES + part, v[u]);
     }
   }
 }

@@ -16,6 +16,18 @@ struct Divider {
   }
 };
 
+// 16 bytes that are read or written once: they go past the caches' order of use, and a write does not stay in
+// L2 until the end of the launch has it written back.
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4)));
+  const Words w = __builtin_nontemporal_load(static_cast<const Words*>(p));
+  return make_uint4(w.x, w.y, w.z, w.w);
+}
+__device__ __forceinline__ void store_once(void* p, const uint4& x) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(Words{x.x, x.y, x.z, x.w}, static_cast<Words*>(p));
+}
+
 struct Pages {
   const int32_t* table;
   int n_pages, n_seqs, per_seq, Hkv;

@@ -50,9 +50,6 @@ struct Span {
   __device__ __forceinline__ int rows(int listed) const { return sinks + listed + length - recent; }
 };
 
-__device__ __forceinline__ int wave_sum_i(int v) {
-  return __builtin_amdgcn_readlane(wave_inclusive_scan(v), WAVE - 1);
-}
 __device__ __forceinline__ int64_t wave_sum_l(int64_t v) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
@@ -382,8 +379,8 @@ void k_paged_attn(const PagedArgs a) {
     for (int i = 0; i < 4; ++i) {
       const int64_t at = (int64_t)(w[i] < 0 ? 0 : w[i]) * D;
       if constexpr (BF16) {
-        r.k[i] = *reinterpret_cast<const uint4*>(Kc + at);
-        r.v[i] = *reinterpret_cast<const uint4*>(Vc + at);
+        r.k[i] = LIST ? *reinterpret_cast<const uint4*>(Kc + at) : load_once(Kc + at);
+        r.v[i] = LIST ? *reinterpret_cast<const uint4*>(Vc + at) : load_once(Vc + at);
       } else {
         r.k[i][0] = reinterpret_cast<const float4*>(Kc + at)[0];
         r.k[i][1] = reinterpret_cast<const float4*>(Kc + at)[1];

@@ -29,8 +29,8 @@ enum { PAIRS_ADJACENT = 0, PAIRS_HALVES = 1, PAIRS_HALVES_ANY = 2 };   // 1: rot
 template <typename T> struct Vec8;
 template <> struct Vec8<bf16> {
   uint4 w;
-  __device__ __forceinline__ void load(const bf16* p) { w = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void store(bf16* p) const { *reinterpret_cast<uint4*>(p) = w; }
+  __device__ __forceinline__ void load(const bf16* p) { w = load_once(p); }
+  __device__ __forceinline__ void store(bf16* p) const { store_once(p, w); }
   __device__ __forceinline__ void unpack(float (&x)[8]) const {
     x[0] = lo_bf16(w.x); x[1] = hi_bf16(w.x); x[2] = lo_bf16(w.y); x[3] = hi_bf16(w.y);
     x[4] = lo_bf16(w.z); x[5] = hi_bf16(w.z); x[6] = lo_bf16(w.w); x[7] = hi_bf16(w.w);
@@ -55,12 +55,12 @@ template <> struct Vec8<bf16> {
 template <> struct Vec8<float> {
   float4 a, b;
   __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+    a = __builtin_bit_cast(float4, load_once(p));
+    b = __builtin_bit_cast(float4, load_once(p + 4));
   }
   __device__ __forceinline__ void store(float* p) const {
-    reinterpret_cast<float4*>(p)[0] = a;
-    reinterpret_cast<float4*>(p)[1] = b;
+    store_once(p, __builtin_bit_cast(uint4, a));
+    store_once(p + 4, __builtin_bit_cast(uint4, b));
   }
   __device__ __forceinline__ void unpack(float (&x)[8]) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
