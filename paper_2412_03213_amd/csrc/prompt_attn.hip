@@ -150,11 +150,20 @@ __device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
 
 // 16 bytes for every lane from base + offset to LDS at `to` + 16 * lane, on their way when this returns:
 // they are counted with the vector loads (wait_for_tiles).
+// ONCE: no other workgroup reads them.
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(offset), "s"(base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+  if constexpr (ONCE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 template <int LEFT>                                     // loads that may still be on their way
 __device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
@@ -174,7 +183,8 @@ struct Tiles {
 };
 
 // EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page.
-template <int G, bool EIGHTS>
+// SPLIT: the tiles of a block are cut into pieces (a.n_split > 1).
+template <int G, bool EIGHTS, bool SPLIT>
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
   constexpr int TILE_BYTES = PR_TILE * D * 2;
   __shared__ __attribute__((aligned(1024))) char k_tiles[PR_BUFFERS][TILE_BYTES];
@@ -183,12 +193,12 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   static_assert(PR_WAVES == 8 && PR_TILE == 64 && PR_BUFFERS == 3, "eight rows of a tile for each wavefront");
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv, block = w / a.n_split, piece = w % a.n_split;
+  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv, n_split = SPLIT ? a.n_split : 1, block = w / n_split, piece = w % n_split;
   QueryBlock qb;
   if (!qb.find(a, block, PR_ROWS / G)) return;
-  const int tile0 = piece * qb.piece_tiles(a.n_split), n_pieces = qb.pieces(a.n_split);
+  const int tile0 = piece * qb.piece_tiles(n_split), n_pieces = qb.pieces(n_split);
   if (piece >= n_pieces) return;
-  const int n_tiles = min(qb.piece_tiles(a.n_split), qb.n_tiles - tile0);
+  const int n_tiles = min(qb.piece_tiles(n_split), qb.n_tiles - tile0);
 
   // ---- queries: lane holds channels 16 sl + 8 half + (0..7) of row `col` ----
   const QueryRow mine = QueryRow::of<G>(a, qb, h, wave * 32 + col);
@@ -238,9 +248,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if constexpr (EIGHTS)
-        load_to_lds(reinterpret_cast<const char*>(pool) + (int64_t)r.at[0] * (D * 2), own[i], to + i * 1024);
+        load_to_lds<SPLIT>(reinterpret_cast<const char*>(pool) + (int64_t)r.at[0] * (D * 2), own[i], to + i * 1024);
       else
-        load_to_lds(reinterpret_cast<const char*>(pool) + ((int64_t)r.at[i] * (D * 2) + own[i]), to + i * 1024);
+        load_to_lds<SPLIT>(reinterpret_cast<const char*>(pool) + ((int64_t)r.at[i] * (D * 2) + own[i]), to + i * 1024);
     }
   };
   auto rows_of = [&](int t) {                           // in turn: t = 0, 1, 2, ..
@@ -417,22 +427,16 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     wait_for_tiles<0>();
     check_values(0, gone[2], 0);
     group_barrier();
-    Scores sa, sb;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const Group k = read_keys(0, g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) score(k, g, i, sa);
-    }
-    seen = mask(0, gone[2], sa);
-    {
-      float mx = PR_NEG_BIG;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
-      raise(mx);
-    }
     // buffers of tiles t, t + 1 and t + 2
     uint32_t b0 = 0, b1 = TILE_BYTES, b2 = 2 * TILE_BYTES;
+    auto arrived = [&](int t) {                         // tile t + 1 is in LDS
+      wait_for_tiles<4>();                              // all but the last four that have been asked for
+      check_values(t + 1, gone[2], b1);
+      const uint32_t b = b0;
+      b0 = b1;
+      b1 = b2;
+      b2 = b;
+    };
     auto use_tile = [&](int t, Scores& sc, Scores& next) {
       group_barrier();
       request(t + 3, b2, b0);
@@ -493,24 +497,39 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       add_odd_values(t, gone[3]);
       seen = next_seen;
       raise(mx);
-      wait_for_tiles<4>();                              // all but the last four that have been asked for
-      check_values(t + 1, gone[2], b1);
-      const uint32_t b = b0;
-      b0 = b1;
-      b1 = b2;
-      b2 = b;
+      arrived(t);
     };
-    for (int t = 0; t < n_tiles; t += 2) {
-      use_tile(t, sa, sb);
-      use_tile(t + 1, sb, sa);
+    if (wave * 32 < qb.n_tok * G) {
+      Scores sa, sb;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const Group k = read_keys(0, g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) score(k, g, i, sa);
+      }
+      seen = mask(0, gone[2], sa);
+      float mx = PR_NEG_BIG;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
+      raise(mx);
+      for (int t = 0; t < n_tiles; t += 2) {
+        use_tile(t, sa, sb);
+        use_tile(t + 1, sb, sa);
+      }
+    } else {                                            // no query: this wavefront brings its rows, nothing more
+      for (int t = 0; t < n_tiles + (n_tiles & 1); ++t) {
+        group_barrier();
+        request(t + 3, b2, b0);
+        arrived(t);
+      }
     }
     wait_for_tiles<0>();                                // nothing is on its way to LDS behind the end
   }
 
   l = xor32(l, OpSum());
   if (!mine.there) return;
-  if (n_pieces > 1) {
-    const Partial to(a.part, ((int64_t)block * a.Hkv + h) * a.n_split + piece);
+  if (SPLIT && n_pieces > 1) {
+    const Partial to(a.part, ((int64_t)block * a.Hkv + h) * n_split + piece);
     *to.stats(tid) = make_float2(m, l);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -539,18 +558,32 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs 
   if (n == 1 || !mine.there) return;
   const int64_t first = ((int64_t)block * a.Hkv + h) * a.n_split;
   float m = PR_NEG_BIG, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < n; ++k) {
-    const Partial from(a.part, first + k);
-    const float2 st = *from.stats(tid);
-    const float4 f = *from.four(i, tid);
-    const float mx = fmaxf(m, st.x);
-    const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e), add = __builtin_amdgcn_exp2f((st.x - mx) * a.scale_log2e);
-    m = mx;
-    l = l * old + st.y * add;
-    x[0] = x[0] * old + f.x * add;
-    x[1] = x[1] * old + f.y * add;
-    x[2] = x[2] * old + f.z * add;
-    x[3] = x[3] * old + f.w * add;
+  constexpr int BATCH = 8;                              // pieces whose loads are under way together
+  for (int k0 = 0; k0 < n; k0 += BATCH) {
+    float2 st[BATCH];
+    float4 f[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {                   // the last one again behind the end
+      const Partial from(a.part, first + min(k0 + k, n - 1));
+      st[k] = *from.stats(tid);
+      f[k] = *from.four(i, tid);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      if (k0 + k >= n) {                                // uniform
+        st[k] = make_float2(PR_NEG_BIG, 0.f);
+        f[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      const float mx = fmaxf(m, st[k].x);
+      const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e), add = __builtin_amdgcn_exp2f((st[k].x - mx) * a.scale_log2e);
+      m = mx;
+      l = l * old + st[k].y * add;
+      x[0] = x[0] * old + f[k].x * add;
+      x[1] = x[1] * old + f[k].y * add;
+      x[2] = x[2] * old + f[k].z * add;
+      x[3] = x[3] * old + f[k].w * add;
+    }
   }
   const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
@@ -558,14 +591,14 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs 
   store_four(a.out + mine.at, i >> 2, i & 3, lane >> 5, x);
 }
 
-template <bool EIGHTS>
+template <bool EIGHTS, bool SPLIT>
 void launch_prompt_g(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
   const dim3 grid(blocks * a.Hkv * a.n_split), block(PR_WAVES * 64);
   switch (G) {
-    case 1: hipLaunchKernelGGL((k_prompt_attn<1, EIGHTS>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_prompt_attn<2, EIGHTS>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_prompt_attn<4, EIGHTS>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_prompt_attn<8, EIGHTS>), grid, block, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_prompt_attn<1, EIGHTS, SPLIT>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_prompt_attn<2, EIGHTS, SPLIT>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_prompt_attn<4, EIGHTS, SPLIT>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_prompt_attn<8, EIGHTS, SPLIT>), grid, block, 0, st, a); break;
   }
 }
 void launch_join(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
@@ -619,11 +652,13 @@ hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, con
   a.n_split = prompt_split(dm, n_rows);
   a.scale_log2e = softmax_scale * 1.4426950408889634f;
   const unsigned blocks = (unsigned)prompt_blocks(dm, n_rows);
-  if (kv.page_size % 8 == 0)
-    launch_prompt_g<true>(dm.G, blocks, a, st);
-  else
-    launch_prompt_g<false>(dm.G, blocks, a, st);
-  if (a.n_split > 1) launch_join(dm.G, blocks, a, st);
+  const bool eights = kv.page_size % 8 == 0;
+  if (a.n_split == 1) {
+    eights ? launch_prompt_g<true, false>(dm.G, blocks, a, st) : launch_prompt_g<false, false>(dm.G, blocks, a, st);
+  } else {
+    eights ? launch_prompt_g<true, true>(dm.G, blocks, a, st) : launch_prompt_g<false, true>(dm.G, blocks, a, st);
+    launch_join(dm.G, blocks, a, st);
+  }
   return hipGetLastError();
 }
 
