@@ -203,9 +203,6 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   // ---- queries: lane holds channels 16 sl + 8 half + (0..7) of row `col` ----
   const QueryRow mine = QueryRow::of<G>(a, qb, h, wave * 32 + col);
   bf16x8 q[8];
-#pragma unroll
-  for (int sl = 0; sl < 8; ++sl)
-    q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.q + mine.at + sl * 16 + half * 8));
   const int p = mine.there ? qb.p0 + mine.token : -1;   // last row that the lane's query sees
   const int p_lo = qb.p0 + wave * 32 / G;               // of the wavefront's first query
 
@@ -412,8 +409,11 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   // values of t + 2, whose buffers were read for tile t - 1; what was asked for before that has to be there at its end.
   // Tiles behind the last one are asked for and scored too (rows that the pool has, all masked): no conditions.
   if (n_tiles > 0) {
-    __builtin_amdgcn_s_waitcnt(0);                      // the queries: no wait for them inside the loop
     look_up(0);
+#pragma unroll
+    for (int sl = 0; sl < 8; ++sl)
+      q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(a.q + mine.at + sl * 16 + half * 8));
+    __builtin_amdgcn_s_waitcnt(0);                      // the queries: no wait for them inside the loop
     Rows v_rows, k_rows = rows_of(0);
     bring(a.K, k_rows, own_k);
     auto request = [&](int t, uint32_t v_buffer, uint32_t k_buffer) {   // keys of tile t, values of t - 1
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     };
     request(1, 0, TILE_BYTES);
     request(2, TILE_BYTES, 2 * TILE_BYTES);
-    wait_for_tiles<0>();
+    wait_for_tiles<4>();
     check_values(0, gone[2], 0);
     group_barrier();
     // buffers of tiles t, t + 1 and t + 2
