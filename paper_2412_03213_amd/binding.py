@@ -1,5 +1,5 @@
-"""Binding of libclusterkv.so: argument marshalling only, through ctypes and, for the call
-that is made once per layer and generated token, through the native _ckhost module where it
+"""Binding of libclusterkv.so: argument marshalling only, through ctypes and, for the calls
+that are made once per layer and generated token, through the native _ckhost module where it
 has been built for this interpreter.
 
 Functions carry the names of the C entry points (include/clusterkv.h) and take
@@ -84,11 +84,16 @@ def _host_decode_step():
     """Marshals plain arguments of ck_decode_step natively and returns the status code, or None
     for any others.  Without a module for this interpreter every call is of the latter kind:
     the library is the same, the call takes 4 us longer on the host."""
+    return _host("decode_step")
+
+
+def _host(name):
     try:
         from . import _ckhost
     except ImportError:
         return lambda *args: None
-    return _ckhost.decode_step
+    _ckhost.set_types(torch.bfloat16, torch.float32, torch.int32, torch.uint8)
+    return getattr(_ckhost, name)
 
 
 def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
@@ -177,6 +182,10 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.ck_probe_mfma_bf16.argtypes = [I32, I32, P, P, P, ctypes.POINTER(ctypes.c_double), P]
     lib.host_decode_step = _host_decode_step()
     lib.decode_step_entry = ctypes.cast(lib.ck_decode_step, P).value
+    lib.host_rope_append = _host("rope_append")
+    lib.rope_append_entry = ctypes.cast(lib.ck_rope_append, P).value
+    lib.host_paged_decode_attn = _host("paged_decode_attn")
+    lib.paged_decode_attn_entry = ctypes.cast(lib.ck_paged_decode_attn, P).value
     _lib = lib
     return lib
 
@@ -508,6 +517,7 @@ class PagedKV:
         self._c = _CkPagedKV(_ptr(K), _ptr(V), _ptr(page_table), K.shape[0], K.shape[2],
                              page_table.shape[0], page_table.shape[1])
         self._d = K.shape[3]
+        self._address = ctypes.addressof(self._c)
 
     def c(self, sh: Shape) -> _CkPagedKV:
         if self.Hkv != sh.Hkv or self._d != sh.d or self.dtype != sh.torch_dtype:
@@ -571,6 +581,14 @@ def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None,
     """q, k, v: token rows [n, heads, d], views of one projection's output among them; freqs: device
     float32 [rot_dim / 2]; q and q_out may both be None.  interleaved: adjacent channels turn."""
     lib = load_library()
+    flags = CK_ROPE_ADJACENT if interleaved else CK_ROPE_HALVES
+    stream = _stream(k)
+    rc = lib.host_rope_append(lib.rope_append_entry, sh, kv, q, k, v, q_out, lengths, freqs,
+                              q_starts, positions, attn_factor, flags, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return
     n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
     qp, qs = _rows(q, "q", n, sh.Hq, sh)
     kp, ks = _rows(k, "k", n, sh.Hkv, sh)
@@ -583,9 +601,8 @@ def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None,
     _check(lib.ck_rope_append(ctypes.byref(sh.c()), qp, kp, vp, qs, ks, vs, n,
                               _ints(q_starts, "q_starts", (sh.S + 1,)),
                               _ints(lengths, "lengths", (sh.S,)), _ints(positions, "positions", (n,)),
-                              _ptr(freqs), rot, attn_factor,
-                              CK_ROPE_ADJACENT if interleaved else CK_ROPE_HALVES,
-                              _dense(q_out, "q_out", n, sh), _kv(sh, kv), _stream(k)))
+                              _ptr(freqs), rot, attn_factor, flags,
+                              _dense(q_out, "q_out", n, sh), _kv(sh, kv), stream))
 
 
 def paged_decode_workspace(sh: Shape, device) -> torch.Tensor:
@@ -608,6 +625,14 @@ def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window
         softmax_scale = sh.d ** -0.5
     if workspace is None:
         workspace = paged_decode_workspace(sh, q.device)
+    stream = _stream(q)
+    rc = lib.host_paged_decode_attn(lib.paged_decode_attn_entry, sh, kv, q, lengths, out, token_idx,
+                                    n_tokens, workspace, n_sink, window, max_tokens, softmax_scale,
+                                    stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return workspace
     stride = token_idx.shape[-1] if isinstance(token_idx, torch.Tensor) else 0
     if max_tokens is None:
         max_tokens = stride
@@ -616,7 +641,7 @@ def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window
                                     _ints(token_idx, "token_idx", (sh.S, sh.Hkv, stride)),
                                     _ints(n_tokens, "n_tokens", (sh.S, sh.Hkv)), stride, max_tokens,
                                     softmax_scale, _dense(out, "out", sh.S, sh), _ptr(workspace),
-                                    _bytes(workspace), _stream(q)))
+                                    _bytes(workspace), stream))
     return workspace
 
 

@@ -83,7 +83,7 @@ def build(force: bool = False, verbose: bool = True) -> str:
             run([CXX, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", INCLUDE,
                  "-I", sysconfig.get_paths()["include"], HOST_SRC, "-o", HOST_LIB])
         except (RuntimeError, OSError) as e:
-            print(f"_ckhost is not built, decode_step is called through ctypes: {e}", flush=True)
+            print(f"_ckhost is not built, every call goes through ctypes: {e}", flush=True)
     return LIB
 
 

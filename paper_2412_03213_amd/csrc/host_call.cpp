@@ -1,12 +1,15 @@
-// ck_decode_step for the Python binding without ctypes in between.  The call is made once per
-// layer and generated token, and at small batches its marshalling (fifteen tensors, two method
+// The calls that are made once per layer and generated token, for the Python binding without ctypes
+// in between: ck_decode_step, ck_rope_append and ck_paged_decode_attn.
+//
+// ck_decode_step is made once per layer and generated token, and at small batches its marshalling (fifteen tensors, two method
 // calls and two ctypes conversions each) took longer than the kernel: 9.9 us from call to call
 // for 2 head-problems, B = 256, where the kernel needs 7.1.  The host now needs 5.9 us.
 //
 // decode_step(entry, shape, 15 tensors, 9 numbers) takes what ck_decode_step takes, `entry` being
 // its address.  It returns the status code, or None if any argument is not of the plain
 // kind (a contiguous tensor, a number): nothing has been called then, and the caller goes the
-// general way, which accepts or refuses the arguments in its own words.
+// general way, which accepts or refuses the arguments in its own words.  The other two do the same;
+// they also look at the tensors' types, shapes and strides, as the general way does.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -16,8 +19,10 @@ namespace {
 
 using Entry = decltype(&ck_decode_step);
 
-PyObject *s_is_contiguous, *s_data_ptr;
+PyObject *s_is_contiguous, *s_data_ptr, *s_dtype, *s_size, *s_stride, *s_hkv, *s_d, *s_address;
 PyObject* s_shape[7];
+PyObject* types[4];                                     // torch's bfloat16 and float32 (CK_BF16, CK_F32), int32, uint8
+enum { INT32 = 2, UINT8 = 3 };
 
 bool as_int(PyObject* o, int64_t* v) {
   if (!o || !PyLong_Check(o)) return false;
@@ -97,9 +102,178 @@ PyObject* decode_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromLong(rc);
 }
 
+// ---- tensors of a given type, shape and layout ----
+bool has_type(PyObject* t, PyObject* type) {
+  PyObject* a = PyObject_GetAttr(t, s_dtype);
+  const bool ok = a && a == type;
+  Py_XDECREF(a);
+  return ok;
+}
+// attribute or result of a method: a tuple of n numbers at most 4
+bool as_tuple(PyObject* tuple, int n, int64_t* v) {
+  bool ok = tuple && PyTuple_Check(tuple) && PyTuple_GET_SIZE(tuple) == n;
+  for (int i = 0; ok && i < n; ++i) ok = as_int(PyTuple_GET_ITEM(tuple, i), &v[i]);
+  Py_XDECREF(tuple);
+  return ok;
+}
+bool has_shape(PyObject* t, int n, const int64_t* shape) {
+  int64_t v[4];
+  if (!as_tuple(PyObject_GetAttr(t, s_size), n, v)) return false;
+  for (int i = 0; i < n; ++i)
+    if (v[i] != shape[i]) return false;
+  return true;
+}
+// contiguous, of a type and shape; None is a null pointer where it may be
+bool as_dense(PyObject* t, PyObject* type, int n, const int64_t* shape, void** p, bool may_be_none = false) {
+  if (t == Py_None) {
+    *p = nullptr;
+    return may_be_none;
+  }
+  return !PyLong_Check(t) && has_type(t, type) && has_shape(t, n, shape) && as_pointer(t, p);
+}
+// token rows [n, heads, d] that may lie apart
+bool as_rows(PyObject* t, PyObject* type, const int64_t (&shape)[3], void** p, int64_t* row_stride) {
+  if (t == Py_None || PyLong_Check(t) || !has_type(t, type) || !has_shape(t, 3, shape)) return false;
+  int64_t st[3];
+  if (!as_tuple(PyObject_CallMethodNoArgs(t, s_stride), 3, st)) return false;
+  if (st[2] != 1 || (st[1] != shape[2] && shape[1] > 1)) return false;
+  *row_stride = shape[0] > 1 ? st[0] : shape[1] * shape[2];
+  PyObject* a = PyObject_CallMethodNoArgs(t, s_data_ptr);
+  int64_t v = 0;
+  const bool ok = as_int(a, &v);
+  Py_XDECREF(a);
+  *p = reinterpret_cast<void*>(static_cast<uintptr_t>(v));
+  return ok;
+}
+// a cache in pages: its structure's address, if its heads and type are the shape's
+bool as_paged(PyObject* kv, const ck_shape& sh, const ck_paged_kv** p) {
+  int64_t v[2], address;
+  PyObject* const names[2] = {s_hkv, s_d};
+  PyObject* a = PyObject_GetAttr(kv, s_address);
+  bool ok = as_int(a, &address);
+  Py_XDECREF(a);
+  for (int i = 0; ok && i < 2; ++i) {
+    a = PyObject_GetAttr(kv, names[i]);
+    ok = as_int(a, &v[i]);
+    Py_XDECREF(a);
+  }
+  *p = reinterpret_cast<const ck_paged_kv*>(static_cast<uintptr_t>(ok ? address : 0));
+  return ok && *p && v[0] == sh.Hkv && v[1] == sh.d && has_type(kv, types[sh.dtype]);
+}
+bool as_float(PyObject* o, double* v) {
+  if (!PyFloat_Check(o)) return false;
+  *v = PyFloat_AS_DOUBLE(o);
+  return true;
+}
+bool as_call(PyObject* const* args, int64_t* entry, ck_shape* sh, const ck_paged_kv** kv, PyObject** type) {
+  if (!types[0] || !as_int(args[0], entry) || *entry == 0 || !as_shape(args[1], sh)) return false;
+  if (sh->dtype != CK_BF16 && sh->dtype != CK_F32) return false;
+  *type = types[sh->dtype];
+  return as_paged(args[2], *sh, kv);
+}
+PyObject* not_plain() {
+  PyErr_Clear();
+  Py_RETURN_NONE;
+}
+
+// set_types(bfloat16, float32, int32, uint8): torch's
+PyObject* set_types(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "set_types: wrong number of arguments");
+    return nullptr;
+  }
+  for (int i = 0; i < 4; ++i) {
+    Py_INCREF(args[i]);
+    Py_XSETREF(types[i], args[i]);
+  }
+  Py_RETURN_NONE;
+}
+
+// rope_append(entry, shape, cache, q, k, v, q_out, lengths, freqs, q_starts, positions, factor, flags, stream)
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 14) {
+    PyErr_SetString(PyExc_TypeError, "rope_append: wrong number of arguments");
+    return nullptr;
+  }
+  int64_t entry, stream, flags, n = 0, s_q = 0, s_k, s_v, n_freqs = 0;
+  ck_shape sh;
+  const ck_paged_kv* kv;
+  PyObject* type;
+  void *q = nullptr, *k, *v, *q_out, *lengths, *freqs, *starts, *positions;
+  double factor;
+  if (!as_call(a, &entry, &sh, &kv, &type)) return not_plain();
+  int64_t size[3];
+  if (!as_tuple(PyObject_GetAttr(a[4], s_size), 3, size)) return not_plain();
+  n = size[0];
+  const int64_t rows_q[3] = {n, sh.Hq, sh.d}, rows_k[3] = {n, sh.Hkv, sh.d}, per_seq[1] = {sh.S};
+  const int64_t n_starts[1] = {(int64_t)sh.S + 1}, per_row[1] = {n};
+  if (!as_tuple(PyObject_GetAttr(a[8], s_size), 1, &n_freqs)) return not_plain();
+  const int64_t rates[1] = {n_freqs};
+  const bool queries = a[3] != Py_None;
+  s_q = (int64_t)sh.Hq * sh.d;
+  const bool ok = (!queries || as_rows(a[3], type, rows_q, &q, &s_q)) && as_rows(a[4], type, rows_k, &k, &s_k) &&
+                  as_rows(a[5], type, rows_k, &v, &s_v) && as_dense(a[6], type, 3, rows_q, &q_out, !queries) &&
+                  as_dense(a[7], types[INT32], 1, per_seq, &lengths) && as_dense(a[8], types[CK_F32], 1, rates, &freqs) &&
+                  as_dense(a[9], types[INT32], 1, n_starts, &starts, true) &&
+                  as_dense(a[10], types[INT32], 1, per_row, &positions, true) && as_float(a[11], &factor) &&
+                  as_int(a[12], &flags) && as_int(a[13], &stream) && n_freqs <= INT32_MAX / 2;
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_rope_append)>(static_cast<uintptr_t>(entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, q, k, v, s_q, s_k, s_v, n, (const int32_t*)starts, (const int32_t*)lengths, (const int32_t*)positions,
+          (const float*)freqs, (int32_t)(2 * n_freqs), (float)factor, (uint32_t)flags, q_out, kv,
+          reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// paged_decode_attn(entry, shape, cache, q, lengths, out, token_idx, n_tokens, workspace, n_sink, window, max_tokens,
+//                   scale, stream); max_tokens may be None: the lists' width
+PyObject* paged_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 14) {
+    PyErr_SetString(PyExc_TypeError, "paged_decode_attn: wrong number of arguments");
+    return nullptr;
+  }
+  int64_t entry, stream, sink, window, width = 0, ws_bytes;
+  int32_t most;
+  ck_shape sh;
+  const ck_paged_kv* kv;
+  PyObject* type;
+  void *q, *lengths, *out, *list, *counts, *ws;
+  double scale;
+  if (!as_call(a, &entry, &sh, &kv, &type)) return not_plain();
+  if (a[6] != Py_None) {
+    int64_t size[3];
+    if (!as_tuple(PyObject_GetAttr(a[6], s_size), 3, size)) return not_plain();
+    width = size[2];
+  }
+  const int64_t rows[3] = {sh.S, sh.Hq, sh.d}, per_seq[1] = {sh.S}, heads[2] = {sh.S, sh.Hkv};
+  const int64_t lists[3] = {sh.S, sh.Hkv, width};
+  bool ok = as_dense(a[3], type, 3, rows, &q) && as_dense(a[4], types[INT32], 1, per_seq, &lengths) &&
+            as_dense(a[5], type, 3, rows, &out) && as_dense(a[6], types[INT32], 3, lists, &list, true) &&
+            as_dense(a[7], types[INT32], 2, heads, &counts, true) && as_int(a[9], &sink) && as_int(a[10], &window) &&
+            as_float(a[12], &scale) && as_int(a[13], &stream) && width <= INT32_MAX;
+  if (ok) ok = as_tuple(PyObject_GetAttr(a[8], s_size), 1, &ws_bytes) && as_dense(a[8], types[UINT8], 1, &ws_bytes, &ws);
+  most = (int32_t)width;
+  if (ok && a[11] != Py_None) ok = as_i32(a[11], &most);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_paged_decode_attn)>(static_cast<uintptr_t>(entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, q, kv, (const int32_t*)lengths, sink, window, (const int32_t*)list, (const int32_t*)counts,
+          (int32_t)width, most, (float)scale, out, ws, (size_t)ws_bytes,
+          reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+#define CK_METHOD(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
-    {"decode_step", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(decode_step)),
-     METH_FASTCALL, "ck_decode_step on plain tensors; None if an argument is of another kind"},
+    {"decode_step", CK_METHOD(decode_step), "ck_decode_step on plain tensors; None if an argument is of another kind"},
+    {"rope_append", CK_METHOD(rope_append), "ck_rope_append, likewise"},
+    {"paged_decode_attn", CK_METHOD(paged_decode_attn), "ck_paged_decode_attn, likewise"},
+    {"set_types", CK_METHOD(set_types), "torch's bfloat16, float32, int32 and uint8"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ckhost", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
@@ -110,7 +284,10 @@ PyMODINIT_FUNC PyInit__ckhost(void) {
   static const char* const names[7] = {"S", "Hq", "Hkv", "d", "N_cap", "C_cap", "dtype"};
   for (int i = 0; i < 7; ++i)
     if (!(s_shape[i] = PyUnicode_InternFromString(names[i]))) return nullptr;
-  if (!(s_is_contiguous = PyUnicode_InternFromString("is_contiguous"))) return nullptr;
-  if (!(s_data_ptr = PyUnicode_InternFromString("data_ptr"))) return nullptr;
+  const struct { PyObject** to; const char* name; } more[] = {
+      {&s_is_contiguous, "is_contiguous"}, {&s_data_ptr, "data_ptr"}, {&s_dtype, "dtype"}, {&s_size, "shape"},
+      {&s_stride, "stride"}, {&s_hkv, "Hkv"}, {&s_d, "_d"}, {&s_address, "_address"}};
+  for (const auto& m : more)
+    if (!(*m.to = PyUnicode_InternFromString(m.name))) return nullptr;
   return PyModule_Create(&module);
 }

@@ -223,3 +223,100 @@ def test_rates_refuse(bad):
         ck.ck_rope_frequencies(**{**dict(kind=0, rot_dim=128, trained_len=4096.0, fast=32.0, slow=1.0, factor=2.0),
                                   **bad})
     assert e.value.code == EINVALID
+
+
+def _either_way(call, name):
+    """What a call raises with the native marshalling and without it."""
+    lib = ck.load_library()
+    seen = []
+    real = getattr(lib, name)
+    for form in (real, lambda *args: None):
+        setattr(lib, name, form)
+        try:
+            with pytest.raises((ck.ClusterKVError, ValueError, ctypes.ArgumentError)) as e:
+                call()
+        finally:
+            setattr(lib, name, real)
+        seen.append((type(e.value), str(e.value)))
+    return seen
+
+
+_ROPE_CHANGES = {
+    "refused by the library": {}, "strided heads": {"q": lambda a: a["q"].transpose(0, 1)},
+    "channels apart": {"k": lambda a: torch.zeros(3, 2, 256, dtype=torch.bfloat16)[..., ::2]},
+    "other type": {"v": lambda a: a["v"].float()}, "no values": {"v": lambda a: None},
+    "address": {"k": lambda a: 4096}, "no queries": {"q": lambda a: None, "q_out": lambda a: None},
+    "queries without an output": {"q_out": lambda a: None}, "one output row short": {"q_out": lambda a: a["q_out"][:2]},
+    "wide lengths": {"lengths": lambda a: a["lengths"].long()}, "no lengths": {"lengths": lambda a: None},
+    "half rates": {"freqs": lambda a: a["freqs"].bfloat16()}, "table of rates": {"freqs": lambda a: a["freqs"][None]},
+    "starts": {"q_starts": lambda a: torch.zeros(3, dtype=torch.int32)},
+    "positions": {"positions": lambda a: torch.zeros(2, dtype=torch.int32)},
+    "whole factor": {"attn_factor": lambda a: 0}, "other heads": {"kv": lambda a: _cpu_cache(Hkv=1)},
+    "other cache type": {"kv": lambda a: _cpu_cache(dtype=torch.float32)}, "no cache": {"kv": lambda a: None},
+}
+
+
+def _cpu_cache(Hkv=2, dtype=torch.bfloat16):
+    K = torch.zeros(4, Hkv, 8, 128, dtype=dtype)
+    return ck.PagedKV(K, torch.zeros_like(K), torch.zeros(3, 1, dtype=torch.int32))
+
+
+@pytest.mark.parametrize("what", _ROPE_CHANGES)
+def test_rope_append_refuses_the_same_calls_on_either_way(what):
+    bf = dict(dtype=torch.bfloat16)
+    a = dict(q=torch.zeros(3, 4, 128, **bf), k=torch.zeros(3, 2, 128, **bf), v=torch.zeros(3, 2, 128, **bf),
+             kv=_cpu_cache(), lengths=torch.zeros(3, dtype=torch.int32), freqs=torch.zeros(64),
+             q_out=torch.zeros(3, 4, 128, **bf), attn_factor=float("inf"))    # refused where all else is right
+    for k, change in _ROPE_CHANGES[what].items():
+        a[k] = change(a)
+    native, general = _either_way(lambda: ck.ck_rope_append(ck.Shape(3, 4, 2, 8, 1), **a), "host_rope_append")
+    assert native == general
+
+
+_DECODE_CHANGES = {
+    "refused by the library": {}, "strided": {"q": lambda a: a["q"].transpose(0, 1)},
+    "other type": {"out": lambda a: a["out"].float()}, "no output": {"out": lambda a: None},
+    "address": {"q": lambda a: 4096}, "wide lengths": {"lengths": lambda a: a["lengths"].long()},
+    "list": {"token_idx": lambda a: torch.zeros(3, 2, 5, dtype=torch.int32)},
+    "list of one head": {"token_idx": lambda a: torch.zeros(3, 1, 5, dtype=torch.int32)},
+    "flat list": {"token_idx": lambda a: torch.zeros(30, dtype=torch.int32)},
+    "counts": {"n_tokens": lambda a: torch.zeros(3, 2, dtype=torch.int32)},
+    "flat counts": {"n_tokens": lambda a: torch.zeros(6, dtype=torch.int32)},
+    "small workspace": {"workspace": lambda a: a["workspace"][:8], "n_sink": lambda a: 0},
+    "workspace of words": {"workspace": lambda a: torch.zeros(2, dtype=torch.int32), "n_sink": lambda a: 0},
+    "most": {"max_tokens": lambda a: 2.5}, "whole scale": {"softmax_scale": lambda a: 1},
+    "other heads": {"kv": lambda a: _cpu_cache(Hkv=1)}, "no cache": {"kv": lambda a: None},
+    "sinks": {"n_sink": lambda a: 1.0}, "wide window": {"window": lambda a: 1 << 70},
+}
+
+
+@pytest.mark.parametrize("what", _DECODE_CHANGES)
+def test_paged_decode_refuses_the_same_calls_on_either_way(what):
+    bf = dict(dtype=torch.bfloat16)
+    a = dict(q=torch.zeros(3, 4, 128, **bf), kv=_cpu_cache(), lengths=torch.zeros(3, dtype=torch.int32),
+             out=torch.zeros(3, 4, 128, **bf), n_sink=-1, workspace=torch.zeros(1 << 21, dtype=torch.uint8))
+    for k, change in _DECODE_CHANGES[what].items():
+        a[k] = change(a)
+    native, general = _either_way(lambda: ck.ck_paged_decode_attn(ck.Shape(3, 4, 2, 8, 1), **a),
+                                  "host_paged_decode_attn")
+    assert native == general
+
+
+def test_the_native_way_takes_the_plain_calls():
+    """Not None: the general way would be right too, and slower."""
+    lib, bf, i32 = ck.load_library(), dict(dtype=torch.bfloat16), dict(dtype=torch.int32)
+    pytest.importorskip("paper_2412_03213_amd._ckhost")
+    sh, kv, n = ck.Shape(3, 4, 2, 8, 1), _cpu_cache(), torch.zeros(3, **i32)
+    qkv = torch.zeros(3, 8 * 128, **bf)
+    q, k, v = (x.unflatten(1, (-1, 128)) for x in qkv.split([512, 256, 256], dim=1))
+    out = torch.zeros(3, 4, 128, **bf)
+    inf = float("inf")
+    assert lib.host_rope_append(lib.rope_append_entry, sh, kv, q, k, v, out, n, torch.zeros(64), None, None,
+                                inf, 0, 0) == -1
+    assert lib.host_rope_append(lib.rope_append_entry, sh, kv, None, k, v, None, n, torch.zeros(64),
+                                torch.zeros(4, **i32), n, inf, 1, 0) == -1
+    ws = torch.zeros(1 << 21, dtype=torch.uint8)
+    assert lib.host_paged_decode_attn(lib.paged_decode_attn_entry, sh, kv, out, n, out, None, None, ws, -1, -1,
+                                      None, 0.1, 0) == -1
+    assert lib.host_paged_decode_attn(lib.paged_decode_attn_entry, sh, kv, out, n, out, torch.zeros(3, 2, 7, **i32),
+                                      torch.zeros(3, 2, **i32), ws, -1, 2, 5, 0.1, 0) == -1
