@@ -115,7 +115,7 @@ const char* ck_last_error_detail(void);
  *   CK_WS_SPARSE_ATTN:  n = upper bound of attended tokens per head-problem
  *                       (budget + n_sink + recent window), c ignored.
  *   CK_WS_PAGED_ATTN:   n and c ignored: enough for every list, window and lengths.
- *   CK_WS_PROMPT_ATTN:  n = n_rows of ck_prompt_attn, c ignored.
+ *   CK_WS_PROMPT_ATTN:  n = n_rows of ck_prompt_attn, c ignored; enough for fewer rows too.
  * Returns 0 for an invalid request.
  */
 size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c);
@@ -589,7 +589,7 @@ int ck_rope_append(const ck_shape* sh, const void* q, const void* k, const void*
  * token_idx [dev] int32 [S, Hkv, idx_stride], n_tokens [dev] int32 [S, Hkv]: recalled rows, as
  *           ck_gather_indices writes them; both NULL: no list.  Needs window >= 0.  Entries
  *           outside [0, n) are not attended; one that is a sink, in the window or listed
- *           twice counts twice.  max_tokens: upper bound of n_tokens, <= idx_stride.
+ *           twice counts twice.  max_tokens: upper bound of n_tokens, <= idx_stride, <= 2^29.
  * workspace ck_workspace_bytes(sh, CK_WS_PAGED_ATTN, 0, 0); calls that share one must be
  *           ordered (its contents on entry do not matter).
  * The split of the rows over workgroups follows the lengths, which are read on the device:
@@ -609,8 +609,8 @@ int ck_paged_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* k
  * (window counts the token itself; 0 leaves the sinks).  No row at all gives zeros.
  * q, out    [dev] [n_rows, Hq, d], CK_BF16 only; not the same buffer.
  * q_starts, lengths  see above (q_starts is needed here).
- * workspace ck_workspace_bytes(sh, CK_WS_PROMPT_ATTN, n_rows, 0); calls that share one must
- *           be ordered (its contents on entry do not matter).
+ * workspace ck_workspace_bytes(sh, CK_WS_PROMPT_ATTN, n, 0) with n >= n_rows; calls that share
+ *           one must be ordered (its contents on entry do not matter).
  * Products take bf16 operands (probabilities rounded to bf16), maximum, sum and accumulators
  * are fp32.
  */

@@ -512,12 +512,15 @@ class PagedKV:
             raise ValueError("K and V must be [n_pages, Hkv, page_size, d], of one type")
         if page_table.dim() != 2 or page_table.dtype != torch.int32:
             raise ValueError("page_table must be int32 [n_seqs, pages_per_seq]")
+        if not K.device == V.device == page_table.device:
+            raise ValueError("K, V and page_table must be on one device")
         self.K, self.V, self.page_table = K, V, page_table
         self.dtype, self.Hkv, self.page_size = K.dtype, K.shape[1], K.shape[2]
         self._c = _CkPagedKV(_ptr(K), _ptr(V), _ptr(page_table), K.shape[0], K.shape[2],
                              page_table.shape[0], page_table.shape[1])
         self._d = K.shape[3]
         self._address = ctypes.addressof(self._c)
+        self._device = K.get_device()
 
     def c(self, sh: Shape) -> _CkPagedKV:
         if self.Hkv != sh.Hkv or self._d != sh.d or self.dtype != sh.torch_dtype:
@@ -525,23 +528,45 @@ class PagedKV:
         return self._c
 
 
-def _kv(sh: Shape, kv):
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _device(t):
+    """Index of the device of a call's first tensor (-1: host), which has to be the current one: the
+    default streams of all devices have one and the same handle.  None for an address."""
+    if not isinstance(t, torch.Tensor):
+        return None
+    dev = t.get_device()
+    if dev >= 0 and dev != _current_device():
+        raise ValueError(f"tensors on cuda:{dev}, which is not the current device")
+    return dev
+
+
+def _kv(sh: Shape, kv, dev):
     if isinstance(kv, PagedKV):
+        if dev is not None and kv._device != dev:
+            raise ValueError("the cache is on another device")
         return ctypes.byref(kv.c(sh))
     return ctypes.byref(kv) if kv is not None else None      # a structure of raw addresses
 
 
-# The next three check what the kernels take for granted; they are on the path of every generated token.
-def _ints(t, name, shape):
+# These check what the kernels take for granted; they are on the path of every generated token.
+def _same_device(t, name, dev):
+    if dev is not None and t.get_device() != dev:
+        raise ValueError(f"{name} is on another device")
+    return t.data_ptr()
+
+
+def _ints(t, name, shape, dev):
     """Address of an int32 tensor of this shape, of an address, or None."""
     if t is None or isinstance(t, int):
         return t
     if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be int32 {list(shape)}, contiguous")
-    return t.data_ptr()
+    return _same_device(t, name, dev)
 
 
-def _rows(t, name, n, heads: int, sh: Shape):
+def _rows(t, name, n, heads: int, sh: Shape, dev):
     """Address and row stride of n token rows [heads, d] that may lie apart."""
     if t is None or isinstance(t, int):
         return t, heads * sh.d
@@ -549,19 +574,23 @@ def _rows(t, name, n, heads: int, sh: Shape):
     if (t.dtype is not sh.torch_dtype or t.shape != (n, heads, sh.d) or st[2] != 1
             or (st[1] != sh.d and heads > 1)):
         raise ValueError(f"{name} must be token rows [{n}, {heads}, {sh.d}] of the shape's type")
-    return t.data_ptr(), st[0] if n > 1 else heads * sh.d
+    return _same_device(t, name, dev), st[0] if n > 1 else heads * sh.d
 
 
-def _dense(t, name, n, sh: Shape):
+def _dense(t, name, n, sh: Shape, dev):
     if t is None or isinstance(t, int):
         return t
     if t.dtype is not sh.torch_dtype or t.shape != (n, sh.Hq, sh.d) or not t.is_contiguous():
         raise ValueError(f"{name} must be [{n}, {sh.Hq}, {sh.d}] of the shape's type, contiguous")
-    return t.data_ptr()
+    return _same_device(t, name, dev)
 
 
-def _bytes(workspace) -> int:
-    return workspace.numel() * workspace.element_size() if isinstance(workspace, torch.Tensor) else 0
+def _scratch(workspace, dev):
+    """Address and bytes of a workspace."""
+    if not isinstance(workspace, torch.Tensor):
+        return _ptr(workspace), 0
+    _ptr(workspace)
+    return _same_device(workspace, "workspace", dev), workspace.numel() * workspace.element_size()
 
 
 def ck_rope_frequencies(kind: int, rot_dim: int, base: float = 10000.0, factor: float = 1.0,
@@ -582,7 +611,7 @@ def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None,
     float32 [rot_dim / 2]; q and q_out may both be None.  interleaved: adjacent channels turn."""
     lib = load_library()
     flags = CK_ROPE_ADJACENT if interleaved else CK_ROPE_HALVES
-    stream = _stream(k)
+    dev, stream = _device(k), _stream(k)
     rc = lib.host_rope_append(lib.rope_append_entry, sh, kv, q, k, v, q_out, lengths, freqs,
                               q_starts, positions, attn_factor, flags, stream)
     if rc is not None:
@@ -590,19 +619,21 @@ def ck_rope_append(sh: Shape, q, k, v, kv, lengths, freqs, q_out, q_starts=None,
             _check(rc)
         return
     n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
-    qp, qs = _rows(q, "q", n, sh.Hq, sh)
-    kp, ks = _rows(k, "k", n, sh.Hkv, sh)
-    vp, vs = _rows(v, "v", n, sh.Hkv, sh)
+    qp, qs = _rows(q, "q", n, sh.Hq, sh, dev)
+    kp, ks = _rows(k, "k", n, sh.Hkv, sh, dev)
+    vp, vs = _rows(v, "v", n, sh.Hkv, sh, dev)
     rot = sh.d
     if isinstance(freqs, torch.Tensor):
         if freqs.dtype is not torch.float32 or freqs.dim() != 1:
             raise ValueError("freqs must be float32 [rot_dim / 2]")
+        _same_device(freqs, "freqs", dev)
         rot = 2 * freqs.shape[0]
     _check(lib.ck_rope_append(ctypes.byref(sh.c()), qp, kp, vp, qs, ks, vs, n,
-                              _ints(q_starts, "q_starts", (sh.S + 1,)),
-                              _ints(lengths, "lengths", (sh.S,)), _ints(positions, "positions", (n,)),
+                              _ints(q_starts, "q_starts", (sh.S + 1,), dev),
+                              _ints(lengths, "lengths", (sh.S,), dev),
+                              _ints(positions, "positions", (n,), dev),
                               _ptr(freqs), rot, attn_factor, flags,
-                              _dense(q_out, "q_out", n, sh), _kv(sh, kv), stream))
+                              _dense(q_out, "q_out", n, sh, dev), _kv(sh, kv, dev), stream))
 
 
 def paged_decode_workspace(sh: Shape, device) -> torch.Tensor:
@@ -625,7 +656,7 @@ def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window
         softmax_scale = sh.d ** -0.5
     if workspace is None:
         workspace = paged_decode_workspace(sh, q.device)
-    stream = _stream(q)
+    dev, stream = _device(q), _stream(q)
     rc = lib.host_paged_decode_attn(lib.paged_decode_attn_entry, sh, kv, q, lengths, out, token_idx,
                                     n_tokens, workspace, n_sink, window, max_tokens, softmax_scale,
                                     stream)
@@ -636,12 +667,14 @@ def ck_paged_decode_attn(sh: Shape, q, kv, lengths, out, n_sink: int = 0, window
     stride = token_idx.shape[-1] if isinstance(token_idx, torch.Tensor) else 0
     if max_tokens is None:
         max_tokens = stride
-    _check(lib.ck_paged_decode_attn(ctypes.byref(sh.c()), _dense(q, "q", sh.S, sh), _kv(sh, kv),
-                                    _ints(lengths, "lengths", (sh.S,)), n_sink, window,
-                                    _ints(token_idx, "token_idx", (sh.S, sh.Hkv, stride)),
-                                    _ints(n_tokens, "n_tokens", (sh.S, sh.Hkv)), stride, max_tokens,
-                                    softmax_scale, _dense(out, "out", sh.S, sh), _ptr(workspace),
-                                    _bytes(workspace), stream))
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(lib.ck_paged_decode_attn(ctypes.byref(sh.c()), _dense(q, "q", sh.S, sh, dev),
+                                    _kv(sh, kv, dev), _ints(lengths, "lengths", (sh.S,), dev),
+                                    n_sink, window,
+                                    _ints(token_idx, "token_idx", (sh.S, sh.Hkv, stride), dev),
+                                    _ints(n_tokens, "n_tokens", (sh.S, sh.Hkv), dev), stride,
+                                    max_tokens, softmax_scale, _dense(out, "out", sh.S, sh, dev),
+                                    ws, ws_bytes, stream))
     return workspace
 
 
@@ -653,23 +686,26 @@ def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, wi
     n = q.shape[0] if isinstance(q, torch.Tensor) else 1
     if workspace is None:
         workspace = prompt_workspace(sh, n, q.device)
-    _check(lib.ck_prompt_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh), n,
-                              _ints(q_starts, "q_starts", (sh.S + 1,)), _kv(sh, kv),
-                              _ints(lengths, "lengths", (sh.S,)), n_sink, window, softmax_scale,
-                              _dense(out, "out", n, sh), _ptr(workspace), _bytes(workspace),
+    dev = _device(q)
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(lib.ck_prompt_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh, dev), n,
+                              _ints(q_starts, "q_starts", (sh.S + 1,), dev), _kv(sh, kv, dev),
+                              _ints(lengths, "lengths", (sh.S,), dev), n_sink, window,
+                              softmax_scale, _dense(out, "out", n, sh, dev), ws, ws_bytes,
                               _stream(q)))
     return workspace
 
 
 def ck_copy_rows(sh: Shape, src, dst, n_copy, max_rows: int, row_idx=None, begin=None, src_seq=None):
     lib = load_library()
+    dev = _device(n_copy)
     stride = row_idx.shape[-1] if isinstance(row_idx, torch.Tensor) else max_rows
     per_seq = (sh.S,)
-    _check(lib.ck_copy_rows(ctypes.byref(sh.c()), _kv(sh, src), _kv(sh, dst),
-                            _ints(n_copy, "n_copy", per_seq), max_rows,
-                            _ints(row_idx, "row_idx", (sh.S, sh.Hkv, stride)), stride,
-                            _ints(begin, "begin", per_seq), _ints(src_seq, "src_seq", per_seq),
-                            _stream(n_copy)))
+    _check(lib.ck_copy_rows(ctypes.byref(sh.c()), _kv(sh, src, dev), _kv(sh, dst, dev),
+                            _ints(n_copy, "n_copy", per_seq, dev), max_rows,
+                            _ints(row_idx, "row_idx", (sh.S, sh.Hkv, stride), dev), stride,
+                            _ints(begin, "begin", per_seq, dev),
+                            _ints(src_seq, "src_seq", per_seq, dev), _stream(n_copy)))
 
 
 def _probe_operands(t):

@@ -117,7 +117,7 @@ size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c) {
   if (which == CK_WS_PAGED_ATTN) return ck::paged_workspace_bytes(dm);
   if (which == CK_WS_PROMPT_ATTN) {
     if (n < 1 || n > ck::MAX_NEW_ROWS) return 0;
-    return ck::prompt_workspace_bytes(dm, n);
+    return ck::prompt_workspace_limit(dm);
   }
   return 0;
 }
@@ -935,7 +935,7 @@ int ck_paged_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* k
     if (window < 0) return fail(CK_EINVALID, "a list needs a window: without one every row is attended already");
     if (max_tokens < 0 || idx_stride < max_tokens)
       return fail(CK_EINVALID, "max_tokens=%d outside [0, idx_stride=%d]", max_tokens, idx_stride);
-    if (max_tokens > 1 << 30) return fail(CK_EUNSUPPORTED, "attended set too large");
+    if (max_tokens > 1 << 29) return fail(CK_EUNSUPPORTED, "attended set too large");
   }
   if (!(softmax_scale > 0.f)) return fail(CK_EINVALID, "softmax_scale must be positive");
   CK_REQUIRE_PTR(q);

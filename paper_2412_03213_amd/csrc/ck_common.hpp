@@ -395,7 +395,8 @@ hipError_t launch_paged_attn(const Dims& dm, const void* q, const ck_paged_kv& k
                              int64_t n_sink, int64_t window, const int32_t* token_idx, const int32_t* n_tokens,
                              int idx_stride, int max_tokens, float softmax_scale, void* out, void* workspace,
                              hipStream_t st);
-size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows);
+size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows);   // of a call
+size_t prompt_workspace_limit(const Dims& dm);                   // of any call
 hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
                               const ck_paged_kv& kv, const int32_t* lengths, int64_t n_sink, int64_t window,
                               float softmax_scale, void* out, void* workspace, hipStream_t st);

@@ -19,7 +19,8 @@ namespace {
 
 using Entry = decltype(&ck_decode_step);
 
-PyObject *s_is_contiguous, *s_data_ptr, *s_dtype, *s_size, *s_stride, *s_hkv, *s_d, *s_address;
+PyObject *s_is_contiguous, *s_data_ptr, *s_dtype, *s_size, *s_stride, *s_hkv, *s_d, *s_address, *s_device,
+    *s_get_device;
 PyObject* s_shape[7];
 PyObject* types[4];                                     // torch's bfloat16 and float32 (CK_BF16, CK_F32), int32, uint8
 enum { INT32 = 2, UINT8 = 3 };
@@ -123,17 +124,35 @@ bool has_shape(PyObject* t, int n, const int64_t* shape) {
     if (v[i] != shape[i]) return false;
   return true;
 }
+// index of its device; -1 for the host
+bool as_device(PyObject* t, int64_t* device) {
+  PyObject* a = PyObject_CallMethodNoArgs(t, s_get_device);
+  const bool ok = as_int(a, device);
+  Py_XDECREF(a);
+  return ok;
+}
+// what the tensors of a call have in common
+struct Common {
+  int64_t entry, device;
+  ck_shape sh;
+  const ck_paged_kv* kv;
+  PyObject* type;
+  bool here(PyObject* t) const {
+    int64_t d;
+    return as_device(t, &d) && d == device;
+  }
+};
 // contiguous, of a type and shape; None is a null pointer where it may be
-bool as_dense(PyObject* t, PyObject* type, int n, const int64_t* shape, void** p, bool may_be_none = false) {
+bool as_dense(const Common& c, PyObject* t, PyObject* type, int n, const int64_t* shape, void** p, bool may_be_none = false) {
   if (t == Py_None) {
     *p = nullptr;
     return may_be_none;
   }
-  return !PyLong_Check(t) && has_type(t, type) && has_shape(t, n, shape) && as_pointer(t, p);
+  return !PyLong_Check(t) && has_type(t, type) && has_shape(t, n, shape) && c.here(t) && as_pointer(t, p);
 }
 // token rows [n, heads, d] that may lie apart
-bool as_rows(PyObject* t, PyObject* type, const int64_t (&shape)[3], void** p, int64_t* row_stride) {
-  if (t == Py_None || PyLong_Check(t) || !has_type(t, type) || !has_shape(t, 3, shape)) return false;
+bool as_rows(const Common& c, PyObject* t, const int64_t (&shape)[3], void** p, int64_t* row_stride) {
+  if (t == Py_None || PyLong_Check(t) || !has_type(t, c.type) || !has_shape(t, 3, shape) || !c.here(t)) return false;
   int64_t st[3];
   if (!as_tuple(PyObject_CallMethodNoArgs(t, s_stride), 3, st)) return false;
   if (st[2] != 1 || (st[1] != shape[2] && shape[1] > 1)) return false;
@@ -145,31 +164,27 @@ bool as_rows(PyObject* t, PyObject* type, const int64_t (&shape)[3], void** p, i
   *p = reinterpret_cast<void*>(static_cast<uintptr_t>(v));
   return ok;
 }
-// a cache in pages: its structure's address, if its heads and type are the shape's
-bool as_paged(PyObject* kv, const ck_shape& sh, const ck_paged_kv** p) {
-  int64_t v[2], address;
-  PyObject* const names[2] = {s_hkv, s_d};
-  PyObject* a = PyObject_GetAttr(kv, s_address);
-  bool ok = as_int(a, &address);
-  Py_XDECREF(a);
-  for (int i = 0; ok && i < 2; ++i) {
-    a = PyObject_GetAttr(kv, names[i]);
-    ok = as_int(a, &v[i]);
+// Arguments entry, shape and cache, and a tensor that says which device; the cache has to fit them.
+bool as_call(PyObject* const* args, PyObject* tensor, Common* c) {
+  if (!types[0] || !as_int(args[0], &c->entry) || c->entry == 0 || !as_shape(args[1], &c->sh)) return false;
+  if (c->sh.dtype != CK_BF16 && c->sh.dtype != CK_F32) return false;
+  c->type = types[c->sh.dtype];
+  if (tensor == Py_None || PyLong_Check(tensor) || !as_device(tensor, &c->device)) return false;
+  PyObject* const names[4] = {s_address, s_hkv, s_d, s_device};
+  int64_t v[4];
+  for (int i = 0; i < 4; ++i) {
+    PyObject* a = PyObject_GetAttr(args[2], names[i]);
+    const bool ok = as_int(a, &v[i]);
     Py_XDECREF(a);
+    if (!ok) return false;
   }
-  *p = reinterpret_cast<const ck_paged_kv*>(static_cast<uintptr_t>(ok ? address : 0));
-  return ok && *p && v[0] == sh.Hkv && v[1] == sh.d && has_type(kv, types[sh.dtype]);
+  c->kv = reinterpret_cast<const ck_paged_kv*>(static_cast<uintptr_t>(v[0]));
+  return c->kv && v[1] == c->sh.Hkv && v[2] == c->sh.d && v[3] == c->device && has_type(args[2], c->type);
 }
 bool as_float(PyObject* o, double* v) {
   if (!PyFloat_Check(o)) return false;
   *v = PyFloat_AS_DOUBLE(o);
   return true;
-}
-bool as_call(PyObject* const* args, int64_t* entry, ck_shape* sh, const ck_paged_kv** kv, PyObject** type) {
-  if (!types[0] || !as_int(args[0], entry) || *entry == 0 || !as_shape(args[1], sh)) return false;
-  if (sh->dtype != CK_BF16 && sh->dtype != CK_F32) return false;
-  *type = types[sh->dtype];
-  return as_paged(args[2], *sh, kv);
 }
 PyObject* not_plain() {
   PyErr_Clear();
@@ -195,34 +210,31 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     PyErr_SetString(PyExc_TypeError, "rope_append: wrong number of arguments");
     return nullptr;
   }
-  int64_t entry, stream, flags, n = 0, s_q = 0, s_k, s_v, n_freqs = 0;
-  ck_shape sh;
-  const ck_paged_kv* kv;
-  PyObject* type;
+  Common c;
+  int64_t stream, flags, size[3], n_freqs, s_q, s_k, s_v;
   void *q = nullptr, *k, *v, *q_out, *lengths, *freqs, *starts, *positions;
   double factor;
-  if (!as_call(a, &entry, &sh, &kv, &type)) return not_plain();
-  int64_t size[3];
-  if (!as_tuple(PyObject_GetAttr(a[4], s_size), 3, size)) return not_plain();
-  n = size[0];
-  const int64_t rows_q[3] = {n, sh.Hq, sh.d}, rows_k[3] = {n, sh.Hkv, sh.d}, per_seq[1] = {sh.S};
-  const int64_t n_starts[1] = {(int64_t)sh.S + 1}, per_row[1] = {n};
-  if (!as_tuple(PyObject_GetAttr(a[8], s_size), 1, &n_freqs)) return not_plain();
-  const int64_t rates[1] = {n_freqs};
+  if (!as_call(a, a[4], &c) || !as_tuple(PyObject_GetAttr(a[4], s_size), 3, size) ||
+      !as_tuple(PyObject_GetAttr(a[8], s_size), 1, &n_freqs) || n_freqs > INT32_MAX / 2)
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t n = size[0], rows_q[3] = {n, sh.Hq, sh.d}, rows_k[3] = {n, sh.Hkv, sh.d}, per_seq[1] = {sh.S};
+  const int64_t n_starts[1] = {(int64_t)sh.S + 1}, per_row[1] = {n}, rates[1] = {n_freqs};
   const bool queries = a[3] != Py_None;
   s_q = (int64_t)sh.Hq * sh.d;
-  const bool ok = (!queries || as_rows(a[3], type, rows_q, &q, &s_q)) && as_rows(a[4], type, rows_k, &k, &s_k) &&
-                  as_rows(a[5], type, rows_k, &v, &s_v) && as_dense(a[6], type, 3, rows_q, &q_out, !queries) &&
-                  as_dense(a[7], types[INT32], 1, per_seq, &lengths) && as_dense(a[8], types[CK_F32], 1, rates, &freqs) &&
-                  as_dense(a[9], types[INT32], 1, n_starts, &starts, true) &&
-                  as_dense(a[10], types[INT32], 1, per_row, &positions, true) && as_float(a[11], &factor) &&
-                  as_int(a[12], &flags) && as_int(a[13], &stream) && n_freqs <= INT32_MAX / 2;
+  const bool ok = (!queries || as_rows(c, a[3], rows_q, &q, &s_q)) && as_rows(c, a[4], rows_k, &k, &s_k) &&
+                  as_rows(c, a[5], rows_k, &v, &s_v) && as_dense(c, a[6], c.type, 3, rows_q, &q_out, !queries) &&
+                  as_dense(c, a[7], types[INT32], 1, per_seq, &lengths) &&
+                  as_dense(c, a[8], types[CK_F32], 1, rates, &freqs) &&
+                  as_dense(c, a[9], types[INT32], 1, n_starts, &starts, true) &&
+                  as_dense(c, a[10], types[INT32], 1, per_row, &positions, true) && as_float(a[11], &factor) &&
+                  as_int(a[12], &flags) && as_int(a[13], &stream);
   if (!ok) return not_plain();
-  const auto fn = reinterpret_cast<decltype(&ck_rope_append)>(static_cast<uintptr_t>(entry));
+  const auto fn = reinterpret_cast<decltype(&ck_rope_append)>(static_cast<uintptr_t>(c.entry));
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = fn(&sh, q, k, v, s_q, s_k, s_v, n, (const int32_t*)starts, (const int32_t*)lengths, (const int32_t*)positions,
-          (const float*)freqs, (int32_t)(2 * n_freqs), (float)factor, (uint32_t)flags, q_out, kv,
+          (const float*)freqs, (int32_t)(2 * n_freqs), (float)factor, (uint32_t)flags, q_out, c.kv,
           reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
   Py_END_ALLOW_THREADS
   return PyLong_FromLong(rc);
@@ -235,33 +247,29 @@ PyObject* paged_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     PyErr_SetString(PyExc_TypeError, "paged_decode_attn: wrong number of arguments");
     return nullptr;
   }
-  int64_t entry, stream, sink, window, width = 0, ws_bytes;
+  Common c;
+  int64_t stream, sink, window, size[3] = {0, 0, 0}, ws_bytes;
   int32_t most;
-  ck_shape sh;
-  const ck_paged_kv* kv;
-  PyObject* type;
   void *q, *lengths, *out, *list, *counts, *ws;
   double scale;
-  if (!as_call(a, &entry, &sh, &kv, &type)) return not_plain();
-  if (a[6] != Py_None) {
-    int64_t size[3];
-    if (!as_tuple(PyObject_GetAttr(a[6], s_size), 3, size)) return not_plain();
-    width = size[2];
-  }
-  const int64_t rows[3] = {sh.S, sh.Hq, sh.d}, per_seq[1] = {sh.S}, heads[2] = {sh.S, sh.Hkv};
+  if (!as_call(a, a[3], &c) || (a[6] != Py_None && !as_tuple(PyObject_GetAttr(a[6], s_size), 3, size)) ||
+      !as_tuple(PyObject_GetAttr(a[8], s_size), 1, &ws_bytes))
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t width = size[2], rows[3] = {sh.S, sh.Hq, sh.d}, per_seq[1] = {sh.S}, heads[2] = {sh.S, sh.Hkv};
   const int64_t lists[3] = {sh.S, sh.Hkv, width};
-  bool ok = as_dense(a[3], type, 3, rows, &q) && as_dense(a[4], types[INT32], 1, per_seq, &lengths) &&
-            as_dense(a[5], type, 3, rows, &out) && as_dense(a[6], types[INT32], 3, lists, &list, true) &&
-            as_dense(a[7], types[INT32], 2, heads, &counts, true) && as_int(a[9], &sink) && as_int(a[10], &window) &&
-            as_float(a[12], &scale) && as_int(a[13], &stream) && width <= INT32_MAX;
-  if (ok) ok = as_tuple(PyObject_GetAttr(a[8], s_size), 1, &ws_bytes) && as_dense(a[8], types[UINT8], 1, &ws_bytes, &ws);
   most = (int32_t)width;
-  if (ok && a[11] != Py_None) ok = as_i32(a[11], &most);
+  const bool ok = as_dense(c, a[3], c.type, 3, rows, &q) && as_dense(c, a[4], types[INT32], 1, per_seq, &lengths) &&
+                  as_dense(c, a[5], c.type, 3, rows, &out) && as_dense(c, a[6], types[INT32], 3, lists, &list, true) &&
+                  as_dense(c, a[7], types[INT32], 2, heads, &counts, true) &&
+                  as_dense(c, a[8], types[UINT8], 1, &ws_bytes, &ws) && as_int(a[9], &sink) &&
+                  as_int(a[10], &window) && (a[11] == Py_None || as_i32(a[11], &most)) && as_float(a[12], &scale) &&
+                  as_int(a[13], &stream) && width <= INT32_MAX;
   if (!ok) return not_plain();
-  const auto fn = reinterpret_cast<decltype(&ck_paged_decode_attn)>(static_cast<uintptr_t>(entry));
+  const auto fn = reinterpret_cast<decltype(&ck_paged_decode_attn)>(static_cast<uintptr_t>(c.entry));
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = fn(&sh, q, kv, (const int32_t*)lengths, sink, window, (const int32_t*)list, (const int32_t*)counts,
+  rc = fn(&sh, q, c.kv, (const int32_t*)lengths, sink, window, (const int32_t*)list, (const int32_t*)counts,
           (int32_t)width, most, (float)scale, out, ws, (size_t)ws_bytes,
           reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
   Py_END_ALLOW_THREADS
@@ -286,7 +294,8 @@ PyMODINIT_FUNC PyInit__ckhost(void) {
     if (!(s_shape[i] = PyUnicode_InternFromString(names[i]))) return nullptr;
   const struct { PyObject** to; const char* name; } more[] = {
       {&s_is_contiguous, "is_contiguous"}, {&s_data_ptr, "data_ptr"}, {&s_dtype, "dtype"}, {&s_size, "shape"},
-      {&s_stride, "stride"}, {&s_hkv, "Hkv"}, {&s_d, "_d"}, {&s_address, "_address"}};
+      {&s_stride, "stride"}, {&s_hkv, "Hkv"}, {&s_d, "_d"}, {&s_address, "_address"},
+      {&s_device, "_device"}, {&s_get_device, "get_device"}};
   for (const auto& m : more)
     if (!(*m.to = PyUnicode_InternFromString(m.name))) return nullptr;
   return PyModule_Create(&module);

@@ -71,16 +71,17 @@ struct Piece {
       total += mine;
     }
     total = wave_sum_l(total) * a.Hkv;
-    const int64_t even = (total + PA_PIECES - 1) / PA_PIECES;
-    length = (int)((even + PA_MIN_PIECE - 1) / PA_MIN_PIECE * PA_MIN_PIECE);
-    length = __builtin_amdgcn_readfirstlane(length < PA_MIN_PIECE ? PA_MIN_PIECE : length);
+    const int64_t even = ((total + PA_PIECES - 1) / PA_PIECES + PA_MIN_PIECE - 1) / PA_MIN_PIECE * PA_MIN_PIECE;
+    // a sequence has less than 2^31 - PA_MIN_PIECE rows (2^30 of the table, 2^29 listed): one piece then
+    const int most = 0x7FFFFFFF / PA_MIN_PIECE * PA_MIN_PIECE;
+    length = __builtin_amdgcn_readfirstlane(even < PA_MIN_PIECE ? PA_MIN_PIECE : (even < most ? (int)even : most));
     int before = 0;
     for (int s0 = 0; s0 < a.S; s0 += WAVE) {
       if (a.S > WAVE) {
         len = a.lengths[min(s0 + lane, a.S - 1)];
         mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
       }
-      int n = (mine + length - 1) / length;
+      int n = (int)(((uint32_t)mine + (uint32_t)length - 1) / (uint32_t)length);
       n = s0 + lane < a.S ? (n < 1 ? 1 : n) : 0;
       const int upto = wave_inclusive_scan(n);
       const int group = before + __builtin_amdgcn_readlane(upto, WAVE - 1);

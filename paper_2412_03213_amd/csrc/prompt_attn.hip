@@ -630,6 +630,11 @@ size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows) {
   return (size_t)prompt_blocks(dm, n_rows) * dm.Hkv * n_split * Partial::FLOATS * sizeof(float);
 }
 
+// Groups times pieces are at most PR_CUS, and least groups are those of one row.
+size_t prompt_workspace_limit(const Dims& dm) {
+  return prompt_split(dm, 1) == 1 ? 256 : (size_t)PR_CUS * Partial::FLOATS * sizeof(float);
+}
+
 hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
                               const ck_paged_kv& kv, const int32_t* lengths, int64_t n_sink, int64_t window,
                               float softmax_scale, void* out, void* workspace, hipStream_t st) {

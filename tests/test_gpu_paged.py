@@ -337,6 +337,51 @@ def test_prompt_keys_that_are_not_finite_in_masked_rows():
     close(out[sees_none, 0], want, tol, "queries that do not see them")
 
 
+@pytest.mark.parametrize("page,window", [(16, -1), (16, 2900), (12, -1), (12, 2900)])
+@pytest.mark.parametrize("n,m", [(3000, 3), (1000, 40)])
+def test_prompt_few_queries_and_values_that_are_not_finite(n, m, page, window):
+    """Pieces of one block, most of whose wavefronts have no query but bring rows: infinite values that every query
+    sees, that the last one sees, that none sees, and a page that is gone."""
+    c = Cache([n], 1, page, BF, 11, DEV)
+    last = n - 1                                        # only the last token sees it
+    for r, j, x in ((n // 2, 3, math.inf), (last, 9, -math.inf), (n - m - 1, 5, math.inf), (0, 7, math.nan)):
+        v = c.rows_v[0][0, r].clone()
+        v[j] = x
+        c.write(0, 0, r, v=v)
+    hole = (n // 2 + 3 * page) // page                  # its rows: NaN in the pool, -1 in the table
+    for r in range(hole * page, (hole + 1) * page):
+        c.write(0, 0, r, k=torch.full((D,), math.nan), v=torch.full((D,), math.nan))
+    c.table[0, hole] = -1
+    G = 4
+    q = (torch.randn(m, G, D, generator=torch.Generator().manual_seed(1)) * 0.2).to(BF)
+    out = torch.empty(m, G, D, dtype=BF, device=DEV)
+    ck.ck_prompt_attn(shape(1, 1, G), q.to(DEV), i32([0, m]), c.kv(), i32([n]), out, window=window)
+    seen = np.stack([seen_rows(n, n - m + i, 0, window) for i in range(m)]) & c.there(0)[None]
+    clean = [torch.nan_to_num(x[0][0], nan=0.0, posinf=0.0, neginf=0.0) for x in (c.rows_k, c.rows_v)]
+    want, tol = attend(q.reshape(m * G, D), clean[0], clean[1], seen.repeat(G, 0), BF, p_step=2.0 ** -8)
+    got = out.double().cpu().reshape(m * G, D).numpy()
+    ok = np.ones((m, D), dtype=bool)
+    for r, j in ((n // 2, 3), (last, 9), (n - m - 1, 5), (0, 7)):
+        ok[seen[:, r], j] = False
+    ok = ok.repeat(G, 0)
+    assert np.isfinite(got[ok]).all() and (np.abs(got - want) <= tol)[ok].all()
+    for r, j, x in ((n // 2, 3, math.inf), (last, 9, -math.inf), (n - m - 1, 5, math.inf)):
+        assert (got[seen[:, r].repeat(G), j] == x).all()
+    assert np.isnan(got[seen[:, 0].repeat(G), 7]).all()
+
+
+def test_prompt_workspace_serves_fewer_rows():
+    c = Cache([600], 1, 16, BF, 2, DEV)
+    sh, kv = shape(1, 1, 2), c.kv()
+    ws = ck.prompt_workspace(sh, 100000, DEV)
+    for m in (1, 17, 600):
+        q = torch.randn(m, 2, D, device=DEV).to(BF)
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        ck.ck_prompt_attn(sh, q, i32([0, m]), kv, i32([600]), a, workspace=ws)
+        ck.ck_prompt_attn(sh, q, i32([0, m]), kv, i32([600]), b)
+        assert torch.equal(a, b)
+
+
 def test_prompt_scores_far_apart_and_growing():
     """Maxima that grow from tile to tile, and one row that outweighs all."""
     n = 400
@@ -610,6 +655,43 @@ def test_copy_within_one_pool():
 
 
 # ---------------------------------------------------------------- together
+def test_tensors_on_another_device_are_refused(monkeypatch):
+    """Host memory among device tensors, and a device that is not the current one, whose default stream has the
+    same handle as the current one's."""
+    c = Cache([20, 30], 2, 16, BF, 1, DEV)
+    sh, kv, n = shape(2, 2, 4), c.kv(), i32([20, 30])
+    x = torch.zeros(2, 8, D, dtype=BF, device=DEV)
+    k, f, out = torch.zeros(2, 2, D, dtype=BF, device=DEV), torch.ones(64, device=DEV), torch.empty_like(x)
+    host = ck.PagedKV(c.K, c.V, c.table)
+    calls = [lambda **o: ck.ck_rope_append(sh, **{**dict(q=x, k=k, v=k, kv=kv, lengths=n, freqs=f, q_out=out), **o}),
+             lambda **o: ck.ck_paged_decode_attn(sh, **{**dict(q=x, kv=kv, lengths=n, out=out), **o}),
+             lambda **o: ck.ck_prompt_attn(sh, **{**dict(q=x, q_starts=i32([0, 1, 2]), kv=kv, lengths=n, out=out), **o})]
+    for call in calls:
+        for change in (dict(lengths=n.cpu()), dict(kv=host)):
+            with pytest.raises(ValueError):
+                call(**change)
+    for change in (dict(freqs=f.cpu()), dict(v=k.cpu()), dict(q=x.cpu()), dict(q_out=out.cpu()),
+                   dict(positions=n.cpu())):
+        with pytest.raises(ValueError):
+            calls[0](**change)
+    for change in (dict(out=out.cpu()), dict(workspace=torch.zeros(1 << 21, dtype=torch.uint8))):
+        for call in calls[1:]:
+            with pytest.raises(ValueError):
+                call(**change)
+    with pytest.raises(ValueError):
+        ck.ck_copy_rows(sh, kv, host, n, 4)
+    with pytest.raises(ValueError):
+        ck.ck_copy_rows(sh, kv, kv, n, 4, begin=n.cpu())
+    with pytest.raises(ValueError):
+        ck.PagedKV(c.K.to(DEV), c.V.to(DEV), c.table)
+    monkeypatch.setattr(ck.binding, "_current_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(ValueError):
+        ck.ck_copy_rows(sh, kv, kv, n, 4)
+
+
 def test_a_sequence_from_prompt_to_recalled_decode():
     """Prompts are turned and stored, attend, are moved to the contiguous form that clustering reads, and generated
     tokens recall their clusters from the pages: each step against the plain forms on what the steps before left."""

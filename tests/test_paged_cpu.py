@@ -174,6 +174,8 @@ def test_workspaces():
         assert ck.ck_workspace_bytes(sh, binding.CK_WS_PAGED_ATTN, 0) >= need
         assert ck.ck_workspace_bytes(sh, binding.CK_WS_PROMPT_ATTN, 100) > 0
         assert ck.ck_workspace_bytes(sh, binding.CK_WS_PROMPT_ATTN, 0) == 0
+        sizes = [ck.ck_workspace_bytes(sh, binding.CK_WS_PROMPT_ATTN, n) for n in (1, 17, 1000, 100000)]
+        assert sizes == sorted(sizes)                     # enough for fewer rows too
 
 
 def plain_rates(rot, base=10000.0):
