@@ -407,7 +407,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   // Vector instructions are laid between the products by hand; operands are read two groups of four products ahead
   // (LDS answers later than one group takes).  At the begin of tile t all wavefronts ask for the keys of t + 3 and the
   // values of t + 2, whose buffers were read for tile t - 1; what was asked for before that has to be there at its end.
-  // Tiles behind the last one are asked for and scored too (rows that the pool has, all masked): no conditions.
+  // Tiles behind the last one are asked for too (rows that the pool has): no conditions.
   if (n_tiles > 0) {
     look_up(0);
 #pragma unroll
@@ -499,6 +499,30 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       raise(mx);
       arrived(t);
     };
+    auto use_last = [&](int t, Scores& sc) {            // without a next tile; gone: of t + 2, t + 1, t
+      group_barrier();
+      const float mc = m * a.scale_log2e;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const Group v = read_values(b0, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = 4 * s + i;
+          bf16x2 two;
+          float e[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            e[u] = __builtin_amdgcn_exp2f(fmaf(sc[j >> 3][2 * (j & 7) + u], a.scale_log2e, -mc));
+            two[u] = (bf16)e[u];
+          }
+          l += e[0] + e[1];
+          pb[s][i] = __builtin_bit_cast(uint32_t, two);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) weigh(v, s, c);
+      }
+      add_odd_values(t, gone[2]);
+    };
     if (wave * 32 < qb.n_tok * G) {
       Scores sa, sb;
 #pragma unroll
@@ -512,16 +536,24 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
       raise(mx);
-      for (int t = 0; t < n_tiles; t += 2) {
+      int t = 0;
+      for (; t + 2 < n_tiles; t += 2) {
         use_tile(t, sa, sb);
         use_tile(t + 1, sb, sa);
       }
+      if (t + 1 < n_tiles) {
+        use_tile(t, sa, sb);
+        use_last(t + 1, sb);
+      } else {
+        use_last(t, sa);
+      }
     } else {                                            // no query: this wavefront brings its rows, nothing more
-      for (int t = 0; t < n_tiles + (n_tiles & 1); ++t) {
+      for (int t = 0; t + 1 < n_tiles; ++t) {
         group_barrier();
         request(t + 3, b2, b0);
         arrived(t);
       }
+      group_barrier();
     }
     wait_for_tiles<0>();                                // nothing is on its way to LDS behind the end
   }
