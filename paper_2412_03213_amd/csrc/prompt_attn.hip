@@ -129,15 +129,13 @@ struct Partial {
   }
 };
 
-// channels 32 c + 8 j + 4 half + (0..3) of a query
-__device__ __forceinline__ void store_four(bf16* out, int c, int j, int half, const float (&x)[4]) {
+__device__ __forceinline__ uint2 four_bf16(float x0, float x1, float x2, float x3) {
   bf16x2 lo, hi;
-  lo[0] = (bf16)x[0];
-  lo[1] = (bf16)x[1];
-  hi[0] = (bf16)x[2];
-  hi[1] = (bf16)x[3];
-  *reinterpret_cast<uint2*>(out + 32 * c + 8 * j + 4 * half) =
-      make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+  lo[0] = (bf16)x0;
+  lo[1] = (bf16)x1;
+  hi[0] = (bf16)x2;
+  hi[1] = (bf16)x3;
+  return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
 // one of the two bf16 of a word is infinite or not a number
@@ -559,8 +557,8 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   }
 
   l = xor32(l, OpSum());
-  if (!mine.there) return;
   if (SPLIT && n_pieces > 1) {
+    if (!mine.there) return;
     const Partial to(a.part, ((int64_t)block * a.Hkv + h) * n_split + piece);
     *to.stats(tid) = make_float2(m, l);
 #pragma unroll
@@ -569,14 +567,29 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
                                      acc[i >> 2][4 * (i & 3) + 3]);
     return;
   }
+  // ---- output: 64 channels at a time go through LDS, so that whole lines are written ----
+  // The wavefront's part of two key buffers: nobody reads keys any more, and its own loads have arrived.  Piece p of
+  // 16 bytes of row r stands at piece p ^ (r % 8) of its 128.
   const float inv = l > 0.f ? 1.0f / l : 0.f;
+  auto staged = [&](int r, int p) { return k_tiles[r >> 4] + wave * 8 * 256 + (r & 15) * 128 + ((p ^ (r & 7)) << 4); };
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+  for (int pass = 0; pass < 2; ++pass) {
+    wave_lds_order();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float x[4] = {acc[c][4 * j] * inv, acc[c][4 * j + 1] * inv, acc[c][4 * j + 2] * inv, acc[c][4 * j + 3] * inv};
-      store_four(a.out + mine.at, c, j, half, x);
+    for (int cj = 0; cj < 8; ++cj) {                    // channels 32 c + 8 j + 4 half + (0..3)
+      const int c = 2 * pass + (cj >> 2), j = cj & 3;
+      *reinterpret_cast<uint2*>(staged(col, cj) + 8 * half) =
+          four_bf16(acc[c][4 * j] * inv, acc[c][4 * j + 1] * inv, acc[c][4 * j + 2] * inv, acc[c][4 * j + 3] * inv);
     }
+    wave_lds_order();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * i + (lane >> 3);
+      const QueryRow to = QueryRow::of<G>(a, qb, h, wave * 32 + row);
+      const uint4 x = *reinterpret_cast<const uint4*>(staged(row, lane & 7));
+      if (to.there) store_once(a.out + to.at + pass * 64 + (lane & 7) * 8, x);
+    }
+  }
 }
 
 // The pieces of a block joined, in their order: blockIdx.y has four of the 64 accumulators of every lane.
@@ -618,9 +631,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs 
     }
   }
   const float inv = l > 0.f ? 1.0f / l : 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] *= inv;
-  store_four(a.out + mine.at, i >> 2, i & 3, lane >> 5, x);
+  // channels 8 i + 4 (lane / 32) + (0..3)
+  *reinterpret_cast<uint2*>(a.out + mine.at + 8 * i + 4 * (lane >> 5)) =
+      four_bf16(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
 }
 
 template <bool EIGHTS, bool SPLIT>
