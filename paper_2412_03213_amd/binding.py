@@ -185,6 +185,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.host_rope_append = _host("rope_append")
     lib.rope_append_entry = ctypes.cast(lib.ck_rope_append, P).value
     lib.host_paged_decode_attn = _host("paged_decode_attn")
+    lib.host_copy_rows = _host("copy_rows")
+    lib.copy_rows_entry = ctypes.cast(lib.ck_copy_rows, P).value
     lib.paged_decode_attn_entry = ctypes.cast(lib.ck_paged_decode_attn, P).value
     _lib = lib
     return lib
@@ -698,14 +700,20 @@ def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, wi
 
 def ck_copy_rows(sh: Shape, src, dst, n_copy, max_rows: int, row_idx=None, begin=None, src_seq=None):
     lib = load_library()
-    dev = _device(n_copy)
+    dev, stream = _device(n_copy), _stream(n_copy)
+    rc = lib.host_copy_rows(lib.copy_rows_entry, sh, src, dst, n_copy, max_rows, row_idx, begin,
+                            src_seq, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return
     stride = row_idx.shape[-1] if isinstance(row_idx, torch.Tensor) else max_rows
     per_seq = (sh.S,)
     _check(lib.ck_copy_rows(ctypes.byref(sh.c()), _kv(sh, src, dev), _kv(sh, dst, dev),
                             _ints(n_copy, "n_copy", per_seq, dev), max_rows,
                             _ints(row_idx, "row_idx", (sh.S, sh.Hkv, stride), dev), stride,
                             _ints(begin, "begin", per_seq, dev),
-                            _ints(src_seq, "src_seq", per_seq, dev), _stream(n_copy)))
+                            _ints(src_seq, "src_seq", per_seq, dev), stream))
 
 
 def _probe_operands(t):

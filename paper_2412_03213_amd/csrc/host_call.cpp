@@ -1,5 +1,5 @@
 // The calls that are made once per layer and generated token, for the Python binding without ctypes
-// in between: ck_decode_step, ck_rope_append and ck_paged_decode_attn.
+// in between: ck_decode_step, ck_rope_append, ck_paged_decode_attn and ck_copy_rows.
 //
 // ck_decode_step is made once per layer and generated token, and at small batches its marshalling (fifteen tensors, two method
 // calls and two ctypes conversions each) took longer than the kernel: 9.9 us from call to call
@@ -8,7 +8,7 @@
 // decode_step(entry, shape, 15 tensors, 9 numbers) takes what ck_decode_step takes, `entry` being
 // its address.  It returns the status code, or None if any argument is not of the plain
 // kind (a contiguous tensor, a number): nothing has been called then, and the caller goes the
-// general way, which accepts or refuses the arguments in its own words.  The other two do the same;
+// general way, which accepts or refuses the arguments in its own words.  The others do the same;
 // they also look at the tensors' types, shapes and strides, as the general way does.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -164,22 +164,26 @@ bool as_rows(const Common& c, PyObject* t, const int64_t (&shape)[3], void** p, 
   *p = reinterpret_cast<void*>(static_cast<uintptr_t>(v));
   return ok;
 }
-// Arguments entry, shape and cache, and a tensor that says which device; the cache has to fit them.
+// a cache in pages whose heads, type and device are the call's
+bool as_paged(const Common& c, PyObject* kv, const ck_paged_kv** p) {
+  PyObject* const names[4] = {s_address, s_hkv, s_d, s_device};
+  int64_t v[4];
+  for (int i = 0; i < 4; ++i) {
+    PyObject* a = PyObject_GetAttr(kv, names[i]);
+    const bool ok = as_int(a, &v[i]);
+    Py_XDECREF(a);
+    if (!ok) return false;
+  }
+  *p = reinterpret_cast<const ck_paged_kv*>(static_cast<uintptr_t>(v[0]));
+  return *p && v[1] == c.sh.Hkv && v[2] == c.sh.d && v[3] == c.device && has_type(kv, c.type);
+}
+// Arguments entry, shape and cache, and a tensor that says which device.
 bool as_call(PyObject* const* args, PyObject* tensor, Common* c) {
   if (!types[0] || !as_int(args[0], &c->entry) || c->entry == 0 || !as_shape(args[1], &c->sh)) return false;
   if (c->sh.dtype != CK_BF16 && c->sh.dtype != CK_F32) return false;
   c->type = types[c->sh.dtype];
   if (tensor == Py_None || PyLong_Check(tensor) || !as_device(tensor, &c->device)) return false;
-  PyObject* const names[4] = {s_address, s_hkv, s_d, s_device};
-  int64_t v[4];
-  for (int i = 0; i < 4; ++i) {
-    PyObject* a = PyObject_GetAttr(args[2], names[i]);
-    const bool ok = as_int(a, &v[i]);
-    Py_XDECREF(a);
-    if (!ok) return false;
-  }
-  c->kv = reinterpret_cast<const ck_paged_kv*>(static_cast<uintptr_t>(v[0]));
-  return c->kv && v[1] == c->sh.Hkv && v[2] == c->sh.d && v[3] == c->device && has_type(args[2], c->type);
+  return as_paged(*c, args[2], &c->kv);
 }
 bool as_float(PyObject* o, double* v) {
   if (!PyFloat_Check(o)) return false;
@@ -276,11 +280,43 @@ PyObject* paged_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return PyLong_FromLong(rc);
 }
 
+// copy_rows(entry, shape, source, destination, n_copy, max_rows, row_idx, begin, src_seq, stream)
+PyObject* copy_rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 10) {
+    PyErr_SetString(PyExc_TypeError, "copy_rows: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  const ck_paged_kv* dst;
+  int64_t stream, size[3] = {0, 0, 0};
+  int32_t most;
+  void *counts, *list, *begin, *src_seq;
+  if (!as_call(a, a[4], &c) || !as_paged(c, a[3], &dst) || !as_i32(a[5], &most) ||
+      (a[6] != Py_None && !as_tuple(PyObject_GetAttr(a[6], s_size), 3, size)))
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t per_seq[1] = {sh.S}, lists[3] = {sh.S, sh.Hkv, size[2]};
+  const bool ok = as_dense(c, a[4], types[INT32], 1, per_seq, &counts) &&
+                  as_dense(c, a[6], types[INT32], 3, lists, &list, true) &&
+                  as_dense(c, a[7], types[INT32], 1, per_seq, &begin, true) &&
+                  as_dense(c, a[8], types[INT32], 1, per_seq, &src_seq, true) && as_int(a[9], &stream) &&
+                  size[2] <= INT32_MAX;
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_copy_rows)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, c.kv, dst, (const int32_t*)counts, most, (const int32_t*)list, list ? (int32_t)size[2] : most,
+          (const int32_t*)begin, (const int32_t*)src_seq, reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 #define CK_METHOD(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
     {"decode_step", CK_METHOD(decode_step), "ck_decode_step on plain tensors; None if an argument is of another kind"},
     {"rope_append", CK_METHOD(rope_append), "ck_rope_append, likewise"},
     {"paged_decode_attn", CK_METHOD(paged_decode_attn), "ck_paged_decode_attn, likewise"},
+    {"copy_rows", CK_METHOD(copy_rows), "ck_copy_rows, likewise"},
     {"set_types", CK_METHOD(set_types), "torch's bfloat16, float32, int32 and uint8"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ckhost", nullptr, -1, methods,

@@ -304,6 +304,28 @@ def test_paged_decode_refuses_the_same_calls_on_either_way(what):
     assert native == general
 
 
+_COPY_CHANGES = {
+    "refused by the library": {}, "wide counts": {"n_copy": lambda a: a["n_copy"].long()},
+    "no counts": {"n_copy": lambda a: None}, "most": {"max_rows": lambda a: 2.5},
+    "many": {"max_rows": lambda a: (1 << 32) + 1}, "short list": {"max_rows": lambda a: 8, "row_idx": lambda a: a["row_idx"][..., :4]},
+    "narrow list": {"max_rows": lambda a: 8, "row_idx": lambda a: a["row_idx"][..., :4].contiguous()},
+    "flat list": {"row_idx": lambda a: a["row_idx"].flatten()}, "begin": {"begin": lambda a: a["begin"][:2]},
+    "source": {"src_seq": lambda a: a["begin"].float()}, "no source": {"src": lambda a: None},
+    "other heads": {"dst": lambda a: _cpu_cache(Hkv=1)}, "other type": {"src": lambda a: _cpu_cache(dtype=torch.float32)},
+}
+
+
+@pytest.mark.parametrize("what", _COPY_CHANGES)
+def test_copy_rows_refuses_the_same_calls_on_either_way(what):
+    i32 = dict(dtype=torch.int32)
+    a = dict(src=_cpu_cache(), dst=_cpu_cache(), n_copy=torch.zeros(3, **i32), max_rows=0,
+             row_idx=torch.zeros(3, 2, 16, **i32), begin=torch.zeros(3, **i32))     # no row at most
+    for k, change in _COPY_CHANGES[what].items():
+        a[k] = change(a)
+    native, general = _either_way(lambda: ck.ck_copy_rows(ck.Shape(3, 4, 2, 8, 1), **a), "host_copy_rows")
+    assert native == general
+
+
 def test_the_native_way_takes_the_plain_calls():
     """Not None: the general way would be right too, and slower."""
     lib, bf, i32 = ck.load_library(), dict(dtype=torch.bfloat16), dict(dtype=torch.int32)
@@ -322,3 +344,5 @@ def test_the_native_way_takes_the_plain_calls():
                                       None, 0.1, 0) == -1
     assert lib.host_paged_decode_attn(lib.paged_decode_attn_entry, sh, kv, out, n, out, torch.zeros(3, 2, 7, **i32),
                                       torch.zeros(3, 2, **i32), ws, -1, 2, 5, 0.1, 0) == -1
+    assert lib.host_copy_rows(lib.copy_rows_entry, sh, kv, _cpu_cache(), n, 0, torch.zeros(3, 2, 7, **i32), n, n, 0) == -1
+    assert lib.host_copy_rows(lib.copy_rows_entry, sh, kv, kv, n, 0, None, None, None, 0) == -1
