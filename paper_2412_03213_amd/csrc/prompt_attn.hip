@@ -92,6 +92,10 @@ struct QueryBlock {
     }
     return false;
   }
+  // of the tiles, how many are among the first `cache_tiles` of the cache
+  __device__ __forceinline__ int index(int cache_tiles) const {
+    return max(min(cache_tiles, sink_tiles), cache_tiles - gap);
+  }
   __device__ __forceinline__ int first_row(int tile) const { return (tile < sink_tiles ? tile : tile + gap) * PR_TILE; }
   // Few blocks: their tiles are cut into pieces for n_split workgroups, short ones into fewer.
   __device__ __forceinline__ int piece_tiles(int n_split) const {
@@ -209,6 +213,12 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   const int from_whole = max(window_in, qb.sink_tiles) - tile0;
   const Tiles all_whole(from_whole, max(0, qb.p0 + 1) / PR_TILE - qb.gap - tile0);
   const Tiles whole(from_whole, max(0, p_lo + 1) / PR_TILE - qb.gap - tile0);
+
+  // Tiles that some query of the wavefront sees something of: in [my_first, my_end).
+  const int n_mine = min(32, qb.n_tok * G - wave * 32);
+  const int my_cache_end = n_mine > 0 ? max(0, qb.p0 + (wave * 32 + n_mine - 1) / G + PR_TILE) / PR_TILE : 0;
+  const int my_end = min(n_tiles, qb.index(my_cache_end) - tile0);
+  const int my_first = a.window < 0 || qb.sink_tiles > 0 ? 0 : max(0, max(0, p_lo - a.window + 1) / PR_TILE - qb.gap - tile0);
 
   floatx16 acc[4];
 #pragma unroll
@@ -521,38 +531,43 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       }
       add_odd_values(t, gone[2]);
     };
-    if (wave * 32 < qb.n_tok * G) {
-      Scores sa, sb;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const Group k = read_keys(0, g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) score(k, g, i, sa);
-      }
-      seen = mask(0, gone[2], sa);
-      float mx = PR_NEG_BIG;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
-      raise(mx);
-      int t = 0;
-      for (; t + 2 < n_tiles; t += 2) {
-        use_tile(t, sa, sb);
-        use_tile(t + 1, sb, sa);
-      }
-      if (t + 1 < n_tiles) {
-        use_tile(t, sa, sb);
-        use_last(t + 1, sb);
-      } else {
-        use_last(t, sa);
-      }
-    } else {                                            // no query: this wavefront brings its rows, nothing more
-      for (int t = 0; t + 1 < n_tiles; ++t) {
+    // Tiles that none of the wavefront's queries sees: it brings its rows of them, nothing more.
+    auto pass_by = [&](int from, int end) {
+      for (int t = from; t < end; ++t) {
         group_barrier();
         request(t + 3, b2, b0);
         arrived(t);
       }
-      group_barrier();
+    };
+    pass_by(0, min(my_first, n_tiles));
+    if (my_first < my_end) {
+      Scores sa, sb;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const Group k = read_keys(b0, g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) score(k, g, i, sa);
+      }
+      seen = mask(my_first, gone[2], sa);
+      float mx = PR_NEG_BIG;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
+      raise(mx);
+      const bool last = my_end == n_tiles;              // otherwise a next one is scored, of which nothing is seen
+      const int end = last ? n_tiles - 1 : my_end;
+      int t = my_first;
+      for (; t + 1 < end; t += 2) {
+        use_tile(t, sa, sb);
+        use_tile(t + 1, sb, sa);
+      }
+      if (t < end) {
+        use_tile(t, sa, sb);
+        if (last) use_last(t + 1, sb);
+      } else if (last) {
+        use_last(t, sa);
+      }
     }
+    pass_by(max(my_first, my_end), n_tiles);
     wait_for_tiles<0>();                                // nothing is on its way to LDS behind the end
   }
 
