@@ -1,5 +1,5 @@
 """Binding of libclusterkv.so: argument marshalling only, through ctypes and, for the calls
-that are made once per layer and generated token, through the native _ckhost module where it
+that are made once per layer and step, through the native _ckhost module where it
 has been built for this interpreter.
 
 Functions carry the names of the C entry points (include/clusterkv.h) and take
@@ -185,6 +185,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.host_rope_append = _host("rope_append")
     lib.rope_append_entry = ctypes.cast(lib.ck_rope_append, P).value
     lib.host_paged_decode_attn = _host("paged_decode_attn")
+    lib.host_prompt_attn = _host("prompt_attn")
+    lib.prompt_attn_entry = ctypes.cast(lib.ck_prompt_attn, P).value
     lib.host_copy_rows = _host("copy_rows")
     lib.copy_rows_entry = ctypes.cast(lib.ck_copy_rows, P).value
     lib.paged_decode_attn_entry = ctypes.cast(lib.ck_paged_decode_attn, P).value
@@ -688,13 +690,19 @@ def ck_prompt_attn(sh: Shape, q, q_starts, kv, lengths, out, n_sink: int = 0, wi
     n = q.shape[0] if isinstance(q, torch.Tensor) else 1
     if workspace is None:
         workspace = prompt_workspace(sh, n, q.device)
-    dev = _device(q)
+    dev, stream = _device(q), _stream(q)
+    rc = lib.host_prompt_attn(lib.prompt_attn_entry, sh, kv, q, q_starts, lengths, out, workspace,
+                              n_sink, window, softmax_scale, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return workspace
     ws, ws_bytes = _scratch(workspace, dev)
     _check(lib.ck_prompt_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh, dev), n,
                               _ints(q_starts, "q_starts", (sh.S + 1,), dev), _kv(sh, kv, dev),
                               _ints(lengths, "lengths", (sh.S,), dev), n_sink, window,
                               softmax_scale, _dense(out, "out", n, sh, dev), ws, ws_bytes,
-                              _stream(q)))
+                              stream))
     return workspace
 
 

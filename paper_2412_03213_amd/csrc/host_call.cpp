@@ -1,5 +1,5 @@
-// The calls that are made once per layer and generated token, for the Python binding without ctypes
-// in between: ck_decode_step, ck_rope_append, ck_paged_decode_attn and ck_copy_rows.
+// The calls that are made once per layer and step, for the Python binding without ctypes in between:
+// ck_decode_step and the four on caches in pages.
 //
 // ck_decode_step is made once per layer and generated token, and at small batches its marshalling (fifteen tensors, two method
 // calls and two ctypes conversions each) took longer than the kernel: 9.9 us from call to call
@@ -280,6 +280,35 @@ PyObject* paged_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return PyLong_FromLong(rc);
 }
 
+// prompt_attn(entry, shape, cache, q, q_starts, lengths, out, workspace, n_sink, window, scale, stream)
+PyObject* prompt_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 12) {
+    PyErr_SetString(PyExc_TypeError, "prompt_attn: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  int64_t stream, sink, window, size[3], ws_bytes;
+  void *q, *starts, *lengths, *out, *ws;
+  double scale;
+  if (!as_call(a, a[3], &c) || !as_tuple(PyObject_GetAttr(a[3], s_size), 3, size) ||
+      !as_tuple(PyObject_GetAttr(a[7], s_size), 1, &ws_bytes))
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t rows[3] = {size[0], sh.Hq, sh.d}, n_starts[1] = {(int64_t)sh.S + 1}, per_seq[1] = {sh.S};
+  const bool ok = as_dense(c, a[3], c.type, 3, rows, &q) && as_dense(c, a[4], types[INT32], 1, n_starts, &starts) &&
+                  as_dense(c, a[5], types[INT32], 1, per_seq, &lengths) && as_dense(c, a[6], c.type, 3, rows, &out) &&
+                  as_dense(c, a[7], types[UINT8], 1, &ws_bytes, &ws) && as_int(a[8], &sink) && as_int(a[9], &window) &&
+                  as_float(a[10], &scale) && as_int(a[11], &stream);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_prompt_attn)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, q, size[0], (const int32_t*)starts, c.kv, (const int32_t*)lengths, sink, window, (float)scale, out, ws,
+          (size_t)ws_bytes, reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 // copy_rows(entry, shape, source, destination, n_copy, max_rows, row_idx, begin, src_seq, stream)
 PyObject* copy_rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   if (n_args != 10) {
@@ -316,6 +345,7 @@ PyMethodDef methods[] = {
     {"decode_step", CK_METHOD(decode_step), "ck_decode_step on plain tensors; None if an argument is of another kind"},
     {"rope_append", CK_METHOD(rope_append), "ck_rope_append, likewise"},
     {"paged_decode_attn", CK_METHOD(paged_decode_attn), "ck_paged_decode_attn, likewise"},
+    {"prompt_attn", CK_METHOD(prompt_attn), "ck_prompt_attn, likewise"},
     {"copy_rows", CK_METHOD(copy_rows), "ck_copy_rows, likewise"},
     {"set_types", CK_METHOD(set_types), "torch's bfloat16, float32, int32 and uint8"},
     {nullptr, nullptr, 0, nullptr}};

@@ -304,6 +304,29 @@ def test_paged_decode_refuses_the_same_calls_on_either_way(what):
     assert native == general
 
 
+_PROMPT_CHANGES = {
+    "refused by the library": {}, "strided": {"q": lambda a: a["q"].transpose(0, 1)}, "address": {"q": lambda a: 4096},
+    "other type": {"out": lambda a: a["out"].float()}, "one output row short": {"out": lambda a: a["out"][:4]},
+    "starts": {"q_starts": lambda a: a["lengths"]}, "no starts": {"q_starts": lambda a: None},
+    "wide lengths": {"lengths": lambda a: a["lengths"].long()}, "no cache": {"kv": lambda a: None},
+    "small workspace": {"workspace": lambda a: a["workspace"][:8], "n_sink": lambda a: 0},
+    "whole scale": {"softmax_scale": lambda a: 1}, "sinks": {"n_sink": lambda a: 1.0},
+    "no rows": {"q": lambda a: a["q"][:0], "out": lambda a: a["out"][:0]},
+}
+
+
+@pytest.mark.parametrize("what", _PROMPT_CHANGES)
+def test_prompt_attn_refuses_the_same_calls_on_either_way(what):
+    bf, i32 = dict(dtype=torch.bfloat16), dict(dtype=torch.int32)
+    a = dict(q=torch.zeros(5, 4, 128, **bf), q_starts=torch.zeros(4, **i32), kv=_cpu_cache(),
+             lengths=torch.zeros(3, **i32), out=torch.zeros(5, 4, 128, **bf), n_sink=-1,
+             workspace=torch.zeros(1 << 26, dtype=torch.uint8))
+    for k, change in _PROMPT_CHANGES[what].items():
+        a[k] = change(a)
+    native, general = _either_way(lambda: ck.ck_prompt_attn(ck.Shape(3, 4, 2, 8, 1), **a), "host_prompt_attn")
+    assert native == general
+
+
 _COPY_CHANGES = {
     "refused by the library": {}, "wide counts": {"n_copy": lambda a: a["n_copy"].long()},
     "no counts": {"n_copy": lambda a: None}, "most": {"max_rows": lambda a: 2.5},
@@ -346,3 +369,4 @@ def test_the_native_way_takes_the_plain_calls():
                                       torch.zeros(3, 2, **i32), ws, -1, 2, 5, 0.1, 0) == -1
     assert lib.host_copy_rows(lib.copy_rows_entry, sh, kv, _cpu_cache(), n, 0, torch.zeros(3, 2, 7, **i32), n, n, 0) == -1
     assert lib.host_copy_rows(lib.copy_rows_entry, sh, kv, kv, n, 0, None, None, None, 0) == -1
+    assert lib.host_prompt_attn(lib.prompt_attn_entry, sh, kv, out, torch.zeros(4, **i32), n, out, ws, -1, -1, 0.1, 0) == -1
