@@ -25,6 +25,8 @@ constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
 constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;   // two steps of each wavefront
 constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
+constexpr int PA_SLACK = 64; 
+constexpr int PA_FAN = 16;                              // pieces that are joined in one stage
 constexpr int PA_PART = D + 2;                          // floats of a (piece, query head): max, sum, acc[128]
 constexpr unsigned long long PA_TICKET = 0x434B5061676Eull;   // marks a ticket word as ours
 
@@ -32,7 +34,7 @@ struct PagedArgs {
   const void *q, *K, *V;
   void* out;
   float* part;                                          // [pieces, G, PA_PART]
-  unsigned long long* tickets;                          // [HP]
+  unsigned long long* tickets;                          // [HP], then one for each piece
   const int32_t *lengths, *token_idx, *n_tokens;
   Pages pages;
   int S, Hq, Hkv, n_sink, window, idx_stride, max_tokens;   // window < 0: every row
@@ -81,7 +83,8 @@ struct Piece {
         len = a.lengths[min(s0 + lane, a.S - 1)];
         mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
       }
-      int n = (int)(((uint32_t)mine + (uint32_t)length - 1) / (uint32_t)length);
+      // a piece more costs a join, so it is taken only for more than PA_SLACK rows
+      int n = (int)(((uint32_t)max(mine - PA_SLACK, 0) + (uint32_t)length - 1) / (uint32_t)length);
       n = s0 + lane < a.S ? (n < 1 ? 1 : n) : 0;
       const int upto = wave_inclusive_scan(n);
       const int group = before + __builtin_amdgcn_readlane(upto, WAVE - 1);
@@ -303,6 +306,73 @@ struct StateF32 {
   }
 };
 
+// Whether this workgroup is the last of `expected` that have written what others will read.  The stores before it are
+// performed where every XCD looks; each thread waits for its own before the barrier, only then is the ticket drawn.  A
+// ticket word that does not carry the mark (memory that held something else) is taken over by a compare-and-swap;
+// whoever added to it before that adds itself again.
+__device__ __forceinline__ bool last_to_arrive(unsigned long long* ticket, int expected, int* s_last) {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const unsigned long long old = __hip_atomic_fetch_add(ticket, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    unsigned long long now = old + 1;
+    if ((old >> 16) != PA_TICKET) {
+      unsigned long long seen = now;
+      do {
+        now = (seen >> 16) == PA_TICKET ? seen + 1 : ((PA_TICKET << 16) | 1ull);
+      } while (!__hip_atomic_compare_exchange_strong(ticket, &seen, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                                     __HIP_MEMORY_SCOPE_AGENT));
+    }
+    const int last = (int)(now & 0xFFFFull) == expected;
+    if (last) __hip_atomic_store(ticket, PA_TICKET << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *s_last = last;
+  }
+  __syncthreads();
+  const bool last = *s_last != 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+  return last;
+}
+
+// Pieces put together: channel pair e % 64 of head e / 64.
+struct Joined { float m, l, x, y; };
+template <int G>
+__device__ __forceinline__ Joined join_pieces(const float* part, int64_t stride, int n, int e) {
+  const float* base = part + (e / (D / 2)) * PA_PART;
+  const int c2 = (e % (D / 2)) * 2;
+  Joined r = {PA_NEG_BIG, 0.f, 0.f, 0.f};
+  constexpr int BATCH = 16;                             // pieces whose loads are under way together
+  for (int i0 = 0; i0 < n; i0 += BATCH) {
+    float2 ml[BATCH], av[BATCH];
+    float mx = r.m;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      ml[i] = make_float2(PA_NEG_BIG, 0.f);
+      av[i] = make_float2(0.f, 0.f);
+      if (i0 + i < n) {
+        const float* p = base + (int64_t)(i0 + i) * stride;
+        ml[i] = get_pair(p);
+        av[i] = get_pair(p + 2 + c2);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) mx = fmaxf(mx, ml[i].x);
+    const float corr = __builtin_amdgcn_exp2f(r.m - mx);
+    r.l *= corr;
+    r.x *= corr;
+    r.y *= corr;
+    r.m = mx;
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - mx);
+      r.l += ml[i].y * f;
+      r.x += av[i].x * f;
+      r.y += av[i].y * f;
+    }
+  }
+  return r;
+}
+
 template <typename T, int G, bool LIST>
 __global__ __launch_bounds__(PA_WAVES * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void k_paged_attn(const PagedArgs a) {
@@ -329,7 +399,7 @@ void k_paged_attn(const PagedArgs a) {
   const int n_total = span.rows(listed);
   const int64_t p_begin64 = (int64_t)pc.split * pc.length;
   const int p_begin = p_begin64 < n_total ? (int)p_begin64 : n_total;
-  const int n_pos = min(n_total - p_begin, pc.length);
+  const int n_pos = pc.split == pc.n_split - 1 ? n_total - p_begin : min(n_total - p_begin, pc.length);
   // a contiguous run of whole steps for every wavefront
   const int run = ((n_pos + PA_WAVES - 1) / PA_WAVES + PA_STEP - 1) / PA_STEP * PA_STEP;
   const int w_begin = p_begin + min(wave * run, n_pos), w_end = p_begin + min((wave + 1) * run, n_pos);
@@ -380,8 +450,8 @@ void k_paged_attn(const PagedArgs a) {
     for (int i = 0; i < 4; ++i) {
       const int64_t at = (int64_t)(w[i] < 0 ? 0 : w[i]) * D;
       if constexpr (BF16) {
-        r.k[i] = LIST ? *reinterpret_cast<const uint4*>(Kc + at) : load_once(Kc + at);
-        r.v[i] = LIST ? *reinterpret_cast<const uint4*>(Vc + at) : load_once(Vc + at);
+        r.k[i] = load_once(Kc + at);
+        r.v[i] = load_once(Vc + at);
       } else {
         r.k[i][0] = reinterpret_cast<const float4*>(Kc + at)[0];
         r.k[i][1] = reinterpret_cast<const float4*>(Kc + at)[1];
@@ -390,17 +460,14 @@ void k_paged_attn(const PagedArgs a) {
       }
     }
   };
-  // Register sets in rotation: the loads of the next steps (three in bf16, one in fp32) are under way while one is
-  // reduced.  They go on behind the end (tokens that are not there read row 0), so that every step is followed by as
-  // many loads and waits for its own only.
-  constexpr int NS = BF16 ? 4 : 2;
+  // Two register sets in turn: the loads of the next step are under way while one is reduced.  They go on behind the
+  // end (tokens that are not there read row 0), so that every step is followed by as many loads and waits for its own only.
   if (n_steps > 0) {                                    // wave-uniform
     put_rows(0, look_up(0));
     Found next = look_up(1);
     wave_lds_order();
-    Step sets[NS];
-#pragma unroll
-    for (int j = 0; j < NS - 1; ++j) fetch(j, sets[j]);
+    Step sets[2];
+    fetch(0, sets[0]);
     for (int group = 0;; ++group) {
       wave_lds_order();
       put_rows(group + 1, next);
@@ -409,12 +476,12 @@ void k_paged_attn(const PagedArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int t = group * 4 + j;
-        fetch(t + NS - 1, sets[(j + NS - 1) % NS]);
+        fetch(t + 1, sets[(j + 1) & 1]);
         const int4 tr = step_rows(t);
         if constexpr (BF16)
-          state.add(sets[j % NS], tr, qb, stage, a.scale_log2e);
+          state.add(sets[j & 1], tr, qb, stage, a.scale_log2e);
         else
-          state.add(sets[j % NS], tr, qv);
+          state.add(sets[j & 1], tr, qv);
         if (t + 1 >= n_steps) goto reduced;             // out of both loops: no path back without all of the loads
       }
     }
@@ -456,70 +523,46 @@ reduced:
   }
   if (pc.n_split == 1) return;
 
-  // ---- the last workgroup of the head-problem joins the pieces ----
-  // The stores above are performed where every XCD looks; each thread waits for its own before the barrier,
-  // only then is the ticket drawn.  A ticket word that does not carry the mark (memory that held something
-  // else) is taken over by a compare-and-swap; whoever added to it before that adds itself again.
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-  __builtin_amdgcn_s_waitcnt(0);
-  __syncthreads();
-  if (tid == 0) {
-    unsigned long long* tk = a.tickets + hp;
-    const unsigned long long old = __hip_atomic_fetch_add(tk, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    unsigned long long now = old + 1;
-    if ((old >> 16) != PA_TICKET) {
-      unsigned long long seen = now;
-      do {
-        now = (seen >> 16) == PA_TICKET ? seen + 1 : ((PA_TICKET << 16) | 1ull);
-      } while (!__hip_atomic_compare_exchange_strong(tk, &seen, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                     __HIP_MEMORY_SCOPE_AGENT));
+  // ---- the last workgroup of a head-problem joins the pieces, in their order; many of them in two stages ----
+  // One workgroup reads what the others left at 15 to 20 GB/s only (past L2), so more than PA_FAN pieces are joined in
+  // groups first, each by the last workgroup of the group, which leaves the result in the place of its first piece.
+  const int fan = pc.n_split <= PA_FAN ? pc.n_split : (int)ceilf(sqrtf((float)pc.n_split));
+  const int group = pc.split / fan, n_groups = (pc.n_split + fan - 1) / fan;
+  float* from = part + group * fan * stride;
+  int64_t step = stride;
+  int n = min(fan, pc.n_split - group * fan);
+  unsigned long long* ticket = a.tickets + a.S * a.Hkv + pc.first + h + group * fan * a.Hkv;   // of the first piece
+  constexpr int ITEMS = (G * (D / 2) + NT - 1) / NT;
+  Joined r[ITEMS];
+  for (bool last = n_groups == 1;; last = true) {
+    if (!last_to_arrive(ticket, n, &s_last)) return;
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) r[k] = join_pieces<G>(from, step, n, min(tid + k * NT, G * (D / 2) - 1));
+    if (last) break;
+    __syncthreads();                                    // the first piece has been read by all
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) {
+      const int e = tid + k * NT, g = e / (D / 2), c2 = (e % (D / 2)) * 2;
+      if (e >= G * (D / 2)) continue;
+      float* p = from + g * PA_PART;
+      if (c2 == 0) put_pair(p, r[k].m, r[k].l);
+      put_pair(p + 2 + c2, r[k].x, r[k].y);
     }
-    const int last = (int)(now & 0xFFFFull) == pc.n_split;
-    if (last) __hip_atomic_store(tk, PA_TICKET << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = last;
+    ticket = a.tickets + hp;
+    from = part;
+    step = stride * fan;
+    n = n_groups;
   }
-  __syncthreads();
-  if (!s_last) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-  for (int e = tid; e < G * (D / 2); e += NT) {
-    const int g = e / (D / 2), c2 = (e % (D / 2)) * 2;
-    const float* base = part + g * PA_PART;
-    float M = PA_NEG_BIG, ls = 0.f, a0 = 0.f, a1 = 0.f;
-    constexpr int BATCH = 16;                           // pieces whose loads are under way together
-    for (int i0 = 0; i0 < pc.n_split; i0 += BATCH) {
-      float2 ml[BATCH], av[BATCH];
-      float mx = M;
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        ml[i] = make_float2(PA_NEG_BIG, 0.f);
-        av[i] = make_float2(0.f, 0.f);
-        if (i0 + i < pc.n_split) {
-          const float* p = base + (int64_t)(i0 + i) * stride;
-          ml[i] = get_pair(p);
-          av[i] = get_pair(p + 2 + c2);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) mx = fmaxf(mx, ml[i].x);
-      const float corr = __builtin_amdgcn_exp2f(M - mx);
-      ls *= corr;
-      a0 *= corr;
-      a1 *= corr;
-      M = mx;
-#pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const float f = __builtin_amdgcn_exp2f(ml[i].x - mx);
-        ls += ml[i].y * f;
-        a0 += av[i].x * f;
-        a1 += av[i].y * f;
-      }
-    }
-    const float inv = ls > 0.f ? 1.0f / ls : 0.f;
-    store2(out + g * D + c2, a0 * inv, a1 * inv);
+  for (int k = 0; k < ITEMS; ++k) {
+    const int e = tid + k * NT;
+    const float inv = r[k].l > 0.f ? 1.0f / r[k].l : 0.f;
+    if (e < G * (D / 2)) store2(out + (e / (D / 2)) * D + (e % (D / 2)) * 2, r[k].x * inv, r[k].y * inv);
   }
 }
 
-size_t ticket_bytes(const Dims& dm) { return ((size_t)dm.HP * 8 + 255) & ~(size_t)255; }
+// Of the head-problems, then of the groups of pieces (by their first piece).
+size_t ticket_bytes(const Dims& dm) { return ((size_t)(2 * dm.HP + PA_PIECES) * 8 + 255) & ~(size_t)255; }
 
 template <typename T, bool LIST>
 void launch_paged_t(int G, dim3 grid, const PagedArgs& a, hipStream_t st) {

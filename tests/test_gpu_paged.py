@@ -99,6 +99,38 @@ def test_decode_long_ragged(dtype):
     run_decode([40003, 17, 9000, 0, 12345], 1, 4, 64, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("G", [1, 8])
+@pytest.mark.parametrize("lens", [[2241], [2049, 64, 191], [9001], [33000]])
+def test_decode_pieces_joined_in_stages(lens, G, dtype):
+    """17, 16, 70 and 256 pieces of one head-problem, whose last may be longer or short; some hold an infinite value,
+    and a workspace of any contents."""
+    c = Cache(lens, 1, 32, dtype, 21, DEV)
+    n = lens[0]
+    for r in (3, n - 2):
+        v = c.rows_v[0][0, r].clone()
+        v[5] = math.inf
+        c.write(0, 0, r, v=v)
+    q = (torch.randn(len(lens), G, D, generator=torch.Generator().manual_seed(4)) * 0.2).to(dtype)
+    out = torch.empty(len(lens), G, D, dtype=dtype, device=DEV)
+    sh = shape(len(lens), 1, G, dtype)
+    ws = ck.paged_decode_workspace(sh, DEV)
+    ws.random_(0, 256)
+    again = torch.empty_like(out)
+    ck.ck_paged_decode_attn(sh, q.to(DEV), c.kv(), i32(lens), out, workspace=ws)
+    ck.ck_paged_decode_attn(sh, q.to(DEV), c.kv(), i32(lens), again, workspace=ws)
+    assert torch.equal(out, again)
+    assert (out[0, :, 5] == math.inf).all()
+    out[0, :, 5] = 0.0
+    for s, m in enumerate(lens):
+        v = c.rows_v[s][0].clone()
+        v[torch.isinf(v)] = 0.0
+        if s == 0:
+            v[:, 5] = 0.0
+        want, tol = attend(q[s], c.rows_k[s][0], v, np.ones((G, m)), dtype, p_step=2.0 ** -15 if dtype is BF else 0.0)
+        close(out[s], want, tol, f"sequence {s}")
+
+
 def test_decode_many_head_problems():
     # more head-problems than pieces
     run_decode([33] * 70, 8, 1, 32, BF)
