@@ -21,7 +21,7 @@ constexpr float PR_NEG_BIG = -1.0e30f;
 constexpr int PR_WAVES = 8;
 constexpr int PR_ROWS = PR_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int PR_TILE = 64;                             // cache rows of a tile
-constexpr int PR_MIN_TILES = 4;                         // of a piece
+constexpr int PR_MIN_TILES = 2;                         // of a piece
 constexpr int PR_CUS = 256;
 constexpr int PR_BUFFERS = 3;                           // tiles of keys, and of values, in LDS
 
@@ -99,10 +99,11 @@ struct QueryBlock {
   __device__ __forceinline__ int first_row(int tile) const { return (tile < sink_tiles ? tile : tile + gap) * PR_TILE; }
   // Few blocks: their tiles are cut into pieces for n_split workgroups, short ones into fewer.
   __device__ __forceinline__ int piece_tiles(int n_split) const {
-    return n_split == 1 ? n_tiles : max(PR_MIN_TILES, (n_tiles + n_split - 1) / n_split);
+    const int n = max(1, min(n_split, n_tiles / PR_MIN_TILES));
+    return max(1, (n_tiles + n - 1) / n);
   }
   __device__ __forceinline__ int pieces(int n_split) const {
-    return n_split == 1 || n_tiles == 0 ? 1 : (n_tiles + piece_tiles(n_split) - 1) / piece_tiles(n_split);
+    return max(1, (n_tiles + piece_tiles(n_split) - 1) / piece_tiles(n_split));
   }
 };
 
@@ -675,24 +676,32 @@ void launch_join(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
 int64_t prompt_blocks(const Dims& dm, int64_t n_rows) {
   return n_rows / (PR_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S);
 }
-// Workgroups that share the tiles of a block.  One workgroup fills a compute unit; what does not fill half of the
-// chip is cut.
-int prompt_split(const Dims& dm, int64_t n_rows) {
+// Workgroups that may share the tiles of a block: one workgroup fills a compute unit.
+int prompt_most_pieces(const Dims& dm, int64_t n_rows) {
   const int64_t groups = prompt_blocks(dm, n_rows) * dm.Hkv;
   return groups >= PR_CUS ? 1 : (int)(PR_CUS / groups);
+}
+// ... and that do, for blocks that see up to `tiles` tiles: what the pieces spare, in tiles, has to be more than what
+// their join costs, a launch and 1 KB of partial results a query row, written and read.
+int prompt_split(const Dims& dm, int64_t n_rows, int64_t tiles) {
+  const int64_t most = prompt_most_pieces(dm, n_rows);
+  const int64_t pieces = most < tiles / PR_MIN_TILES ? most : tiles / PR_MIN_TILES;
+  if (pieces < 2) return 1;
+  const int64_t join = 3 + n_rows * dm.Hq * pieces / 6000;
+  return tiles - (tiles + pieces - 1) / pieces >= join ? (int)pieces : 1;
 }
 
 }  // namespace
 
 size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows) {
-  const int n_split = prompt_split(dm, n_rows);
+  const int n_split = prompt_most_pieces(dm, n_rows);
   if (n_split == 1) return 256;
   return (size_t)prompt_blocks(dm, n_rows) * dm.Hkv * n_split * Partial::FLOATS * sizeof(float);
 }
 
 // Groups times pieces are at most PR_CUS, and least groups are those of one row.
 size_t prompt_workspace_limit(const Dims& dm) {
-  return prompt_split(dm, 1) == 1 ? 256 : (size_t)PR_CUS * Partial::FLOATS * sizeof(float);
+  return prompt_most_pieces(dm, 1) == 1 ? 256 : (size_t)PR_CUS * Partial::FLOATS * sizeof(float);
 }
 
 hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
@@ -714,7 +723,9 @@ hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, con
   const int64_t rows = a.pages.rows;
   a.n_sink = (int)(n_sink < rows ? n_sink : rows);
   a.window = window < 0 || window >= rows ? -1 : (int)window;
-  a.n_split = prompt_split(dm, n_rows);
+  int64_t seen = rows;                                  // by a block, at most
+  if (a.window >= 0 && a.n_sink + a.window + PR_ROWS / dm.G < rows) seen = a.n_sink + a.window + PR_ROWS / dm.G;
+  a.n_split = prompt_split(dm, n_rows, (seen + PR_TILE - 1) / PR_TILE);
   a.scale_log2e = softmax_scale * 1.4426950408889634f;
   const unsigned blocks = (unsigned)prompt_blocks(dm, n_rows);
   const bool eights = kv.page_size % 8 == 0;
