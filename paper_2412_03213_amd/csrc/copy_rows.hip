@@ -1,6 +1,8 @@
 // Rows of K and V from one cache to another: paged or contiguous, whole or by a list per KV head.
 // Bound by memory: every row is read and written once.  A row of 256 (bf16) or 512 (fp32) bytes goes
 // through 16 or 32 lanes; a wavefront has several rows of K and of V under way.
+// 8 x 4096 listed rows of 8 heads (270 MB) take 53 us, 5.1 TB/s, what a copy reaches: 78 us with loads and stores that stay
+// in the caches, the same with 64 rows to a wavefront instead of 16.  One page of each of 24 sequences: 2.8 us in a graph.
 #include "paged.hpp"
 
 namespace ck {

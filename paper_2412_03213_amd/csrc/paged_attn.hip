@@ -8,6 +8,11 @@
 // each wavefront.  The running maximum and sum of the softmax are kept per wavefront, then joined over the
 // workgroup and, by the workgroup of a head-problem that is through last, over its pieces in their order.
 //
+// 8 KV heads, G = 4, bf16: 4 x 131072 rows 328 us (2.15 GB, 6.5 TB/s; 369 with loads that stay in the caches), 32 ragged
+// sequences of up to 8191 rows 102 us (605 MB, 5.9 TB/s), 16 x (1024 listed + 233) rows 18.7 us (83 MB).  2048 rows of one
+// sequence take 8.9 us in a graph: a launch 1.7, the piece found 0.3, rows and products 2.5, wavefronts joined 1, pieces
+// joined 3.5 (three round trips past L2).
+//
 // bf16: both products on the matrix cores, 16 tokens a step, as in the attention over recalled tokens:
 // q K^T with the K rows turned into operand layout through LDS, P V with the operands in the lanes that hold
 // them.  A probability enters the product as two bf16 numbers that hold 16 bits of it.
@@ -23,10 +28,17 @@ namespace {
 constexpr float PA_NEG_BIG = -1.0e30f;                  // "no row yet": finite so that differences stay finite
 constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
-constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;   // two steps of each wavefront
+// Pieces of a batch and their least length, two steps of each wavefront.  The times of half and twice as many pieces
+// or rows, in us: 2048 rows 10.6 with 64, 9.1 with 256 instead of 8.9; 32 ragged sequences 109 and 106 instead of 102; with
+// 1024 pieces 99, but 32000 rows of one sequence 30 instead of 26 and 64 recalled lists 59 instead of 52.
+constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;
 constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
-constexpr int PA_SLACK = 64; 
-constexpr int PA_FAN = 16;                              // pieces that are joined in one stage
+// Rows by which the last piece may be longer than the others: a piece more costs a join (64 sequences of up to 500 rows,
+// one piece each or a short second one: 16.3 us, 18.4 without; with 128 rows 14.6, but 500 rows of one sequence 8.2, not 7.1).
+constexpr int PA_SLACK = 64;
+// Pieces that are joined in one stage.  One stage for all: 8000 rows (63 pieces) 18.6 us, not 11.8; 131072 rows of one KV head
+// with G = 8 (500 pieces) 88 us, not 25.  In one stage up to 32 pieces: 4000 rows 12.0 us, not 9.7.
+constexpr int PA_FAN = 16;
 constexpr int PA_PART = D + 2;                          // floats of a (piece, query head): max, sum, acc[128]
 constexpr unsigned long long PA_TICKET = 0x434B5061676Eull;   // marks a ticket word as ours
 
@@ -462,6 +474,7 @@ void k_paged_attn(const PagedArgs a) {
   };
   // Two register sets in turn: the loads of the next step are under way while one is reduced.  They go on behind the
   // end (tokens that are not there read row 0), so that every step is followed by as many loads and waits for its own only.
+  // Four sets: 9.0 us for 2048 rows, not 8.5, 20.7 for the listed rows, not 19.0, the long caches alike.
   if (n_steps > 0) {                                    // wave-uniform
     put_rows(0, look_up(0));
     Found next = look_up(1);

@@ -11,6 +11,15 @@
 //                 the transposing reads (ds_read_b64_tr_b16) in the same order.  The accumulator has the
 //                 queries in its lanes again, so scaling it is in-lane too.
 // Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
+//
+// G = 4, 8 KV heads: 8192 tokens from the beginning take 490 to 505 us, 1.1 PFLOP/s of the products that the mask leaves
+// (a large library product reaches 1.52 to 1.58); the matrix pipe is busy for 58 % of the cycles at 2.1 GHz.  What
+// stands against more is power: the same launch on zeros takes 451 us at 2.35 GHz, on uniform random numbers 600 at
+// 1.8, and arrangements with fewer vector instructions or no barrier between the phases came out the same.  Tiles
+// straight to LDS and eight wavefronts on them instead of four with loads through registers: 532 us, not 600.
+// Chunks with a window of 1024 (G = 8): 215 us, 0.79 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
+// outputs, whose traffic nothing else overlaps.  17 tokens behind 30011 rows for each of two sequences: 47 us, 224 MB
+// at 4.8 TB/s.
 #include "paged.hpp"
 
 namespace ck {
@@ -21,9 +30,9 @@ constexpr float PR_NEG_BIG = -1.0e30f;
 constexpr int PR_WAVES = 8;
 constexpr int PR_ROWS = PR_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int PR_TILE = 64;                             // cache rows of a tile
-constexpr int PR_MIN_TILES = 2;                         // of a piece
+constexpr int PR_MIN_TILES = 2;                         // of a piece (4: 17 tokens behind 1000 rows 13.1 us, not 11.0)
 constexpr int PR_CUS = 256;
-constexpr int PR_BUFFERS = 3;                           // tiles of keys, and of values, in LDS
+constexpr int PR_BUFFERS = 3;                           // tiles of keys, and of values, in LDS: loads run two tiles ahead
 
 struct PromptArgs {
   const bf16 *q, *K, *V;
@@ -153,7 +162,7 @@ __device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
 
 // 16 bytes for every lane from base + offset to LDS at `to` + 16 * lane, on their way when this returns:
 // they are counted with the vector loads (wait_for_tiles).
-// ONCE: no other workgroup reads them.
+// ONCE: no other workgroup reads them (blocks in pieces, few to a sequence: 71 us, not 76, with this alone).
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
   if constexpr (ONCE)
@@ -185,7 +194,9 @@ struct Tiles {
   __device__ __forceinline__ bool has(int t) const { return (uint32_t)(t - lo) < n; }
 };
 
-// EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page.
+// EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page: one
+// address, and page numbers looked up for eight tiles at a time.  8192 tokens 479 us, row by row 495; chunks with a
+// window 197 and 204 (one box, pages of 64 and 32 rows).
 // SPLIT: the tiles of a block are cut into pieces (a.n_split > 1).
 template <int G, bool EIGHTS, bool SPLIT>
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
@@ -196,7 +207,8 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   static_assert(PR_WAVES == 8 && PR_TILE == 64 && PR_BUFFERS == 3, "eight rows of a tile for each wavefront");
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv, n_split = SPLIT ? a.n_split : 1, block = w / n_split, piece = w % n_split;
+  const int h = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv, n_split = SPLIT ? a.n_split : 1;
+  const int block = w / n_split, piece = w % n_split;
   QueryBlock qb;
   if (!qb.find(a, block, PR_ROWS / G)) return;
   const int tile0 = piece * qb.piece_tiles(n_split), n_pieces = qb.pieces(n_split);
@@ -215,7 +227,8 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   const Tiles all_whole(from_whole, max(0, qb.p0 + 1) / PR_TILE - qb.gap - tile0);
   const Tiles whole(from_whole, max(0, p_lo + 1) / PR_TILE - qb.gap - tile0);
 
-  // Tiles that some query of the wavefront sees something of: in [my_first, my_end).
+  // Tiles that some query of the wavefront sees something of: in [my_first, my_end).  (G = 1, a window of 8 rows:
+  // 34 us, 40 where all wavefronts take all tiles of the block; a window of 1024 83 and 87.)
   const int n_mine = min(32, qb.n_tok * G - wave * 32);
   const int my_cache_end = n_mine > 0 ? max(0, qb.p0 + (wave * 32 + n_mine - 1) / G + PR_TILE) / PR_TILE : 0;
   const int my_end = min(n_tiles, qb.index(my_cache_end) - tile0);
@@ -584,6 +597,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     return;
   }
   // ---- output: 64 channels at a time go through LDS, so that whole lines are written ----
+  // (8 bytes of a row at a time, as the accumulators hold them: 249 us for the chunks with a window, not 215.)
   // The wavefront's part of two key buffers: nobody reads keys any more, and its own loads have arrived.  Piece p of
   // 16 bytes of row r stands at piece p ^ (r % 8) of its 128.
   const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -637,7 +651,8 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs 
         f[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
       const float mx = fmaxf(m, st[k].x);
-      const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e), add = __builtin_amdgcn_exp2f((st[k].x - mx) * a.scale_log2e);
+      const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e);
+      const float add = __builtin_amdgcn_exp2f((st[k].x - mx) * a.scale_log2e);
       m = mx;
       l = l * old + st[k].y * add;
       x[0] = x[0] * old + f[k].x * add;
@@ -682,7 +697,10 @@ int prompt_most_pieces(const Dims& dm, int64_t n_rows) {
   return groups >= PR_CUS ? 1 : (int)(PR_CUS / groups);
 }
 // ... and that do, for blocks that see up to `tiles` tiles: what the pieces spare, in tiles, has to be more than what
-// their join costs, a launch and 1 KB of partial results a query row, written and read.
+// their join costs, a launch and 1 KB of partial results a query row, written and read.  Cut and not, in us, of one
+// sequence with 8 KV heads, G = 4: 17 tokens behind 250 rows 11.0 / 10.1, 500 11.0 / 14.2, 4000 14.1 / 66.9; 100 tokens
+// behind 200 rows 14.9 / 12.1, 400 14.3 / 16.6; 700 behind 1000 31.9 / 30.0, 1500 37.9 / 41.0, 3000 53.6 / 73.4; all of
+// 1000 34.5 / 28.8.  The rule takes the smaller of every pair.
 int prompt_split(const Dims& dm, int64_t n_rows, int64_t tiles) {
   const int64_t most = prompt_most_pieces(dm, n_rows);
   const int64_t pieces = most < tiles / PR_MIN_TILES ? most : tiles / PR_MIN_TILES;
