@@ -1,8 +1,9 @@
 """MI355X-native ClusterKV hot path: thin Python binding over libclusterkv.so.
 
 Every step of the path (K-means assignment/update, metadata, cluster selection,
-index gather, sparse decode attention) runs in the HIP kernels of the C-ABI
-library declared in include/clusterkv.h.  This package only marshals torch
+index gather, sparse decode attention), and of what stands beside it on caches in
+pages (rotary append, prompt and one-token attention, row copies), runs in the HIP
+kernels of the C-ABI library declared in include/clusterkv.h.  This package only marshals torch
 tensors (device memory, current stream) into those calls.  There is no CPU or
 PyTorch fallback: a missing library is an error.
 """

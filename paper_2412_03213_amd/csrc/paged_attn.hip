@@ -28,9 +28,9 @@ namespace {
 constexpr float PA_NEG_BIG = -1.0e30f;                  // "no row yet": finite so that differences stay finite
 constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
-// Pieces of a batch and their least length, two steps of each wavefront.  The times of half and twice as many pieces
-// or rows, in us: 2048 rows 10.6 with 64, 9.1 with 256 instead of 8.9; 32 ragged sequences 109 and 106 instead of 102; with
-// 1024 pieces 99, but 32000 rows of one sequence 30 instead of 26 and 64 recalled lists 59 instead of 52.
+// Pieces of a batch and their least length, two steps of each wavefront.  With 64 and 256 rows: 2048 rows of one sequence
+// 9.2 and 9.1 us, not 8.9, 32 ragged sequences 109 and 106, not 102; the listed rows alone gain from 64 (17.6, not 18.7).
+// With 1024 pieces: the ragged sequences 99, but 32000 rows of one sequence 30, not 26, and 64 recalled lists 59, not 52.
 constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;
 constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
 // Rows by which the last piece may be longer than the others: a piece more costs a join (64 sequences of up to 500 rows,
