@@ -288,6 +288,13 @@ def test_prompt_window_and_sinks(n_sink, window):
     run_prompt([5, 64, 333, 400], [5, 1, 333, 150], 2, 4, 24, n_sink, window)
 
 
+@pytest.mark.parametrize("G,page,n_sink,window", [(1, 16, 0, 5), (1, 20, 0, 130), (2, 64, 0, 64), (1, 16, 70, 3),
+                                                  (2, 9, 3, 200)])
+def test_prompt_blocks_of_many_tokens_and_short_windows(G, page, n_sink, window):
+    """Wavefronts of one workgroup see different tiles, some none of those at the begin, at the end or between."""
+    run_prompt([900, 777], [700, 333], 1, G, page, n_sink, window)
+
+
 @pytest.mark.parametrize("n_sink,window", [(0, 3), (2, 100), (0, -1), (5, 0)])
 @pytest.mark.parametrize("G", [1, 8])
 def test_prompt_masks_row_by_row(n_sink, window, G):
@@ -687,6 +694,43 @@ def test_copy_within_one_pool():
 
 
 # ---------------------------------------------------------------- together
+def test_pools_beyond_32_bit_offsets():
+    """The same rows in a small pool and on the last pages of one of 5 GB: the same bits from every operator."""
+    lens, Hkv, G, page = [200, 131], 2, 4, 64
+    c = Cache(lens, Hkv, page, BF, 5, DEV, spare=0)
+    small, sh = c.kv(), shape(2, Hkv, G)
+    n_pages = 164000
+    K = torch.empty(n_pages, Hkv, page, D, dtype=BF, device=DEV)
+    assert K.numel() * 2 > 2 ** 32
+    table = torch.where((c.table >= 0) & (c.table < c.K.shape[0]), c.table + n_pages - c.K.shape[0],
+                        torch.tensor(-1, dtype=torch.int32)).to(DEV)
+    big = ck.PagedKV(K, torch.empty_like(K), table)
+    n = i32(lens)
+    ck.ck_copy_rows(sh, small, big, n, 200)
+    at = n_pages - c.K.shape[0]
+    k = torch.randn(5, Hkv, D, device=DEV).to(BF)
+    q = torch.randn(5, Hkv * G, D, device=DEV).to(BF)
+    freqs = torch.ones(64, device=DEV) * 0.1
+    for kv in (small, big):
+        ck.ck_rope_append(sh, None, k, k, kv, n, freqs, None, q_starts=i32([0, 3, 5]))
+    for s in range(2):
+        for r in range(lens[s]):
+            p = int(c.table[s, r // page])
+            if r % 50 == 0 or r >= lens[s] - 3:
+                assert torch.equal(big.K[at + p, :, r % page], small.K[p, :, r % page])
+                assert torch.equal(big.V[at + p, :, r % page], small.V[p, :, r % page])
+    outs = [[torch.empty_like(q), torch.empty_like(q[:2])] for _ in range(2)]
+    for kv, (a, b) in zip((small, big), outs):
+        ck.ck_prompt_attn(sh, q, i32([0, 3, 5]), kv, n, a)
+        ck.ck_paged_decode_attn(sh, q[:2], kv, n, b)
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    back = ck.PagedKV(torch.zeros_like(small.K), torch.zeros_like(small.V), small.page_table)
+    ck.ck_copy_rows(sh, big, back, n, 200)
+    for s in range(2):
+        p, r = int(c.table[s, (lens[s] - 1) // page]), (lens[s] - 1) % page
+        assert torch.equal(back.V[p, :, :r + 1], small.V[p, :, :r + 1])
+
+
 def test_tensors_on_another_device_are_refused(monkeypatch):
     """Host memory among device tensors, and a device that is not the current one, whose default stream has the
     same handle as the current one's."""
