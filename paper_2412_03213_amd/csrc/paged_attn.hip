@@ -36,6 +36,9 @@ constexpr int PA_PIECES = 512;                          // workgroups of four wa
 // Rows by which the last piece may be longer than the others: a piece more costs a join (64 sequences of up to 500 rows,
 // one piece each or a short second one: 16.3 us, 18.4 without; with 128 rows 14.6, but 500 rows of one sequence 8.2, not 7.1).
 constexpr int PA_SLACK = 64;
+// Times that the pieces are made longer by an eighth.  Never: 16 ragged sequences of up to 30000 rows 216 us, not 184, of
+// 8191 rows 57, not 54, 40 of 8191 rows 138, not 127.
+constexpr int PA_TRIES = 8;
 // Pieces that are joined in one stage.  One stage for all: 8000 rows (63 pieces) 18.6 us, not 11.8; 131072 rows of one KV head
 // with G = 8 (500 pieces) 88 us, not 25.  In one stage up to 32 pieces: 4000 rows 12.0 us, not 9.7.
 constexpr int PA_FAN = 16;
@@ -89,16 +92,31 @@ struct Piece {
     // a sequence has less than 2^31 - PA_MIN_PIECE rows (2^30 of the table, 2^29 listed): one piece then
     const int most = 0x7FFFFFFF / PA_MIN_PIECE * PA_MIN_PIECE;
     length = __builtin_amdgcn_readfirstlane(even < PA_MIN_PIECE ? PA_MIN_PIECE : (even < most ? (int)even : most));
-    int before = 0;
-    for (int s0 = 0; s0 < a.S; s0 += WAVE) {
+    int n = 0, upto = 0;                                // pieces of sequence s0 + lane, and up to it from s0 on
+    auto cut = [&](int s0) {
       if (a.S > WAVE) {
         len = a.lengths[min(s0 + lane, a.S - 1)];
         mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
       }
       // a piece more costs a join, so it is taken only for more than PA_SLACK rows
-      int n = (int)(((uint32_t)max(mine - PA_SLACK, 0) + (uint32_t)length - 1) / (uint32_t)length);
+      n = (int)(((uint32_t)max(mine - PA_SLACK, 0) + (uint32_t)length - 1) / (uint32_t)length);
       n = s0 + lane < a.S ? (n < 1 ? 1 : n) : 0;
-      const int upto = wave_inclusive_scan(n);
+      upto = wave_inclusive_scan(n);
+    };
+    // Lengths that no piece divides make more pieces than fit, and the rest would run alone: longer ones then.
+    const int more = max(PA_MIN_PIECE, length / 8 / PA_MIN_PIECE * PA_MIN_PIECE);
+    for (int tries = 0;; ++tries) {
+      int all = 0;
+      for (int s0 = 0; s0 < a.S; s0 += WAVE) {
+        cut(s0);
+        all += __builtin_amdgcn_readlane(upto, WAVE - 1);
+      }
+      if (all * a.Hkv <= PA_PIECES || a.S * a.Hkv > PA_PIECES || tries == PA_TRIES || length >= most - more) break;
+      length += more;
+    }
+    int before = 0;
+    for (int s0 = 0; s0 < a.S; s0 += WAVE) {
+      if (a.S > WAVE) cut(s0);
       const int group = before + __builtin_amdgcn_readlane(upto, WAVE - 1);
       if (w < group * a.Hkv) {
         const uint64_t beyond = __ballot((before + upto) * a.Hkv > w);
