@@ -9,7 +9,7 @@
 // workgroup and, by the workgroup of a head-problem that is through last, over its pieces in their order.
 //
 // 8 KV heads, G = 4, bf16: 4 x 131072 rows 328 us (2.15 GB, 6.5 TB/s; 369 with loads that stay in the caches), 32 ragged
-// sequences of up to 8191 rows 102 us (605 MB, 5.9 TB/s), 16 x (1024 listed + 233) rows 18.7 us (83 MB).  2048 rows of one
+// sequences of up to 8191 rows 102 us (605 MB, 5.9 TB/s), 16 x (1024 listed + 233) rows 18.1 us (83 MB).  2048 rows of one
 // sequence take 8.9 us in a graph: a launch 1.7, the piece found 0.3, rows and products 2.5, wavefronts joined 1, pieces
 // joined 3.5 (three round trips past L2).
 //
@@ -28,19 +28,15 @@ namespace {
 constexpr float PA_NEG_BIG = -1.0e30f;                  // "no row yet": finite so that differences stay finite
 constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
-// Pieces of a batch and their least length, two steps of each wavefront.  With 64 and 256 rows: 2048 rows of one sequence
-// 9.2 and 9.1 us, not 8.9, 32 ragged sequences 109 and 106, not 102; the listed rows alone gain from 64 (17.6, not 18.7).
-// With 1024 pieces: the ragged sequences 99, but 32000 rows of one sequence 30, not 26, and 64 recalled lists 59, not 52.
+// Pieces of a batch and their least length, two steps of each wavefront.  Half as long: 4000 rows of one sequence 10.3 us,
+// not 9.6; twice as long: 500 rows 8.1, not 7.1.  1024 pieces: 32000 rows 30 us, not 26, the listed rows 23, not 18.
 constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;
 constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
-// Rows by which the last piece may be longer than the others: a piece more costs a join (64 sequences of up to 500 rows,
-// one piece each or a short second one: 16.3 us, 18.4 without; with 128 rows 14.6, but 500 rows of one sequence 8.2, not 7.1).
-constexpr int PA_SLACK = 64;
 // Times that the pieces are made longer by an eighth.  Never: 16 ragged sequences of up to 30000 rows 216 us, not 184, of
 // 8191 rows 57, not 54, 40 of 8191 rows 138, not 127.
 constexpr int PA_TRIES = 8;
-// Pieces that are joined in one stage.  One stage for all: 8000 rows (63 pieces) 18.6 us, not 11.8; 131072 rows of one KV head
-// with G = 8 (500 pieces) 88 us, not 25.  In one stage up to 32 pieces: 4000 rows 12.0 us, not 9.7.
+// Pieces that are joined in one stage.  One stage for all: 8000 rows (63 pieces) 17.8 us, not 11.5; 131072 rows of one KV
+// head with G = 8 (512 pieces) 90 us, not 26.  In one stage up to 32 pieces: 4000 rows 11.6 us, not 9.6.
 constexpr int PA_FAN = 16;
 constexpr int PA_PART = D + 2;                          // floats of a (piece, query head): max, sum, acc[128]
 constexpr unsigned long long PA_TICKET = 0x434B5061676Eull;   // marks a ticket word as ours
@@ -88,9 +84,10 @@ struct Piece {
       total += mine;
     }
     total = wave_sum_l(total) * a.Hkv;
-    const int64_t even = ((total + PA_PIECES - 1) / PA_PIECES + PA_MIN_PIECE - 1) / PA_MIN_PIECE * PA_MIN_PIECE;
-    // a sequence has less than 2^31 - PA_MIN_PIECE rows (2^30 of the table, 2^29 listed): one piece then
-    const int most = 0x7FFFFFFF / PA_MIN_PIECE * PA_MIN_PIECE;
+    constexpr int UNIT = PA_WAVES * PA_STEP;
+    const int64_t even = ((total + PA_PIECES - 1) / PA_PIECES + UNIT - 1) / UNIT * UNIT;
+    // a sequence has less than 2^31 - UNIT rows (2^30 of the table, 2^29 listed): one piece then
+    const int most = 0x7FFFFFFF / UNIT * UNIT;
     length = __builtin_amdgcn_readfirstlane(even < PA_MIN_PIECE ? PA_MIN_PIECE : (even < most ? (int)even : most));
     int n = 0, upto = 0;                                // pieces of sequence s0 + lane, and up to it from s0 on
     auto cut = [&](int s0) {
@@ -98,13 +95,12 @@ struct Piece {
         len = a.lengths[min(s0 + lane, a.S - 1)];
         mine = s0 + lane < a.S ? Span(a, len).rows(listed) : 0;
       }
-      // a piece more costs a join, so it is taken only for more than PA_SLACK rows
-      n = (int)(((uint32_t)max(mine - PA_SLACK, 0) + (uint32_t)length - 1) / (uint32_t)length);
+      n = (int)(((uint32_t)mine + (uint32_t)length - 1) / (uint32_t)length);
       n = s0 + lane < a.S ? (n < 1 ? 1 : n) : 0;
       upto = wave_inclusive_scan(n);
     };
     // Lengths that no piece divides make more pieces than fit, and the rest would run alone: longer ones then.
-    const int more = max(PA_MIN_PIECE, length / 8 / PA_MIN_PIECE * PA_MIN_PIECE);
+    const int more = max(UNIT, length / 8 / UNIT * UNIT);
     for (int tries = 0;; ++tries) {
       int all = 0;
       for (int s0 = 0; s0 < a.S; s0 += WAVE) {
@@ -429,7 +425,7 @@ void k_paged_attn(const PagedArgs a) {
   const int n_total = span.rows(listed);
   const int64_t p_begin64 = (int64_t)pc.split * pc.length;
   const int p_begin = p_begin64 < n_total ? (int)p_begin64 : n_total;
-  const int n_pos = pc.split == pc.n_split - 1 ? n_total - p_begin : min(n_total - p_begin, pc.length);
+  const int n_pos = min(n_total - p_begin, pc.length);
   // a contiguous run of whole steps for every wavefront
   const int run = ((n_pos + PA_WAVES - 1) / PA_WAVES + PA_STEP - 1) / PA_STEP * PA_STEP;
   const int w_begin = p_begin + min(wave * run, n_pos), w_end = p_begin + min((wave + 1) * run, n_pos);

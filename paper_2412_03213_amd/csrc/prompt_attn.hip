@@ -12,7 +12,7 @@
 //                 queries in its lanes again, so scaling it is in-lane too.
 // Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
 //
-// G = 4, 8 KV heads: 8192 tokens from the beginning take 490 to 505 us, 1.1 PFLOP/s of the products that the mask leaves
+// G = 4, 8 KV heads: 8192 tokens from the beginning take 486 to 505 us, 1.1 PFLOP/s of the products that the mask leaves
 // (a large library product reaches 1.52 to 1.58); the matrix pipe is busy for 58 % of the cycles at 2.1 GHz.  What
 // stands against more is power: the same launch on zeros takes 451 us at 2.35 GHz, on uniform random numbers 600 at
 // 1.8, and arrangements with fewer vector instructions or no barrier between the phases came out the same.  Tiles
