@@ -196,7 +196,7 @@ struct Tiles {
 
 // EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page: one
 // address, and page numbers looked up for eight tiles at a time.  8192 tokens 479 us, row by row 495; chunks with a
-// window 197 and 204 (one box, pages of 64 and 32 rows).
+// window 197 and 204 (timed in turn, pages of 64 and 32 rows).
 // SPLIT: the tiles of a block are cut into pieces (a.n_split > 1).
 template <int G, bool EIGHTS, bool SPLIT>
 __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_prompt_attn(const PromptArgs a) {
