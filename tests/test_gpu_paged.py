@@ -99,6 +99,13 @@ def test_decode_long_ragged(dtype):
     run_decode([40003, 17, 9000, 0, 12345], 1, 4, 64, dtype)
 
 
+def test_decode_ragged_batches_that_fit_with_longer_pieces():
+    # at an even share the sequences would be cut into more pieces than run at once: longer ones are tried, for batches
+    # of fewer and of more sequences than lanes
+    run_decode([(s * 37) % 2000 + 1 for s in range(200)], 1, 2, 64, BF)
+    run_decode([(s * 379) % 4000 + 1 for s in range(40)], 8, 1, 64, BF)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("G", [1, 8])
 @pytest.mark.parametrize("lens", [[2241], [2049, 64, 191], [9001], [33000]])
