@@ -14,7 +14,7 @@
 //
 // G = 4, 8 KV heads: 8192 tokens from the beginning take 475 to 505 us, 1.1 PFLOP/s of the products that the mask leaves
 // (a large library product reaches 1.52 to 1.58); the matrix pipe is busy for 58 % of the cycles at 2.1 GHz.  What
-// stands against more is issue (the same launch on zeros, at the full clock, takes 400 us) and then power; arrangements
+// stands against more is issue (the same launch on zeros, at the full clock, takes 380 us) and then power; arrangements
 // with fewer vector instructions, phases of the two wavefronts of a SIMD against each other or a barrier for every two
 // tiles, with four buffers, came out the same.  Tiles
 // straight to LDS and eight wavefronts on them instead of four with loads through registers: 532 us, not 600.
@@ -240,7 +240,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-  float m = PR_NEG_BIG, l = 0.f;                        // of the unscaled scores; l: of this lane's rows
+  // Scores are held in powers of two relative to m.  Nothing seen yet: m = 0, and any score is above the threshold.
+  constexpr float NOTHING = -3.0e38f, LAZY = 8.f;
+  float m = 0.f, above = NOTHING, l = 0.f;              // l: of this lane's rows
 
   // ---- where rows are ----
   // Page numbers are looked up by whole wavefronts: EIGHTS: lane 8 i + j for rows 8 j of tile i of the next eight
@@ -312,13 +314,26 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     }
     if (lane == 0) odd_lds[t & 3][wave] = (uint8_t)rows;
   };
+  // Rows of a tile that the query sees.
+  auto seen_of = [&](int t, uint64_t missing) -> uint64_t {
+    const int r0 = qb.first_row(tile0 + t), last = p - r0;
+    uint64_t sees = last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1);
+    if (a.window >= 0) {
+      const int first = p - a.window + 1 - r0, sinks = qb.n_sink - r0;
+      uint64_t near = first <= 0 ? ~0ull : (first > 63 ? 0 : ~0ull << first);
+      near |= sinks <= 0 ? 0 : (sinks > 63 ? ~0ull : (1ull << sinks) - 1);
+      sees &= near;
+    }
+    return sees & ~missing;
+  };
   // ... and what has left the tile is added to the queries that see it
-  uint64_t seen = 0;                                    // rows of the tile that the query sees
   auto add_odd_values = [&](int t, uint64_t missing) {
     if (all_whole.has(t) && missing == 0) return;
     const uint64_t in_lds = *reinterpret_cast<const uint64_t*>(odd_lds[t & 3]);
     uint64_t rows = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)in_lds) |
                     (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(in_lds >> 32)) << 32;
+    if (rows == 0) return;
+    const uint64_t seen = seen_of(t, missing);
     for (; rows; rows &= rows - 1) {
       const int r = __builtin_ctzll(rows);
       const int at = a.pages.row(qb.s, h, qb.first_row(tile0 + t) + r);
@@ -379,18 +394,9 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
     acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.f[c], pr, acc[c], 0, 0, 0);
   };
   // Scores of rows that the query does not see become -infinity.
-  auto mask = [&](int t, uint64_t missing, Scores& sc) -> uint64_t {
-    if (whole.has(t) && missing == 0) return ~0ull;
-    const int r0 = qb.first_row(tile0 + t), last = p - r0;
-    uint64_t sees = last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1);
-    if (a.window >= 0) {
-      const int first = p - a.window + 1 - r0, sinks = qb.n_sink - r0;
-      uint64_t near = first <= 0 ? ~0ull : (first > 63 ? 0 : ~0ull << first);
-      near |= sinks <= 0 ? 0 : (sinks > 63 ? ~0ull : (1ull << sinks) - 1);
-      sees &= near;
-    }
-    sees &= ~missing;
-    const uint64_t rows = sees >> (4 * half);
+  auto mask = [&](int t, uint64_t missing, Scores& sc) {
+    if (whole.has(t) && missing == 0) return;
+    const uint64_t rows = seen_of(t, missing) >> (4 * half);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -398,35 +404,42 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
         const uint32_t bit = 1u << (8 * (i >> 2) + (i & 3));
         sc[b][i] = ((uint32_t)(rows >> (32 * b)) & bit) ? sc[b][i] : -INFINITY;
       }
-    return sees;
+  };
+  // Scores (2 j) and (2 j + 1) of the 32, relative to m, and their maximum.
+  auto relative = [&](int j, Scores& sc, float& mx) {
+    float x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) x[u] = fmaf(sc[j >> 3][2 * (j & 7) + u], a.scale_log2e, -m);
+    mx = fmaxf(fmaxf(mx, x[0]), x[1]);
+    asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(mx));
+#pragma unroll
+    for (int u = 0; u < 2; ++u) sc[j >> 3][2 * (j & 7) + u] = x[u];
   };
   // The maximum in use may be smaller than the true one by 8 powers of two: probabilities are relative to
   // each other, and up to 256 they are as exact as up to 1.
-  auto raise = [&](float mx) {
+  auto raise = [&](float mx, Scores& sc) {
     mx = xor32(mx, OpMax());
-    if (__ballot((mx - m) * a.scale_log2e > 8.f)) {
-      mx = fmaxf(mx, m);
-      const float corr = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e);
+    if (__ballot(mx > above)) {
+      const bool first = above == NOTHING;
+      const float up = first ? (mx > NOTHING ? mx : 0.f) : fmaxf(mx, 0.f);
+      const float corr = first ? 1.f : __builtin_amdgcn_exp2f(-up);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[c][i] *= corr;
       l *= corr;
-      m = mx;
-    }
-  };
-  auto max_of = [&](float mx, const Scores& sc, int quarter) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const int e = 8 * (quarter & 1) + i;
-      mx = fmaxf(fmaxf(mx, sc[quarter >> 1][e]), sc[quarter >> 1][e + 1]);
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[b][i] -= up;
+      m += up;
+      above = mx > NOTHING ? LAZY : above;
     }
-    return mx;
   };
 
   // A tile in two parts, so that there is something for the matrix cores and something for the vector ALUs in both:
   //   the scores of the next tile, while the probabilities of this one are taken;
-  //   the products of this one's probabilities and values, while the maximum of the next scores is found.
+  //   the products of this one's probabilities and values, while the next scores are scaled and their maximum is found.
   // Vector instructions are laid between the products by hand; operands are read two groups of four products ahead
   // (LDS answers later than one group takes).  At the begin of tile t all wavefronts ask for the keys of t + 3 and the
   // values of t + 2, whose buffers were read for tile t - 1; what was asked for before that has to be there at its end.
@@ -464,17 +477,11 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
       group_barrier();
       request(t + 3, b2, b0);
       // gone: of tiles t + 3, t + 2, t + 1, t
-      const float mc = m * a.scale_log2e;
       Group k0 = read_keys(b1, 0), k1, k2, k3, v0, v1;
-      float x[17][2], e[17][2];
-      auto scaled = [&](int j) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) x[j][u] = fmaf(sc[j >> 3][2 * (j & 7) + u], a.scale_log2e, -mc);
-        asm volatile("" : "+v"(x[j][0]), "+v"(x[j][1]));
-      };
+      float e[17][2];
       auto powers = [&](int j) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) e[j][u] = __builtin_amdgcn_exp2f(x[j][u]);
+        for (int u = 0; u < 2; ++u) e[j][u] = __builtin_amdgcn_exp2f(sc[j >> 3][2 * (j & 7) + u]);
         asm volatile("" : "+v"(e[j][0]), "+v"(e[j][1]));
       };
       auto packed = [&](int j) {
@@ -486,24 +493,22 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
         asm volatile("" : "+v"(pb[j >> 2][j & 3]), "+v"(l));
       };
       __builtin_amdgcn_s_setprio(1);
-      scaled(0);
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {                    // one product, and one step of each of three pairs
+      for (int j = 0; j < 16; ++j) {                    // one product, and one step of each of two pairs
         const int g = j >> 2;
         if (j == 0) k1 = read_keys(b1, 1);
         if (j == 4) k2 = read_keys(b1, 2);
         if (j == 8) k3 = read_keys(b1, 3);
         if (j == 12) v0 = read_values(b0, 0);
         score(g == 0 ? k0 : (g == 1 ? k1 : (g == 2 ? k2 : k3)), g, j & 3, next);
-        if (j + 1 < 16) scaled(j + 1);
         powers(j);
         if (j > 0) packed(j - 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       packed(15);
       __builtin_amdgcn_s_setprio(0);
-      const uint64_t next_seen = mask(t + 1, gone[2], next);
-      float mx = PR_NEG_BIG;
+      mask(t + 1, gone[2], next);
+      float mx = NOTHING;
       v1 = read_values(b0, 1);
       Group v2, v3;
 #pragma unroll
@@ -512,19 +517,15 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
         if (j == 0) v2 = read_values(b0, 2);
         if (j == 4) v3 = read_values(b0, 3);
         weigh(s == 0 ? v0 : (s == 1 ? v1 : (s == 2 ? v2 : v3)), s, j & 3);
-        if (j & 3) continue;
-        if (s > 0) mx = max_of(mx, next, s - 1);
+        relative(j, next, mx);
         __builtin_amdgcn_sched_barrier(0);
       }
-      mx = max_of(mx, next, 3);
       add_odd_values(t, gone[3]);
-      seen = next_seen;
-      raise(mx);
+      raise(mx, next);
       arrived(t);
     };
     auto use_last = [&](int t, Scores& sc) {            // without a next tile; gone: of t + 2, t + 1, t
       group_barrier();
-      const float mc = m * a.scale_log2e;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const Group v = read_values(b0, s);
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
           float e[2];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            e[u] = __builtin_amdgcn_exp2f(fmaf(sc[j >> 3][2 * (j & 7) + u], a.scale_log2e, -mc));
+            e[u] = __builtin_amdgcn_exp2f(sc[j >> 3][2 * (j & 7) + u]);
             two[u] = (bf16)e[u];
           }
           l += e[0] + e[1];
@@ -563,11 +564,11 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
         for (int i = 0; i < 4; ++i) score(k, g, i, sa);
       }
-      seen = mask(my_first, gone[2], sa);
-      float mx = PR_NEG_BIG;
+      mask(my_first, gone[2], sa);
+      float mx = NOTHING;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = max_of(mx, sa, i);
-      raise(mx);
+      for (int j = 0; j < 16; ++j) relative(j, sa, mx);
+      raise(mx, sa);
       const bool last = my_end == n_tiles;              // otherwise a next one is scored, of which nothing is seen
       const int end = last ? n_tiles - 1 : my_end;
       int t = my_first;
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
   if (SPLIT && n_pieces > 1) {
     if (!mine.there) return;
     const Partial to(a.part, ((int64_t)block * a.Hkv + h) * n_split + piece);
-    *to.stats(tid) = make_float2(m, l);
+    *to.stats(tid) = make_float2(above == NOTHING ? PR_NEG_BIG : m, l);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       *to.four(i, tid) = make_float4(acc[i >> 2][4 * (i & 3)], acc[i >> 2][4 * (i & 3) + 1], acc[i >> 2][4 * (i & 3) + 2],
@@ -652,8 +653,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) void k_prompt_join(const PromptArgs 
         f[k] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
       const float mx = fmaxf(m, st[k].x);
-      const float old = __builtin_amdgcn_exp2f((m - mx) * a.scale_log2e);
-      const float add = __builtin_amdgcn_exp2f((st[k].x - mx) * a.scale_log2e);
+      const float old = __builtin_amdgcn_exp2f(m - mx), add = __builtin_amdgcn_exp2f(st[k].x - mx);
       m = mx;
       l = l * old + st[k].y * add;
       x[0] = x[0] * old + f[k].x * add;

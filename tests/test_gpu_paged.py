@@ -445,6 +445,22 @@ def test_prompt_scores_far_apart_and_growing():
     close(out[:, 0], want, tol, "falling scores")
 
 
+@pytest.mark.parametrize("n_sink,window", [(0, -1), (0, 70), (3, 40)])
+@pytest.mark.parametrize("level", [-50.0, 50.0])
+def test_prompt_scores_far_from_zero(level, n_sink, window):
+    """All scores near 565 or -565, and queries that see nothing of their first tiles."""
+    n, m = 400, 300
+    c = Cache([n], 1, 16, BF, 9, DEV)
+    for r in range(n):
+        c.write(0, 0, r, k=torch.full((D,), level * (1 + r % 3 / 64)))
+    q = torch.ones(m, 1, D, dtype=BF)
+    out = torch.empty(m, 1, D, dtype=BF, device=DEV)
+    ck.ck_prompt_attn(shape(1, 1, 1), q.to(DEV), i32([0, m]), c.kv(), i32([n]), out, n_sink=n_sink, window=window)
+    seen = np.stack([seen_rows(n, n - m + i, n_sink, window) for i in range(m)])
+    want, tol = attend(q[:, 0], c.rows_k[0][0], c.rows_v[0][0], seen, BF, p_step=2.0 ** -8)
+    close(out[:, 0], want, tol, "scores far from zero")
+
+
 def test_prompt_long_runs_twice_the_same_and_from_a_graph():
     lens, news, Hkv, G = [1500, 700], [1500, 300], 2, 4
     c = Cache(lens, Hkv, 64, BF, 8, DEV)
