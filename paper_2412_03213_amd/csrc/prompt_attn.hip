@@ -12,13 +12,14 @@
 //                 queries in its lanes again, so scaling it is in-lane too.
 // Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
 //
-// G = 4, 8 KV heads: 8192 tokens from the beginning take 475 to 505 us, 1.1 PFLOP/s of the products that the mask leaves
+// G = 4, 8 KV heads: 8192 tokens from the beginning take 475 to 490 us, 1.1 PFLOP/s of the products that the mask leaves
 // (a large library product reaches 1.52 to 1.58); the matrix pipe is busy for 58 % of the cycles at 2.1 GHz.  What
 // stands against more is issue (the same launch on zeros, at the full clock, takes 380 us) and then power; arrangements
 // with fewer vector instructions, phases of the two wavefronts of a SIMD against each other or a barrier for every two
-// tiles, with four buffers, came out the same.  Tiles
+// tiles, with four buffers, came out the same.  Scores scaled before the exponent instead of under the products with the
+// values: 484 us, not 476.  Tiles
 // straight to LDS and eight wavefronts on them instead of four with loads through registers: 532 us, not 600.
-// Chunks with a window of 1024 (G = 8): 215 us, 0.79 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
+// Chunks with a window of 1024 (G = 8): 210 us, 0.81 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
 // outputs, whose traffic nothing else overlaps.  17 tokens behind 30011 rows for each of two sequences: 47 us, 224 MB
 // at 4.8 TB/s.
 #include "paged.hpp"
