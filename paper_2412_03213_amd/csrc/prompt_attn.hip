@@ -57,23 +57,24 @@ typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
 __device__ __forceinline__ int swizzle(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
 
 // The block of queries of a workgroup: which sequence, which of its new tokens, which tiles of the cache they see.
-// The last block of a sequence, which sees most rows, comes first.
+// The last block of a sequence, which sees most rows, comes first.  Only tokens that the call has rows for are in
+// blocks; which rows of the cache are theirs goes by all that the starts tell of, those behind the call's rows among them.
 struct QueryBlock {
   int s, begin, tok0, n_tok;                            // rows [begin + tok0, + n_tok) of q
   int p0, p_last, end;                                  // cache rows of the first and last token; rows seen < end
   int n_sink, sink_tiles, gap, n_tiles;                 // tile j < sink_tiles is tile j of the cache, else j + gap
-  __device__ __forceinline__ static int bound(const PromptArgs& a, int s) {
-    const int t = a.starts[s];
+  __device__ __forceinline__ static int bound(const PromptArgs& a, int t) {
     return t < 0 ? 0 : (t < a.n_rows ? t : a.n_rows);
   }
   __device__ __forceinline__ bool find(const PromptArgs& a, int w, int tokens) {
     const int lane = threadIdx.x & 63;
     int before = 0;
     for (int s0 = 0; s0 < a.S; s0 += WAVE) {
-      int b = 0, m = 0;
+      int b = 0, m = 0, ends = 0;                       // ends: starts[s + 1], maybe behind the rows of the call
       if (s0 + lane < a.S) {
-        b = bound(a, s0 + lane);
-        m = max(0, bound(a, s0 + lane + 1) - b);
+        ends = a.starts[s0 + lane + 1];
+        b = bound(a, a.starts[s0 + lane]);
+        m = max(0, bound(a, ends) - b);
       }
       const int n = (m + tokens - 1) / tokens;
       const int upto = before + wave_inclusive_scan(n);
@@ -86,7 +87,9 @@ struct QueryBlock {
         tok0 = (__builtin_amdgcn_readlane(upto, l) - 1 - w) * tokens;
         n_tok = min(tokens, n_new - tok0);
         const int length = __builtin_amdgcn_readfirstlane(a.pages.clamp_length(a.lengths[s]));
-        p0 = length - n_new + tok0;                     // negative: sees nothing
+        // negative: sees nothing.  A block has at most PR_ROWS tokens: from -PR_ROWS down all of them are before row 0.
+        const int64_t first = (int64_t)length - ((int64_t)__builtin_amdgcn_readlane(ends, l) - begin) + tok0;
+        p0 = first > -PR_ROWS ? (int)first : -PR_ROWS;
         p_last = p0 + n_tok - 1;
         end = max(p_last + 1, 0);                       // <= length
         n_sink = a.window < 0 ? 0 : a.n_sink;

@@ -1,0 +1,68 @@
+"""Calls on paged caches at the edge of what the header allows."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2412_03213_amd as ck
+from paged_ref import D, Cache, attend, seen_rows
+from test_gpu_paged import BF, DEV, close, i32, shape
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_sink,window", [(0, -1), (3, 20)])
+@pytest.mark.parametrize("lens,starts,n_rows", [
+    ([10], [0, 10], 6), ([400, 90], [0, 300, 390], 350), ([400, 90], [0, 300, 390], 290), ([64, 700], [0, 64, 2 ** 30], 100),
+    ([40, 300], [-7, 20, 320], 320), ([3000], [-2, 3], 1)])
+def test_starts_beyond_the_rows_of_the_call(lens, starts, n_rows, n_sink, window):
+    """Tokens in front of row 0 and from n_rows on are not there; the others keep the rows of the cache that starts
+    and lengths give them, for the append and for the attention."""
+    Hkv, G, page = 2, 2, 16
+    S = len(lens)
+    c = Cache(lens, Hkv, page, BF, 3, DEV)
+    kv, sh = c.kv(), shape(S, Hkv, G)
+    g = torch.Generator().manual_seed(1)
+    q, v = (torch.randn(n_rows, h, D, generator=g).to(BF) for h in (Hkv * G, Hkv))
+    rows = {}                                            # token row -> sequence, row of the cache
+    for s in range(S):
+        for t in range(max(0, starts[s]), min(n_rows, starts[s + 1])):
+            rows[t] = (s, lens[s] - (starts[s + 1] - starts[s]) + t - starts[s])
+    out = torch.full_like(q, 123.0, device=DEV)
+    ck.ck_prompt_attn(sh, q.to(DEV), i32(starts), kv, i32(lens), out, n_sink=n_sink, window=window)
+    for s in range(S):
+        mine = [t for t in rows if rows[t][0] == s]
+        seen = [seen_rows(lens[s], rows[t][1], n_sink, window) for t in mine]
+        for h in range(Hkv if mine else 0):
+            qs = q[mine, h * G:(h + 1) * G].reshape(-1, D)
+            want, tol = attend(qs, c.rows_k[s][h], c.rows_v[s][h], np.stack(seen).repeat(G, 0), BF, p_step=2.0 ** -8)
+            close(out[mine, h * G:(h + 1) * G].reshape(-1, D), want, tol, f"sequence {s} head {h}")
+    assert (out[[t for t in range(n_rows) if t not in rows]] == 123.0).all()
+    V = kv.V.clone()
+    ck.ck_rope_append(sh, None, v.to(DEV), v.to(DEV), kv, i32(lens), torch.ones(64, device=DEV), None,
+                      q_starts=i32(starts))
+    for t, (s, r) in rows.items():
+        if r >= 0:
+            V[c.table[s, r // page], :, r % page] = v[t].to(DEV)
+    assert torch.equal(kv.V.view(torch.int16), V.view(torch.int16))
+
+
+def test_starts_beyond_the_rows_in_a_replayed_graph():
+    c = Cache([500, 60], 2, 16, BF, 3, DEV)
+    kv, sh = c.kv(), shape(2, 2, 4)
+    q = torch.randn(100, 8, D, device=DEV).to(BF)
+    starts, n, out, ws = i32([0, 60, 100]), i32([500, 60]), torch.empty_like(q), ck.prompt_workspace(sh, 100, DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ck.ck_prompt_attn(sh, q, starts, kv, n, out, workspace=ws)
+    for at in ([0, 60, 100], [0, 450, 500], [0, 90, 150], [0, 60, 100]):
+        starts.copy_(i32(at))
+        graph.replay()
+        torch.cuda.synchronize()
+        # the same tokens, with rows for all of them
+        whole = torch.zeros(at[-1], 8, D, dtype=BF, device=DEV)
+        whole[:100] = q
+        want = torch.empty_like(whole)
+        ck.ck_prompt_attn(sh, whole, starts, kv, n, want)
+        a, b = want[:100].float(), out.float()
+        # cut into other pieces: probabilities of both sides rounded to bf16 relative to other maxima, and the outputs
+        assert ((a - b).abs() <= 2 ** -7 * a.abs() + 2 * 2 ** -8 * 5.0).all()
