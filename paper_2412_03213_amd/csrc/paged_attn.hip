@@ -16,6 +16,8 @@
 // bf16: both products on the matrix cores, 16 tokens a step, as in the attention over recalled tokens:
 // q K^T with the K rows turned into operand layout through LDS, P V with the operands in the lanes that hold
 // them.  A probability enters the product as two bf16 numbers that hold 16 bits of it.
+#include <float.h>
+
 #include <type_traits>
 
 #include "decode_common.hpp"
@@ -25,7 +27,8 @@ namespace ck {
 
 namespace {
 
-constexpr float PA_NEG_BIG = -1.0e30f;                  // "no row yet": finite so that differences stay finite
+// "no row yet", the lowest number: below no score, and finite, so that its difference to itself is zero
+constexpr float PA_NEG_BIG = -FLT_MAX;
 constexpr int PA_WAVES = 4;
 constexpr int PA_STEP = 16;                             // tokens of a wavefront per step
 // Pieces of a batch and their least length, two steps of each wavefront.  Half as long: 4000 rows of one sequence 10.3 us,

@@ -22,13 +22,15 @@
 // Chunks with a window of 1024 (G = 8): 210 us, 0.81 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
 // outputs, whose traffic nothing else overlaps.  17 tokens behind 30011 rows for each of two sequences: 47 us, 224 MB
 // at 4.8 TB/s.
+#include <float.h>
+
 #include "paged.hpp"
 
 namespace ck {
 
 namespace {
 
-constexpr float PR_NEG_BIG = -1.0e30f;
+constexpr float PR_NEG_BIG = -FLT_MAX;                  // no row yet: below no score
 constexpr int PR_WAVES = 8;
 constexpr int PR_ROWS = PR_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int PR_TILE = 64;                             // cache rows of a tile
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(PR_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
   // Scores are held in powers of two relative to m.  Nothing seen yet: m = 0, and any score is above the threshold.
-  constexpr float NOTHING = -3.0e38f, LAZY = 8.f;
+  constexpr float NOTHING = PR_NEG_BIG, LAZY = 8.f;
   float m = 0.f, above = NOTHING, l = 0.f;              // l: of this lane's rows
 
   // ---- where rows are ----

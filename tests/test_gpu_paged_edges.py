@@ -5,7 +5,7 @@ import torch
 
 import paper_2412_03213_amd as ck
 from paged_ref import D, Cache, attend, seen_rows
-from test_gpu_paged import BF, DEV, close, i32, shape
+from test_gpu_paged import BF, DEV, F32, close, i32, shape
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,29 @@ def test_starts_beyond_the_rows_in_a_replayed_graph():
         a, b = want[:100].float(), out.float()
         # cut into other pieces: probabilities of both sides rounded to bf16 relative to other maxima, and the outputs
         assert ((a - b).abs() <= 2 ** -7 * a.abs() + 2 * 2 ** -8 * 5.0).all()
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[1], [3, 1, 40], [2100, 17], [9001]])
+def test_decode_scores_of_any_finite_size(lens, dtype):
+    """Equal scores near -2^110: every row has the same share, as where all scores are zero."""
+    c = Cache(lens, 1, 16, dtype, 5, DEV)
+    c.K.fill_(-2.0 ** 50)
+    q = torch.full((len(lens), 2, D), 2.0 ** 56, dtype=dtype)
+    out = torch.empty(len(lens), 2, D, dtype=dtype, device=DEV)
+    ck.ck_paged_decode_attn(shape(len(lens), 1, 2, dtype), q.to(DEV), c.kv(), i32(lens), out)
+    for s, n in enumerate(lens):
+        want, tol = attend(q[s] * 0, c.rows_k[s][0], c.rows_v[s][0], np.ones((2, n)), dtype,
+                           p_step=2.0 ** -15 if dtype is BF else 0.0)
+        close(out[s], want, tol, f"sequence {s}")
+
+
+@pytest.mark.parametrize("n,m", [(1, 1), (300, 300), (3000, 3), (9000, 40)])
+def test_prompt_scores_of_any_finite_size(n, m):
+    c = Cache([n], 1, 16, BF, 5, DEV)
+    c.K.fill_(-2.0 ** 50)
+    q = torch.full((m, 2, D), 2.0 ** 56, dtype=BF)
+    out = torch.empty(m, 2, D, dtype=BF, device=DEV)
+    ck.ck_prompt_attn(shape(1, 1, 2), q.to(DEV), i32([0, m]), c.kv(), i32([n]), out)
+    seen = np.stack([seen_rows(n, n - m + i, 0, -1) for i in range(m)]).repeat(2, 0)
+    want, tol = attend(q.reshape(2 * m, D) * 0, c.rows_k[0][0], c.rows_v[0][0], seen, BF, p_step=2.0 ** -8)
+    close(out.reshape(2 * m, D), want, tol, "equal scores")
