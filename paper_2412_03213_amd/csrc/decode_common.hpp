@@ -3,8 +3,27 @@
 // size gather / prefix sum of Section IV-C, Fig. 8).
 #pragma once
 #include "ck_common.hpp"
+#include "ticket.hpp"
 
 namespace ck {
+
+// Draws a ticket; whether it is the last of `expected` (below 2^15), which leaves the word idle.  One fetch-add does
+// for a word of ours.  Another word is taken over by a compare-and-swap; whoever added to it before that adds itself again
+// through the same loop, so that every arrival is counted once.
+__device__ __forceinline__ bool draw_ticket(unsigned long long* ticket, int expected) {
+  const Ticket::Word old = __hip_atomic_fetch_add(ticket, Ticket::ONE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  Ticket::Word now = old + Ticket::ONE;
+  if (Ticket::count(old, expected) < 0) {
+    Ticket::Word seen = now;
+    do {
+      now = Ticket::after(seen, expected);
+    } while (!__hip_atomic_compare_exchange_strong(ticket, &seen, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                                   __HIP_MEMORY_SCOPE_AGENT));
+  }
+  const bool last = Ticket::complete(now, expected);
+  if (last) __hip_atomic_store(ticket, Ticket::IDLE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return last;
+}
 
 template <typename T>
 __device__ __forceinline__ void load_row8(const T* p, float (&v)[8]);

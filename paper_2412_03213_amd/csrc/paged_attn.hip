@@ -42,7 +42,6 @@ constexpr int PA_TRIES = 8;
 // head with G = 8 (512 pieces) 90 us, not 26.  In one stage up to 32 pieces: 4000 rows 11.6 us, not 9.6.
 constexpr int PA_FAN = 16;
 constexpr int PA_PART = D + 2;                          // floats of a (piece, query head): max, sum, acc[128]
-constexpr unsigned long long PA_TICKET = 0x434B5061676Eull;   // marks a ticket word as ours
 
 struct PagedArgs {
   const void *q, *K, *V;
@@ -336,27 +335,12 @@ struct StateF32 {
 };
 
 // Whether this workgroup is the last of `expected` that have written what others will read.  The stores before it are
-// performed where every XCD looks; each thread waits for its own before the barrier, only then is the ticket drawn.  A
-// ticket word that does not carry the mark (memory that held something else) is taken over by a compare-and-swap;
-// whoever added to it before that adds itself again.
+// performed where every XCD looks; each thread waits for its own before the barrier, only then is the ticket drawn.
 __device__ __forceinline__ bool last_to_arrive(unsigned long long* ticket, int expected, int* s_last) {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const unsigned long long old = __hip_atomic_fetch_add(ticket, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    unsigned long long now = old + 1;
-    if ((old >> 16) != PA_TICKET) {
-      unsigned long long seen = now;
-      do {
-        now = (seen >> 16) == PA_TICKET ? seen + 1 : ((PA_TICKET << 16) | 1ull);
-      } while (!__hip_atomic_compare_exchange_strong(ticket, &seen, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                     __HIP_MEMORY_SCOPE_AGENT));
-    }
-    const int last = (int)(now & 0xFFFFull) == expected;
-    if (last) __hip_atomic_store(ticket, PA_TICKET << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *s_last = last;
-  }
+  if (threadIdx.x == 0) *s_last = draw_ticket(ticket, expected);
   __syncthreads();
   const bool last = *s_last != 0;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");

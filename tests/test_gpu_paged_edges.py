@@ -92,3 +92,41 @@ def test_prompt_scores_of_any_finite_size(n, m):
     seen = np.stack([seen_rows(n, n - m + i, 0, -1) for i in range(m)]).repeat(2, 0)
     want, tol = attend(q.reshape(2 * m, D) * 0, c.rows_k[0][0], c.rows_v[0][0], seen, BF, p_step=2.0 ** -8)
     close(out.reshape(2 * m, D), want, tol, "equal scores")
+
+
+def overwritten(ws):
+    """A workspace's words as a call has left them, with parts overwritten: what a smaller tensor writes that gets the
+    memory after it was freed, and words that carry marks of their own."""
+    left = ws.clone().view(torch.int16).view(-1, 4)
+    for parts in ([0], [1], [3], [0, 1], [2, 3], [0, 3]):
+        for value in (1, 2, 15, 0x3F80):
+            w = left.clone()
+            w[:, parts] = value
+            yield w
+    for byte in (0, 7):
+        w = left.clone().view(torch.uint8).view(-1, 8)
+        w[:, byte] = 1
+        yield w
+    for mark in (0x434B5061676E, 0x434B7469636B):
+        for value in (1, 15, 0x3F80):
+            yield torch.full_like(left.view(torch.int64), mark << 16 | value)
+
+
+@pytest.mark.parametrize("lens,Hkv", [([2048], 1), ([2049], 1), ([9001, 300], 1), ([3000, 100, 700], 2)])
+def test_decode_workspace_of_any_contents(lens, Hkv):
+    """16 and 17 pieces of a head, joined in one stage and in two, and ragged ones."""
+    c = Cache(lens, Hkv, 32, BF, 21, DEV)
+    kv, sh, n = c.kv(), shape(len(lens), Hkv, 2), i32(lens)
+    q = torch.randn(len(lens), 2 * Hkv, D, device=DEV).to(BF)
+    ws, want, got = ck.paged_decode_workspace(sh, DEV), torch.empty_like(q), torch.empty_like(q)
+    ck.ck_paged_decode_attn(sh, q, kv, n, want, workspace=ws)
+    seen = np.ones((2, lens[0]))
+    exact, tol = attend(q[0, :2].cpu(), c.rows_k[0][0], c.rows_v[0][0], seen, BF, p_step=2.0 ** -15)
+    close(want[0, :2], exact, tol, "sequence 0")
+    for i, words in enumerate(overwritten(ws)):
+        for again in range(2):
+            if again == 0:
+                ws.copy_(words.view(torch.uint8).flatten())
+            got.fill_(float("nan"))
+            ck.ck_paged_decode_attn(sh, q, kv, n, got, workspace=ws)
+            assert torch.equal(got, want), (i, again)
