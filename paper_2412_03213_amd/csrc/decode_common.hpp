@@ -12,15 +12,15 @@ namespace ck {
 // through the same loop, so that every arrival is counted once.
 __device__ __forceinline__ bool draw_ticket(unsigned long long* ticket, int expected) {
   const Ticket::Word old = __hip_atomic_fetch_add(ticket, Ticket::ONE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  Ticket::Word now = old + Ticket::ONE;
-  if (Ticket::count(old, expected) < 0) {
-    Ticket::Word seen = now;
+  bool last = Ticket::complete(old + Ticket::ONE, expected);
+  if (!last && Ticket::count(old, expected) < 0) {
+    Ticket::Word seen = old + Ticket::ONE, now;
     do {
       now = Ticket::after(seen, expected);
     } while (!__hip_atomic_compare_exchange_strong(ticket, &seen, now, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
                                                    __HIP_MEMORY_SCOPE_AGENT));
+    last = Ticket::complete(now, expected);
   }
-  const bool last = Ticket::complete(now, expected);
   if (last) __hip_atomic_store(ticket, Ticket::IDLE, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return last;
 }

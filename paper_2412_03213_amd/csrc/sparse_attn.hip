@@ -46,7 +46,6 @@ constexpr float NEG_BIG = -1.0e30f;        // "no token yet": finite so that dif
 constexpr int ATT_XCD_CUS = 32;            // compute units of one XCD
 constexpr int PART_STRIDE = D + 2;         // floats per (split, query head): max, sum, acc[128]
 constexpr int N_XCD = 8;                   // workgroup i of a launch runs on XCD i % 8
-constexpr unsigned long long TICKET_MAGIC = 0x434B7469636Bull;   // marks a ticket word as ours
 
 enum { ATT_PLAIN = 0, ATT_FUSED = 1, ATT_FUSED_SCORE = 2 };
 
@@ -152,7 +151,7 @@ struct AttnArgs {
   const void *q, *K, *V;
   void* out;
   float* part;                  // [HP, n_split, G, PART_STRIDE]
-  unsigned long long* tickets;  // [HP]: (TICKET_MAGIC << 16) | workgroups arrived so far
+  unsigned long long* tickets;  // [HP], see Ticket
   // given index list
   const int32_t* token_idx;
   const int32_t* n_tokens;
@@ -797,28 +796,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
-  if (tid == 0) {
-    // Idle state of a ticket word: TICKET_MAGIC in the upper 48 bits, count 0.  One
-    // fetch-add draws the ticket.  A word that does not carry the mark (memory this
-    // library has never used: the first launch on a fresh workspace) is taken over with
-    // a compare-and-swap loop instead; whoever added to it before the take-over adds
-    // itself again through the same loop, so every workgroup is counted exactly once.
-    unsigned long long* tk = a.tickets + hp;
-    unsigned long long old =
-        __hip_atomic_fetch_add(tk, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    unsigned long long now = old + 1;
-    if ((old >> 16) != TICKET_MAGIC) {
-      unsigned long long seen = now;
-      do {
-        now = (seen >> 16) == TICKET_MAGIC ? seen + 1 : ((TICKET_MAGIC << 16) | 1ull);
-      } while (!__hip_atomic_compare_exchange_strong(tk, &seen, now, __ATOMIC_RELAXED,
-                                                     __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    }
-    const int last = (int)(now & 0xFFFFull) == a.n_split;
-    // back to idle: ready for the next launch (or a replay of this one from a graph)
-    if (last) __hip_atomic_store(tk, TICKET_MAGIC << 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = last;
-  }
+  // The last one leaves the word ready for the next launch (or a replay of this one from a graph).
+  if (tid == 0) s_last = draw_ticket(a.tickets + hp, a.n_split);
   __syncthreads();
   if (!s_last) return;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");

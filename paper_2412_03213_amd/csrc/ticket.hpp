@@ -16,8 +16,8 @@ struct Ticket {
   static constexpr Word IDLE = 0x4B435469636B0000ull;   // no arrival: 0x5469636B between 0x4B43 and 0
   // arrivals that a word stands for, of fewer than `expected`; -1: none of ours
   static constexpr int count(Word w, int expected) {
-    const Word k = (w - IDLE) & 0xFFFFull;
-    return w - IDLE == k * ONE && (int)k < expected ? (int)k : -1;
+    const Word k = w & 0xFFFFull;
+    return w == IDLE + (k << 48 | k) && (int)k < expected ? (int)k : -1;
   }
   // what an arrival that has not been counted yet makes of a word
   static constexpr Word after(Word w, int expected) { return (count(w, expected) < 0 ? IDLE : w) + ONE; }
