@@ -536,19 +536,26 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 
 def _device(t):
-    """Index of the device of a call's first tensor (-1: host), which has to be the current one: the
-    default streams of all devices have one and the same handle.  None for an address."""
+    """Index of the device of a call's first tensor, which has to be the current one: the default
+    streams of all devices have one and the same handle.  None for an address."""
     if not isinstance(t, torch.Tensor):
         return None
     dev = t.get_device()
-    if dev >= 0 and dev != _current_device():
+    if dev < 0:
+        raise ValueError("tensors on the host: the kernels read device memory")
+    if dev != _current_device():
         raise ValueError(f"tensors on cuda:{dev}, which is not the current device")
     return dev
 
 
+def _elsewhere(t_dev: int, dev) -> bool:
+    """Of a tensor's device index; the call's is not known where its first argument is an address."""
+    return t_dev < 0 if dev is None else t_dev != dev
+
+
 def _kv(sh: Shape, kv, dev):
     if isinstance(kv, PagedKV):
-        if dev is not None and kv._device != dev:
+        if _elsewhere(kv._device, dev):
             raise ValueError("the cache is on another device")
         return ctypes.byref(kv.c(sh))
     return ctypes.byref(kv) if kv is not None else None      # a structure of raw addresses
@@ -556,7 +563,7 @@ def _kv(sh: Shape, kv, dev):
 
 # These check what the kernels take for granted; they are on the path of every generated token.
 def _same_device(t, name, dev):
-    if dev is not None and t.get_device() != dev:
+    if _elsewhere(t.get_device(), dev):
         raise ValueError(f"{name} is on another device")
     return t.data_ptr()
 
