@@ -168,21 +168,22 @@ __device__ __forceinline__ uint32_t finite_mask(uint32_t w) {
 }
 
 // 16 bytes for every lane from base + offset to LDS at `to` + 16 * lane, on their way when this returns:
-// they are counted with the vector loads (wait_for_tiles).
+// they are counted with the vector loads (wait_for_tiles).  The compiler brings `to` into m0, where the instruction
+// looks for it, and so knows what the register holds; a wait state has to lie between (s_nop).
 // ONCE: no other workgroup reads them (blocks in pieces, few to a sequence: 71 us, not 76, with this alone).
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
   if constexpr (ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
 }
 template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
   if constexpr (ONCE)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"{m0}"(to), "v"(from) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
 template <int LEFT>                                     // loads that may still be on their way
 __device__ __forceinline__ void wait_for_tiles() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
