@@ -9,8 +9,9 @@
 // sines of their 8 channels in registers for every head of the token.  The partner of a channel is in
 // the same lane (adjacent pairs) or rot / 2 channels further in the same 16 lanes.
 //
-// Angles: position * frequency in 64 bits, reduced to turns there.  In 32 bits the angle of the fastest
-// pair at position 120000 is off by 2^-8 radians, as much as the rounding of the result to bf16.
+// Angles: position * frequency, and its product with 1 / (2 pi), as sums of two 64-bit numbers, whole turns taken off there.
+// In 32 bits the angle of the fastest pair at position 120000 is off by 2^-8 radians, as much as the rounding of
+// the result to bf16; in single 64-bit products by up to 2^-21 radians at the last positions, more than all else in fp32.
 #include "paged.hpp"
 
 namespace ck {
@@ -81,6 +82,14 @@ template <> struct Vec8<float> {
   }
 };
 
+// pos * w / (2 pi) without its whole turns, within 2^-53 of a turn before it is rounded to 32 bits.
+__device__ __forceinline__ float part_of_a_turn(double pos, double w) {
+  constexpr double PER_TURN = 0x1.45f306dc9c883p-3, REST = -0x1.6b01ec5417056p-57;   // their sum: 1 / (2 pi)
+  const double a = pos * w, rest = fma(pos, w, -a);     // 31 and 24 bits: the product has up to 55
+  const double whole = rint(a * PER_TURN);
+  return (float)(fma(a, PER_TURN, -whole) + fma(a, REST, rest * PER_TURN));
+}
+
 template <typename T, int PAIRS>
 __global__ __launch_bounds__(256) void k_rope_append(const RopeArgs a) {
   __shared__ __attribute__((aligned(16))) float lds[4][2][D / 2 + 8];   // a vector may end behind rot / 2
@@ -102,10 +111,9 @@ __global__ __launch_bounds__(256) void k_rope_append(const RopeArgs a) {
   // ---- cosine and sine of pair `lane` ----
   const int half = a.rot >> 1;
   const float w = a.freqs[lane < half ? lane : 0];
-  double turns = pos * (double)w * 0.15915494309189533577;   // 1 / (2 pi)
-  turns -= rint(turns);
+  const float turns = part_of_a_turn(pos, (double)w);
   float sn, cs;
-  sincospif(2.f * (float)turns, &sn, &cs);
+  sincospif(2.f * turns, &sn, &cs);
   float(&cl)[D / 2 + 8] = lds[wave][0], (&sl)[D / 2 + 8] = lds[wave][1];
   cl[lane] = cs * a.factor;
   sl[lane] = sn * a.factor;

@@ -1,10 +1,13 @@
 """Calls on paged caches at the edge of what the header allows."""
+import math
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2412_03213_amd as ck
-from paged_ref import D, Cache, attend, seen_rows
+from paged_ref import D, STEP, Cache, attend, seen_rows
 from test_gpu_paged import BF, DEV, F32, close, i32, shape
 
 pytestmark = pytest.mark.gpu
@@ -130,3 +133,41 @@ def test_decode_workspace_of_any_contents(lens, Hkv):
             got.fill_(float("nan"))
             ck.ck_paged_decode_attn(sh, q, kv, n, got, workspace=ws)
             assert torch.equal(got, want), (i, again)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_rope_angles_next_to_whole_turns(adjacent, dtype):
+    """Positions that are close to multiples of pi: their sines show an error of the angle that is small beside a turn."""
+    positions = [0, 22, 710, 103993, 833719, 4272943, 80143857, 411557987, 1068966896, 2137933792, 2 ** 31 - 1, -4272943]
+    rates = [1.0, 0.5, float(np.float32(0.1))]
+    pi = 4 * (4 * _atan_of_one_over(5) - _atan_of_one_over(239))
+    n = len(positions)
+    c = Cache([n], 1, 16, dtype, 0, DEV)
+    kv = c.kv()
+    k = torch.zeros(n, 1, D, dtype=dtype)
+    first, second = (slice(0, D, 2), slice(1, D, 2)) if adjacent else (slice(0, D // 2), slice(D // 2, D))
+    k[..., first] = 1.0
+    freqs = torch.tensor(rates + [0.0] * (D // 2 - len(rates)), dtype=torch.float32, device=DEV)
+    out = torch.empty(n, 1, D, dtype=dtype, device=DEV)
+    ck.ck_rope_append(shape(1, 1, 1, dtype), k.to(DEV), k.to(DEV), k.to(DEV), kv, i32([n]), freqs, out,
+                      q_starts=i32([0, n]), positions=i32(positions), interleaved=adjacent)
+    rows = torch.stack([kv.K[c.table[0, r // 16], 0, r % 16] for r in range(n)])
+    for got in (out[:, 0], rows):
+        got = got.double().cpu()
+        for i, p in enumerate(positions):
+            for j, w in enumerate(rates):
+                turns = p * Fraction(w) / (2 * pi)
+                a = 2 * math.pi * float(turns - round(turns))
+                # The reduced angle a is rounded to fp32 once: it is off by d <= 2^-24 |a|, a cosine by |sin a| d, a sine
+                # by |cos a| d (near half a turn, where a sine is small and a is not, that is more than a rounding
+                # of the sine).  Then 4 roundings of fp32 (function 2, factor, sum), and that of the type.
+                d = abs(a) * 2.0 ** -24
+                for want, slope, have in ((math.cos(a), math.sin(a), got[i, first][j]),
+                                          (math.sin(a), math.cos(a), got[i, second][j])):
+                    tol = 2 * math.pi * 2.0 ** -50 + abs(slope) * d + d * d + abs(want) * (4 * 2.0 ** -24 + STEP[dtype])
+                    assert abs(float(have) - want) <= tol, (p, w, float(have), want)
+
+
+def _atan_of_one_over(n):
+    return sum(Fraction((-1) ** i, (2 * i + 1) * n ** (2 * i + 1)) for i in range(40))
