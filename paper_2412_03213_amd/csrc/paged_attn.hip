@@ -9,8 +9,8 @@
 // workgroup and, by the workgroup of a head-problem that is through last, over its pieces in their order.
 //
 // 8 KV heads, G = 4, bf16: 4 x 131072 rows 328 us (2.15 GB, 6.5 TB/s; 369 with loads that stay in the caches), 32 ragged
-// sequences of up to 8191 rows 102 us (605 MB, 5.9 TB/s), 16 x (1024 listed + 233) rows 18.1 us (83 MB).  2048 rows of one
-// sequence take 8.9 us in a graph: a launch 1.7, the piece found 0.3, rows and products 2.5, wavefronts joined 1, pieces
+// sequences of up to 8191 rows 102 us (605 MB, 5.9 TB/s), 16 x (1024 listed + 233) rows 17.5 us (83 MB); fp32, 4 x 32768 rows
+// 191 us (1.07 GB, 5.6 TB/s).  2048 rows of one sequence take 8.7 us in a graph: a launch 1.7, the piece found 0.3, rows and products 2.5, wavefronts joined 1, pieces
 // joined 3.5 (three round trips past L2).
 //
 // bf16: both products on the matrix cores, 16 tokens a step, as in the attention over recalled tokens:
@@ -34,7 +34,9 @@ constexpr int PA_STEP = 16;                             // tokens of a wavefront
 // Pieces of a batch and their least length, two steps of each wavefront.  Half as long: 4000 rows of one sequence 10.3 us,
 // not 9.6; twice as long: 500 rows 8.1, not 7.1.  1024 pieces: 32000 rows 30 us, not 26, the listed rows 23, not 18.
 constexpr int PA_MIN_PIECE = 2 * PA_WAVES * PA_STEP;
-constexpr int PA_PIECES = 512;                          // workgroups of four wavefronts that are resident together
+// Workgroups of four wavefronts that are resident together; 256 in fp32 with G = 8, which has registers for one
+// wavefront a SIMD and runs in two rounds (4 x 32768 rows of 8 heads 206 us, G = 4 191).
+constexpr int PA_PIECES = 512;
 // Times that the pieces are made longer by an eighth.  Never: 16 ragged sequences of up to 30000 rows 216 us, not 184, of
 // 8191 rows 57, not 54, 40 of 8191 rows 138, not 127.
 constexpr int PA_TRIES = 8;

@@ -10,18 +10,20 @@
 //                 taken in the order {16 s + 4 half + i, 16 s + 8 + 4 half + i}; V^T comes from LDS through
 //                 the transposing reads (ds_read_b64_tr_b16) in the same order.  The accumulator has the
 //                 queries in its lanes again, so scaling it is in-lane too.
-// Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.
+// Probabilities are rounded to bf16 for the product, as the values are; their sum is taken in fp32 before.  (A second bf16
+// number for the rest of each, as in the attention of one token, would make it half as many products again.)
 //
 // G = 4, 8 KV heads: 8192 tokens from the beginning take 475 to 490 us, 1.1 PFLOP/s of the products that the mask leaves
-// (a large library product reaches 1.52 to 1.58); the matrix pipe is busy for 58 % of the cycles at 2.1 GHz.  What
+// (a large library product reaches 1.43 to 1.58); the matrix pipe is busy for 60 % of the cycles at 1.8 to 1.9 GHz.  What
 // stands against more is issue (the same launch on zeros, at the full clock, takes 380 us) and then power; arrangements
 // with fewer vector instructions, phases of the two wavefronts of a SIMD against each other or a barrier for every two
 // tiles, with four buffers, came out the same.  Scores scaled before the exponent instead of under the products with the
-// values: 484 us, not 476.  Tiles
-// straight to LDS and eight wavefronts on them instead of four with loads through registers: 532 us, not 600.
-// Chunks with a window of 1024 (G = 8): 210 us, 0.81 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
-// outputs, whose traffic nothing else overlaps.  17 tokens behind 30011 rows for each of two sequences: 47 us, 224 MB
-// at 4.8 TB/s.
+// values: 484 us, not 476.  Tiles straight to LDS and eight wavefronts on them instead of four with loads through
+// registers: 532 us, not 600.
+// Chunks with a window of 1024 (G = 8): 205 to 210 us, 0.82 PFLOP/s; some 6 us of the 42 of a workgroup go to queries and
+// outputs, whose traffic nothing else overlaps.  17 tokens behind 30011 rows for each of two sequences: 43.5 us in a graph,
+// 39.8 for the 224 MB of the pieces (5.6 TB/s), then their join.
+// How the work is cut leaves much of the chip idle between few and many blocks, see prompt_most_pieces.
 #include <float.h>
 
 #include "paged.hpp"
@@ -695,11 +697,15 @@ void launch_join(int G, unsigned blocks, const PromptArgs& a, hipStream_t st) {
   }
 }
 
-// Blocks there can be: one of each sequence may be short.
+// At least the blocks there can be, as one of each sequence may be short; one more than there are where all are whole.
 int64_t prompt_blocks(const Dims& dm, int64_t n_rows) {
   return n_rows / (PR_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S);
 }
-// Workgroups that may share the tiles of a block: one workgroup fills a compute unit.
+// Workgroups that may share the tiles of a block: one workgroup fills a compute unit.  Every block gets as many, by the
+// bound above and by whole numbers, so that from 33 to 255 workgroups' worth of blocks part of the chip stays idle, and just
+// above 256 a second round runs with few.  8 KV heads, G = 4, behind 30000 rows: 256 tokens 132 us, 512 253, 1024 (one piece,
+// 128 workgroups) 661, 1500 722, 2048 (256 workgroups) 897, 2112 1481; 16 ragged sequences of 8 tokens behind 113000
+// rows together, whose longest has 30000, 417 us where the bytes take 70.
 int prompt_most_pieces(const Dims& dm, int64_t n_rows) {
   const int64_t groups = prompt_blocks(dm, n_rows) * dm.Hkv;
   return groups >= PR_CUS ? 1 : (int)(PR_CUS / groups);
@@ -708,7 +714,8 @@ int prompt_most_pieces(const Dims& dm, int64_t n_rows) {
 // their join costs, a launch and 1 KB of partial results a query row, written and read.  Cut and not, in us, of one
 // sequence with 8 KV heads, G = 4: 17 tokens behind 250 rows 11.0 / 10.1, 500 11.0 / 14.2, 4000 14.1 / 66.9; 100 tokens
 // behind 200 rows 14.9 / 12.1, 400 14.3 / 16.6; 700 behind 1000 31.9 / 30.0, 1500 37.9 / 41.0, 3000 53.6 / 73.4; all of
-// 1000 34.5 / 28.8.  The rule takes the smaller of every pair.
+// 1000 34.5 / 28.8.  The rule takes the smaller of every pair where the table is as wide as the longest sequence: the host knows
+// the width only, and takes it for the lengths.
 int prompt_split(const Dims& dm, int64_t n_rows, int64_t tiles) {
   const int64_t most = prompt_most_pieces(dm, n_rows);
   const int64_t pieces = most < tiles / PR_MIN_TILES ? most : tiles / PR_MIN_TILES;
