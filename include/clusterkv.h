@@ -81,6 +81,8 @@ extern "C" {
 #define CK_WS_OBJECTIVE 2
 #define CK_WS_PAGED_ATTN 3
 #define CK_WS_PROMPT_ATTN 4
+#define CK_WS_SHARED_ATTN 5
+#define CK_WS_CROSS_ATTN 6
 
 /* kind argument of ck_rope_frequencies */
 #define CK_ROPE_PLAIN 0
@@ -116,6 +118,8 @@ const char* ck_last_error_detail(void);
  *                       (budget + n_sink + recent window), c ignored.
  *   CK_WS_PAGED_ATTN:   n and c ignored: enough for every list, window and lengths.
  *   CK_WS_PROMPT_ATTN:  n = n_rows of ck_prompt_attn, c ignored; enough for fewer rows too.
+ *   CK_WS_SHARED_ATTN:  n and c ignored: enough for all groups and lengths.
+ *   CK_WS_CROSS_ATTN:   n = n_rows of ck_cross_attn, c ignored; enough for fewer rows too.
  * Returns 0 for an invalid request.
  */
 size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c);
@@ -636,6 +640,79 @@ int ck_prompt_attn(const ck_shape* sh, const void* q, int64_t n_rows, const int3
 int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* dst,
                  const int32_t* n_copy, int32_t max_rows, const int32_t* row_idx,
                  int32_t idx_stride, const int32_t* begin, const int32_t* src_seq, void* stream);
+
+/*
+ * Page tables, reference counts and the slots of new rows from the requests of a batch, on the device: nothing has
+ * to come back to the host between the steps of a server, and a captured call is replayed with other requests.
+ * n_new      [dev] int32 [S]: tokens that a sequence gets, or, negative, that are taken back (at most all: INT32_MIN
+ *            ends a sequence).
+ * lengths    [dev] int32 [S] in/out: rows of every sequence, afterwards with the new tokens.
+ * page_table [dev] int32 [S, pages_per_seq] in/out, page_refs [dev] int32 [n_pages] in/out: how many entries
+ *            of tables name a page; 0: the page is free.  Pages that the caller keeps for other uses have a count too.
+ * parent, shared_rows [dev] int32 [S], both NULL: nobody has a parent.  A sequence that has no rows, does not
+ *            take any back and whose parent is a sequence in [0, S) takes over the whole pages among the first
+ *            shared_rows[s] rows of the parent, as the parent stands before the call: their entries, counted once more, and
+ *            their rows.  Its new tokens come behind them.  What is left of shared_rows is the caller's to compute again.
+ * Then pages of sequences that take tokens back and hold no row any more are given back (entry -1, counted once less), and
+ * every entry from ceil(rows / page_size) on that the new tokens need gets a free page, with count 1: the free pages
+ * in ascending order, sequence by sequence and entry by entry.  Pages given back in the call can be given out in it.
+ * q_starts   [dev] int32 [S + 1] out: prefix sums of the new tokens (none where n_new is negative).
+ * slots      [dev] int32 [n_rows] out, NULL with n_rows = 0: of row t of the batch, page * page_size + row in the
+ *            page; -1 for a row on no page and from q_starts[S] on.
+ * lacking    [dev] int32 [1] out: pages that could not be given, as none was free (entry -1) or the table has no entry.
+ *            Lengths grow all the same: rows on no page are not stored and not attended.
+ * Only sh->S counts, S <= 8192; the sums of new tokens and of a sequence's rows have to stay below 2^31.  A page that
+ * others refer to too must not get rows: share whole pages, as a parent's are, and ck_copy_rows for the rest.
+ */
+int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, int32_t* page_table,
+                  int32_t pages_per_seq, int32_t* page_refs, int32_t n_pages, int32_t page_size,
+                  const int32_t* parent, const int32_t* shared_rows, int32_t* q_starts, int32_t* slots,
+                  int64_t n_rows, int32_t* lacking, void* stream);
+
+/*
+ * Rows of keys and values to their slots, as they are (an encoder's states; rows whose positions are not rotary):
+ * for every t < n_rows with slot p = slots[t] in [0, n_pages * page_size) and every KV head h
+ *   K[p / page_size][h][p % page_size] := k[t][h],  V likewise.
+ * k, v, k_stride, v_stride  as in ck_rope_append.
+ * slots     [dev] int32 [n_rows], as ck_plan_pages writes them; two rows must not have one slot.
+ * Of kv the pool counts, the table does not.
+ */
+int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                  int64_t n_rows, const int32_t* slots, const ck_paged_kv* kv, void* stream);
+
+/*
+ * ck_paged_decode_attn over every row (window < 0) for a batch in which sequences of a group begin with the
+ * same rows, which are read once for the group: one token per sequence, q, out [S, Hq, d], not the same buffer.
+ * group_starts [dev] int32 [n_groups + 1] ascending, n_groups <= S: group g is sequences [group_starts[g],
+ *              group_starts[g + 1]).  Sequences before the first and behind the last group share nothing.
+ * shared_rows  [dev] int32 [S]: the first shared_rows[s] rows of sequence s are those of the first sequence of its
+ *              group too, through whose table they are read; that one's own number is the largest of the group.
+ *              Any numbers, also within a page; taken as at least 0 and at most lengths[s].
+ * workspace    ck_workspace_bytes(sh, CK_WS_SHARED_ATTN, 0, 0); calls that share one must be ordered (its contents
+ *              on entry do not matter).
+ * CK_BF16: products as in ck_prompt_attn.  CK_F32 (check mode): every sequence reads its own table.
+ * Lengths, groups and tables are read on the device: a captured call may be replayed with others.  The order of the
+ * sums depends on the lengths of the whole batch.
+ */
+int ck_shared_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* kv,
+                          const int32_t* lengths, int32_t n_groups, const int32_t* group_starts,
+                          const int32_t* shared_rows, float softmax_scale, void* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Cross attention: GQA attention of tokens to all rows [0, lengths[s]) of a cache of another length, an encoder's
+ * states, without a causal order.  No row at all gives zeros.
+ * q, out    [dev] [n_rows, Hq, d], not the same buffer.
+ * q_starts  [dev] int32 [S + 1], as in ck_prompt_attn, but lengths do not count the new tokens; queries that attend to the same
+ *           states (beams) can be one sequence's.  NULL: n_rows == S, one token per sequence, bf16 or fp32.
+ *           With q_starts CK_BF16 only, products as in ck_prompt_attn.
+ * workspace ck_workspace_bytes(sh, CK_WS_CROSS_ATTN, n, 0) with n >= n_rows; calls that share one must be ordered (its
+ *           contents on entry do not matter).
+ * Captured calls and the order of sums as in ck_shared_decode_attn.
+ */
+int ck_cross_attn(const ck_shape* sh, const void* q, int64_t n_rows, const int32_t* q_starts,
+                  const ck_paged_kv* kv, const int32_t* lengths, float softmax_scale, void* out,
+                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid, not part of the method: a register-only loop of

@@ -2,8 +2,8 @@
 
 Every step of the path (K-means assignment/update, metadata, cluster selection,
 index gather, sparse decode attention), and of what stands beside it on caches in
-pages (rotary append, prompt and one-token attention, row copies), runs in the HIP
-kernels of the C-ABI library declared in include/clusterkv.h.  This package only marshals torch
+pages (page plans, rotary append, rows into slots, prompt and one-token attention, shared
+prefixes, cross attention, row copies), runs in the HIP kernels of the C-ABI library declared in include/clusterkv.h.  This package only marshals torch
 tensors (device memory, current stream) into those calls.  There is no CPU or
 PyTorch fallback: a missing library is an error.
 """
@@ -19,7 +19,9 @@ from .binding import (CK_BF16, CK_F32, CK_KM_UNTIL_CONVERGED, CK_METRIC_COSINE, 
                       ck_sparse_decode_attn_static, ck_token_scores,
                       ck_topk_select, ck_version, ck_workspace_bytes, decode_step, load_library,
                       ck_copy_rows, ck_paged_decode_attn, ck_prompt_attn, ck_rope_append,
-                      ck_rope_frequencies, paged_decode_workspace, prompt_workspace)
+                      ck_rope_frequencies, paged_decode_workspace, prompt_workspace,
+                      ck_cross_attn, ck_plan_pages, ck_shared_decode_attn, ck_store_rows,
+                      cross_workspace, shared_decode_workspace)
 from .driver import LayerStack
 
 __all__ = [
@@ -35,5 +37,7 @@ __all__ = [
     "CK_ROPE_BANDS", "CK_ROPE_BASE", "CK_ROPE_LINEAR", "CK_ROPE_PLAIN", "CK_ROPE_RAMP", "PagedKV",
     "ck_copy_rows", "ck_paged_decode_attn", "ck_prompt_attn", "ck_rope_append",
     "ck_rope_frequencies", "paged_decode_workspace", "prompt_workspace",
+    "ck_cross_attn", "ck_plan_pages", "ck_shared_decode_attn", "ck_store_rows",
+    "cross_workspace", "shared_decode_workspace",
     "ck_topk_select", "ck_version", "ck_workspace_bytes", "decode_step", "load_library",
 ]

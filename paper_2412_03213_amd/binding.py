@@ -19,6 +19,7 @@ CK_SEL_WHOLE, CK_SEL_TRIM_LAST = 0, 1
 CK_MAX_CLUSTERS = 2048
 CK_METRIC_COSINE, CK_METRIC_L2, CK_METRIC_IP, CK_KM_UNTIL_CONVERGED = 0, 1, 2, 4
 CK_WS_CLUSTER_KEYS, CK_WS_SPARSE_ATTN, CK_WS_OBJECTIVE, CK_WS_PAGED_ATTN, CK_WS_PROMPT_ATTN = 0, 1, 2, 3, 4
+CK_WS_SHARED_ATTN, CK_WS_CROSS_ATTN = 5, 6
 CK_ROPE_PLAIN, CK_ROPE_LINEAR, CK_ROPE_BASE, CK_ROPE_RAMP, CK_ROPE_BANDS = 0, 1, 2, 3, 4
 CK_ROPE_HALVES, CK_ROPE_ADJACENT = 0, 1
 
@@ -31,7 +32,8 @@ EXPORTS = ("ck_version", "ck_strerror", "ck_last_error_detail", "ck_workspace_by
            "ck_full_decode_attn", "ck_token_scores", "ck_topk_select", "ck_recall_hits",
            "ck_page_keys", "ck_expand_pages", "ck_host_device_ptr", "ck_cache_reset",
            "ck_cached_decode_step", "ck_rope_frequencies", "ck_rope_append", "ck_paged_decode_attn",
-           "ck_prompt_attn", "ck_copy_rows", "ck_probe_mfma_bf16")
+           "ck_prompt_attn", "ck_copy_rows", "ck_plan_pages", "ck_store_rows",
+           "ck_shared_decode_attn", "ck_cross_attn", "ck_probe_mfma_bf16")
 
 
 class ClusterKVError(RuntimeError):
@@ -178,6 +180,14 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.ck_prompt_attn.argtypes = [SH, P, I64, P, KV, P, I64, I64, F, P, P, SZ, P]
     lib.ck_copy_rows.restype = ctypes.c_int
     lib.ck_copy_rows.argtypes = [SH, KV, KV, P, I32, P, I32, P, P, P]
+    lib.ck_plan_pages.restype = ctypes.c_int
+    lib.ck_plan_pages.argtypes = [SH, P, P, P, I32, P, I32, I32, P, P, P, P, I64, P, P]
+    lib.ck_store_rows.restype = ctypes.c_int
+    lib.ck_store_rows.argtypes = [SH, P, P, I64, I64, I64, P, KV, P]
+    lib.ck_shared_decode_attn.restype = ctypes.c_int
+    lib.ck_shared_decode_attn.argtypes = [SH, P, KV, P, I32, P, P, F, P, P, SZ, P]
+    lib.ck_cross_attn.restype = ctypes.c_int
+    lib.ck_cross_attn.argtypes = [SH, P, I64, P, KV, P, F, P, P, SZ, P]
     lib.ck_probe_mfma_bf16.restype = ctypes.c_int
     lib.ck_probe_mfma_bf16.argtypes = [I32, I32, P, P, P, ctypes.POINTER(ctypes.c_double), P]
     lib.host_decode_step = _host_decode_step()
@@ -729,6 +739,85 @@ def ck_copy_rows(sh: Shape, src, dst, n_copy, max_rows: int, row_idx=None, begin
                             _ints(row_idx, "row_idx", (sh.S, sh.Hkv, stride), dev), stride,
                             _ints(begin, "begin", per_seq, dev),
                             _ints(src_seq, "src_seq", per_seq, dev), stream))
+
+
+def ck_plan_pages(sh: Shape, n_new, lengths, page_table, page_refs, page_size: int, q_starts, lacking,
+                  slots=None, parent=None, shared_rows=None):
+    """lengths, page_table [S, pages_per_seq] (a PagedKV's among them) and page_refs [n_pages] change in
+    place; q_starts, lacking [1] and slots (None: not asked for) are written."""
+    lib = load_library()
+    dev, stream = _device(n_new), _stream(n_new)
+    if not all(isinstance(t, torch.Tensor) and t.dim() == d for t, d in ((page_table, 2), (page_refs, 1))):
+        raise ValueError("page_table must be int32 [S, pages_per_seq], page_refs int32 [n_pages]")
+    width, pages, n = page_table.shape[1], page_refs.shape[0], 0 if slots is None else slots.shape[0]
+    per_seq = (sh.S,)
+    _check(lib.ck_plan_pages(ctypes.byref(sh.c()), _ints(n_new, "n_new", per_seq, dev),
+                             _ints(lengths, "lengths", per_seq, dev),
+                             _ints(page_table, "page_table", (sh.S, width), dev), width,
+                             _ints(page_refs, "page_refs", (pages,), dev), pages, page_size,
+                             _ints(parent, "parent", per_seq, dev),
+                             _ints(shared_rows, "shared_rows", per_seq, dev),
+                             _ints(q_starts, "q_starts", (sh.S + 1,), dev),
+                             _ints(slots, "slots", (n,), dev) if n else None, n,
+                             _ints(lacking, "lacking", (1,), dev), stream))
+
+
+def ck_store_rows(sh: Shape, k, v, slots, kv):
+    """k, v: token rows [n, Hkv, d], views of one projection's output among them; slots int32 [n]."""
+    lib = load_library()
+    dev, stream = _device(k), _stream(k)
+    n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
+    kp, ks = _rows(k, "k", n, sh.Hkv, sh, dev)
+    vp, vs = _rows(v, "v", n, sh.Hkv, sh, dev)
+    _check(lib.ck_store_rows(ctypes.byref(sh.c()), kp, vp, ks, vs, n, _ints(slots, "slots", (n,), dev),
+                             _kv(sh, kv, dev), stream))
+
+
+def shared_decode_workspace(sh: Shape, device) -> torch.Tensor:
+    """Scratch of ck_shared_decode_attn, whatever its groups and lengths."""
+    return torch.empty(max(256, ck_workspace_bytes(sh, CK_WS_SHARED_ATTN, 0)), dtype=torch.uint8,
+                       device=device)
+
+
+def cross_workspace(sh: Shape, n_rows: int, device) -> torch.Tensor:
+    """Scratch of ck_cross_attn for up to n_rows token rows."""
+    return torch.empty(max(256, ck_workspace_bytes(sh, CK_WS_CROSS_ATTN, n_rows)), dtype=torch.uint8,
+                       device=device)
+
+
+def ck_shared_decode_attn(sh: Shape, q, kv, lengths, group_starts, shared_rows, out, softmax_scale=None,
+                          workspace=None):
+    lib = load_library()
+    if softmax_scale is None:
+        softmax_scale = sh.d ** -0.5
+    if workspace is None:
+        workspace = shared_decode_workspace(sh, q.device)
+    dev, stream = _device(q), _stream(q)
+    groups = group_starts.shape[0] - 1 if isinstance(group_starts, torch.Tensor) else 1
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(lib.ck_shared_decode_attn(ctypes.byref(sh.c()), _dense(q, "q", sh.S, sh, dev), _kv(sh, kv, dev),
+                                     _ints(lengths, "lengths", (sh.S,), dev), groups,
+                                     _ints(group_starts, "group_starts", (groups + 1,), dev),
+                                     _ints(shared_rows, "shared_rows", (sh.S,), dev), softmax_scale,
+                                     _dense(out, "out", sh.S, sh, dev), ws, ws_bytes, stream))
+    return workspace
+
+
+def ck_cross_attn(sh: Shape, q, q_starts, kv, lengths, out, softmax_scale=None, workspace=None):
+    """q_starts None: one token for each sequence."""
+    lib = load_library()
+    if softmax_scale is None:
+        softmax_scale = sh.d ** -0.5
+    n = q.shape[0] if isinstance(q, torch.Tensor) else sh.S
+    if workspace is None:
+        workspace = cross_workspace(sh, n, q.device)
+    dev, stream = _device(q), _stream(q)
+    ws, ws_bytes = _scratch(workspace, dev)
+    _check(lib.ck_cross_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh, dev), n,
+                             _ints(q_starts, "q_starts", (sh.S + 1,), dev), _kv(sh, kv, dev),
+                             _ints(lengths, "lengths", (sh.S,), dev), softmax_scale,
+                             _dense(out, "out", n, sh, dev), ws, ws_bytes, stream))
+    return workspace
 
 
 def _probe_operands(t):

@@ -26,6 +26,7 @@ SOURCES = ["api.hip", "kmeans_assign.hip", "kmeans_assign_stream.hip", "kmeans_a
            "kmeans_update.hip", "kmeans_small.hip", "select_gather.hip",
            "sparse_attn.hip", "evaluate.hip", "cluster_cache.hip",
            "rope_append.hip", "copy_rows.hip", "paged_attn.hip", "prompt_attn.hip",
+           "plan_pages.hip", "store_rows.hip", "segment_attn.hip",
            "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")

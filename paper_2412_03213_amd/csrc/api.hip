@@ -74,6 +74,24 @@ int check_ranges(const ck_shape* sh, int64_t tok_begin, int64_t tok_count, int32
   return CK_OK;
 }
 
+// The calls that fall back on the attention of single tokens take its workspace, for their callers' convenience under
+// one name.
+size_t shared_bytes(const ck::Dims& dm) {
+  const size_t single = ck::paged_workspace_bytes(dm), all = ck::shared_workspace_bytes(dm);
+  return dm.dtype == CK_BF16 && all > single ? all : single;
+}
+size_t cross_bytes(const ck::Dims& dm, int64_t n_rows) {
+  const size_t single = ck::paged_workspace_bytes(dm), all = ck::cross_workspace_bytes(dm, n_rows);
+  return dm.dtype == CK_BF16 && all > single ? all : single;
+}
+
+int check_workspace(const void* workspace, size_t bytes, size_t need) {
+  if (!workspace) return fail(CK_EWORKSPACE, "workspace is NULL");
+  if (!aligned16(workspace)) return fail(CK_EMISALIGNED, "workspace is not 16-byte aligned");
+  if (bytes < need) return fail(CK_EWORKSPACE, "workspace has %zu bytes, %zu needed", bytes, need);
+  return CK_OK;
+}
+
 int hip_result(hipError_t e, const char* what) {
   if (e == hipSuccess) return CK_OK;
   return fail(CK_EHIP, "%s: %s", what, hipGetErrorString(e));
@@ -118,6 +136,11 @@ size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c) {
   if (which == CK_WS_PROMPT_ATTN) {
     if (n < 1 || n > ck::MAX_NEW_ROWS) return 0;
     return ck::prompt_workspace_limit(dm);
+  }
+  if (which == CK_WS_SHARED_ATTN) return shared_bytes(dm);
+  if (which == CK_WS_CROSS_ATTN) {
+    if (n < 1 || n > ck::MAX_NEW_ROWS) return 0;
+    return cross_bytes(dm, n);
   }
   return 0;
 }
@@ -1001,6 +1024,112 @@ int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* 
   return hip_result(ck::launch_copy_rows(dm, *src, *dst, n_copy, max_rows, row_idx, idx_stride, begin, src_seq,
                                          (hipStream_t)stream),
                     "row copy launch");
+}
+
+int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, int32_t* page_table,
+                  int32_t pages_per_seq, int32_t* page_refs, int32_t n_pages, int32_t page_size,
+                  const int32_t* parent, const int32_t* shared_rows, int32_t* q_starts, int32_t* slots,
+                  int64_t n_rows, int32_t* lacking, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (sh->S > ck::MAX_PLANNED)
+    return fail(CK_EUNSUPPORTED, "%d sequences (at most %d)", sh->S, ck::MAX_PLANNED);
+  if (pages_per_seq < 1 || n_pages < 1 || page_size < 1)
+    return fail(CK_EINVALID, "pages_per_seq, n_pages and page_size must be positive");
+  if ((int64_t)page_size * pages_per_seq > (int64_t)1 << 30)
+    return fail(CK_EUNSUPPORTED, "more than 2^30 rows of a sequence");
+  if ((int64_t)sh->S * pages_per_seq > 0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "more than 2^31 - 1 entries in the table");
+  if ((int64_t)n_pages * page_size > 0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "more than 2^31 - 1 slots in the pool");
+  if (!parent != !shared_rows) return fail(CK_EINVALID, "parent and shared_rows must be given together");
+  if (n_rows < 0) return fail(CK_EINVALID, "n_rows=%lld is negative", (long long)n_rows);
+  if (n_rows > ck::MAX_NEW_ROWS)
+    return fail(CK_EUNSUPPORTED, "n_rows=%lld (at most %lld)", (long long)n_rows, (long long)ck::MAX_NEW_ROWS);
+  if (!slots != (n_rows == 0)) return fail(CK_EINVALID, "slots and n_rows must be given together");
+  CK_REQUIRE_PTR(n_new);
+  CK_REQUIRE_PTR(lengths);
+  CK_REQUIRE_PTR(page_table);
+  CK_REQUIRE_PTR(page_refs);
+  CK_OPTIONAL_PTR(parent);
+  CK_OPTIONAL_PTR(shared_rows);
+  CK_REQUIRE_PTR(q_starts);
+  CK_OPTIONAL_PTR(slots);
+  CK_REQUIRE_PTR(lacking);
+  return hip_result(ck::launch_plan_pages(sh->S, n_new, lengths, page_table, pages_per_seq, page_refs, n_pages, page_size,
+                                          parent, shared_rows, q_starts, slots, n_rows, lacking, (hipStream_t)stream),
+                    "page plan launch");
+}
+
+int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                  int64_t n_rows, const int32_t* slots, const ck_paged_kv* kv, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if ((rc = check_rows(n_rows))) return rc;
+  if (n_rows * dm.Hkv > (int64_t)1 << 26) return fail(CK_EUNSUPPORTED, "more than 2^26 rows of heads in one call");
+  if ((rc = check_token_rows("k", k, k_stride, dm.Hkv, dm))) return rc;
+  if ((rc = check_token_rows("v", v, v_stride, dm.Hkv, dm))) return rc;
+  CK_REQUIRE_PTR(slots);
+  if ((rc = check_paged(kv, "kv", dm, 1))) return rc;
+  return hip_result(ck::launch_store_rows(dm, k, v, k_stride, v_stride, n_rows, slots, *kv, (hipStream_t)stream),
+                    "row store launch");
+}
+
+int ck_shared_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* kv,
+                          const int32_t* lengths, int32_t n_groups, const int32_t* group_starts,
+                          const int32_t* shared_rows, float softmax_scale, void* out, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (n_groups < 1 || n_groups > sh->S)
+    return fail(CK_EINVALID, "n_groups=%d outside [1, S=%d]", n_groups, sh->S);
+  if (!(softmax_scale > 0.f)) return fail(CK_EINVALID, "softmax_scale must be positive");
+  CK_REQUIRE_PTR(q);
+  CK_REQUIRE_PTR(lengths);
+  CK_REQUIRE_PTR(group_starts);
+  CK_REQUIRE_PTR(shared_rows);
+  CK_REQUIRE_PTR(out);
+  if (q == out) return fail(CK_EINVALID, "out is q");
+  if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, shared_bytes(dm)))) return rc;
+  if (dm.dtype != CK_BF16)                              // check mode: every sequence reads its own table
+    return hip_result(ck::launch_paged_attn(dm, q, *kv, lengths, 0, -1, nullptr, nullptr, 0, 0, softmax_scale, out,
+                                            workspace, (hipStream_t)stream),
+                      "paged attention launch");
+  return hip_result(ck::launch_shared_attn(dm, q, *kv, lengths, n_groups, group_starts, shared_rows, softmax_scale,
+                                           out, workspace, (hipStream_t)stream),
+                    "shared attention launch");
+}
+
+int ck_cross_attn(const ck_shape* sh, const void* q, int64_t n_rows, const int32_t* q_starts,
+                  const ck_paged_kv* kv, const int32_t* lengths, float softmax_scale, void* out,
+                  void* workspace, size_t workspace_bytes, void* stream) {
+  ck::Dims dm;
+  int rc = check_shape(sh, &dm, false);
+  if (rc) return rc;
+  if (q_starts && dm.dtype != CK_BF16)
+    return fail(CK_EUNSUPPORTED, "cross attention of several tokens runs on bf16 only");
+  if ((rc = check_rows(n_rows))) return rc;
+  if (!q_starts && n_rows != sh->S)
+    return fail(CK_EINVALID, "n_rows=%lld without q_starts: one token for each of the %d sequences",
+                (long long)n_rows, sh->S);
+  if (n_rows * dm.Hq > (int64_t)1 << 30) return fail(CK_EUNSUPPORTED, "more than 2^30 query rows in one call");
+  if (!(softmax_scale > 0.f)) return fail(CK_EINVALID, "softmax_scale must be positive");
+  CK_REQUIRE_PTR(q);
+  CK_OPTIONAL_PTR(q_starts);
+  CK_REQUIRE_PTR(lengths);
+  CK_REQUIRE_PTR(out);
+  if (q == out) return fail(CK_EINVALID, "out is q");
+  if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
+  if ((rc = check_workspace(workspace, workspace_bytes, cross_bytes(dm, n_rows)))) return rc;
+  if (!q_starts)
+    return hip_result(ck::launch_paged_attn(dm, q, *kv, lengths, 0, -1, nullptr, nullptr, 0, 0, softmax_scale, out,
+                                            workspace, (hipStream_t)stream),
+                      "paged attention launch");
+  return hip_result(ck::launch_cross_attn(dm, q, n_rows, q_starts, *kv, lengths, softmax_scale, out, workspace,
+                                          (hipStream_t)stream),
+                    "cross attention launch");
 }
 
 int ck_probe_mfma_bf16(int32_t n_workgroups, int32_t iters, const void* operands,

@@ -395,6 +395,21 @@ hipError_t launch_paged_attn(const Dims& dm, const void* q, const ck_paged_kv& k
                              int64_t n_sink, int64_t window, const int32_t* token_idx, const int32_t* n_tokens,
                              int idx_stride, int max_tokens, float softmax_scale, void* out, void* workspace,
                              hipStream_t st);
+hipError_t launch_store_rows(const Dims& dm, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                             int64_t n_rows, const int32_t* slots, const ck_paged_kv& kv, hipStream_t st);
+constexpr int MAX_PLANNED = 8192;            // sequences of ck_plan_pages
+hipError_t launch_plan_pages(int S, const int32_t* n_new, int32_t* lengths, int32_t* page_table, int pages_per_seq,
+                             int32_t* page_refs, int n_pages, int page_size, const int32_t* parent,
+                             const int32_t* shared_rows, int32_t* q_starts, int32_t* slots, int64_t n_rows,
+                             int32_t* lacking, hipStream_t st);
+size_t cross_workspace_bytes(const Dims& dm, int64_t n_rows);
+hipError_t launch_cross_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
+                             const ck_paged_kv& kv, const int32_t* lengths, float softmax_scale, void* out,
+                             void* workspace, hipStream_t st);
+size_t shared_workspace_bytes(const Dims& dm);
+hipError_t launch_shared_attn(const Dims& dm, const void* q, const ck_paged_kv& kv, const int32_t* lengths,
+                              int n_groups, const int32_t* group_starts, const int32_t* shared_rows,
+                              float softmax_scale, void* out, void* workspace, hipStream_t st);
 size_t prompt_workspace_bytes(const Dims& dm, int64_t n_rows);   // of a call
 size_t prompt_workspace_limit(const Dims& dm);                   // of any call
 hipError_t launch_prompt_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
