@@ -661,7 +661,7 @@ int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* 
  *            page; -1 for a row on no page and from q_starts[S] on.
  * lacking    [dev] int32 [1] out: pages that could not be given, as none was free (entry -1) or the table has no entry.
  *            Lengths grow all the same: rows on no page are not stored and not attended.
- * Only sh->S counts, S <= 8192; the sums of new tokens and of a sequence's rows have to stay below 2^31.  A page that
+ * Only sh->S counts, S <= 8192; n_pages <= 2^30; the sums of new tokens and of a sequence's rows have to stay below 2^31.  A page that
  * others refer to too must not get rows: share whole pages, as a parent's are, and ck_copy_rows for the rest.
  */
 int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, int32_t* page_table,

@@ -1041,6 +1041,7 @@ int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, in
     return fail(CK_EUNSUPPORTED, "more than 2^30 rows of a sequence");
   if ((int64_t)sh->S * pages_per_seq > 0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "more than 2^31 - 1 entries in the table");
   if ((int64_t)n_pages * page_size > 0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "more than 2^31 - 1 slots in the pool");
+  if (n_pages > 1 << 30) return fail(CK_EUNSUPPORTED, "n_pages=%d (at most 2^30)", n_pages);
   if (!parent != !shared_rows) return fail(CK_EINVALID, "parent and shared_rows must be given together");
   if (n_rows < 0) return fail(CK_EINVALID, "n_rows=%lld is negative", (long long)n_rows);
   if (n_rows > ck::MAX_NEW_ROWS)

@@ -14,10 +14,11 @@ namespace ck {
 namespace {
 
 constexpr int PL_THREADS = 1024, PL_WAVES = PL_THREADS / 64;
-constexpr int PL_LOADS = 32;                            // of 4 counts a lane, for the pages that are looked at together
+constexpr int PL_LOADS = 32, PL_FIRST_LOADS = 8;        // of 4 counts a lane, for the pages that are looked at together
+constexpr int PL_ITEMS = 4;                             // of a thread at a time
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
 constexpr int PL_OWN_ROWS = 8192;
-constexpr int PL_SLOT_ROWS = 4096;                      // of a workgroup of that launch
+constexpr int PL_SLOT_ROWS = PL_THREADS;                // of a workgroup of that launch
 
 struct PlanArgs {
   const int32_t *n_new, *parent, *shared_rows;
@@ -52,16 +53,23 @@ __device__ __forceinline__ void scan_two(int& x, int& y, int& x_before, int& y_b
   y_before = all.y;
 }
 
-// The first i of [0, n) with upto[i] > x (n - 1 if there is none); upto ascends.
+// The first i of [0, n) with upto[i] > x (n - 1 if there is none), for several x at a time; upto ascends.
+template <int N>
+__device__ __forceinline__ void first_beyond(const int* upto, int n, const int (&x)[N], int (&i)[N]) {
+#pragma unroll
+  for (int u = 0; u < N; ++u) i[u] = 0;
+  for (int b = 1 << (31 - __builtin_clz(n)); b; b >>= 1)
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int k = i[u] + b;
+      i[u] = upto[min(k, n) - 1] <= x[u] && k < n ? k : i[u];
+    }
+}
 __device__ __forceinline__ int first_beyond(const int* upto, int n, int x) {
-  int lo = 0, len = n - 1;                              // in [lo, lo + len]
-  while (len > 0) {
-    const int half = len >> 1;
-    const bool right = upto[lo + half] <= x;
-    lo = right ? lo + half + 1 : lo;
-    len = right ? len - half - 1 : half;
-  }
-  return lo;
+  const int one[1] = {x};
+  int i[1];
+  first_beyond<1>(upto, n, one, i);
+  return i[0];
 }
 
 // Slots of rows t, t + step, ..; ends: q_starts[s + 1] of every sequence.
@@ -95,19 +103,30 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   int* const rows = lds;                                // [S]: of every sequence, before it gives back or gets tokens
   int* const upto = lds + a.S;                          // [S]: prefix sums
   __shared__ int2 tmp[PL_WAVES];
+  __shared__ int free_upto[PL_LOADS * PL_WAVES];        // free pages of a run; then up to its end
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ps = (int)a.size.d;
   auto after = [&](int s, int n) {                      // rows of a sequence after the call
     const int64_t x = (int64_t)rows[s] + n;
     return (int)(x < 0 ? 0 : (x < 0x7FFFFFFF ? x : 0x7FFFFFFF));
   };
-  // items of all sequences, numbered through upto[]: f(sequence, item of it)
-  auto for_items = [&](int total, auto f) {
-    for (int r = tid; r < total; r += PL_THREADS) {
-      const int s = first_beyond(upto, a.S, r);
-      f(s, r - (s > 0 ? upto[s - 1] : 0));
+  // Items of all sequences, numbered through upto[]: get(sequence, item of it) asks for what put takes.  Several at a
+  // time: an item is a chain of look-ups, one after the other.
+  auto for_items = [&](int total, auto get, auto put) {
+    for (int r0 = tid; r0 < total; r0 += PL_ITEMS * PL_THREADS) {
+      decltype(get(0, 0)) x[PL_ITEMS];
+      int r[PL_ITEMS], s[PL_ITEMS];
+#pragma unroll
+      for (int u = 0; u < PL_ITEMS; ++u) r[u] = min(r0 + u * PL_THREADS, total - 1);   // the last one again behind the end
+      first_beyond<PL_ITEMS>(upto, a.S, r, s);
+#pragma unroll
+      for (int u = 0; u < PL_ITEMS; ++u) x[u] = get(s[u], r[u] - (s[u] > 0 ? upto[s[u] - 1] : 0));
+#pragma unroll
+      for (int u = 0; u < PL_ITEMS; ++u)
+        if (r0 + u * PL_THREADS < total) put(x[u]);
     }
   };
+  struct Entry { int32_t* at; int page; };
 
   // ---- sequences without rows take over whole pages of a parent, as it stands before the call ----
   int taken = 0, unused = 0, less = 0;
@@ -133,12 +152,15 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   }
   less = __syncthreads_or(less);
   if (taken > 0) {
-    for_items(taken, [&](int s, int e) {
-      const int page = a.table[(int64_t)a.parent[s] * a.per_seq + e];
-      const bool is = a.is_page(page);
-      a.table[(int64_t)s * a.per_seq + e] = is ? page : -1;
-      if (is) atomicAdd(a.refs + page, 1);
-    });
+    for_items(taken,
+              [&](int s, int e) -> Entry {
+                return {a.table + (int64_t)s * a.per_seq + e, a.table[(int64_t)a.parent[s] * a.per_seq + e]};
+              },
+              [&](const Entry& x) {
+                const bool is = a.is_page(x.page);
+                *x.at = is ? x.page : -1;
+                if (is) atomicAdd(a.refs + x.page, 1);
+              });
     memory_barrier();
   }
 
@@ -154,12 +176,15 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       if (s < a.S) upto[s] = n;
     }
     __syncthreads();
-    for_items(given, [&](int s, int i) {
-      int32_t* entry = a.table + (int64_t)s * a.per_seq + a.pages_of(after(s, a.n_new[s])) + i;
-      const int page = *entry;
-      *entry = -1;
-      if (a.is_page(page)) atomicAdd(a.refs + page, -1);
-    });
+    for_items(given,
+              [&](int s, int i) -> Entry {
+                int32_t* at = a.table + (int64_t)s * a.per_seq + a.pages_of(after(s, a.n_new[s])) + i;
+                return {at, *at};
+              },
+              [&](const Entry& x) {
+                *x.at = -1;
+                if (a.is_page(x.page)) atomicAdd(a.refs + x.page, -1);
+              });
     memory_barrier();
   }
 
@@ -190,14 +215,14 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
     const int s = first_beyond(upto, a.S, r);
     return a.table + (int64_t)s * a.per_seq + a.pages_of(rows[s]) + (r - (s > 0 ? upto[s - 1] : 0));
   };
+  // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.  Few at first:
+  // most calls need few pages.
   int found = 0;                                        // free pages so far
-  constexpr int LOAD = WAVE * 4;                        // pages of a wavefront's load
-  for (int p0 = 0; p0 < a.n_pages && found < wanted; p0 += PL_WAVES * PL_LOADS * LOAD) {
-    const int left = (a.n_pages - p0 + LOAD - 1) / LOAD;
-    const int loads = min(PL_LOADS, (left + PL_WAVES - 1) / PL_WAVES);
-    const int first = p0 + wave * loads * LOAD + lane * 4;
+  constexpr int RUN = WAVE * 4;
+  int loads = PL_FIRST_LOADS;
+  for (int p0 = 0; p0 < a.n_pages && found < wanted; p0 += loads * PL_WAVES * RUN, loads = PL_LOADS) {
+    auto first_of = [&](int k) { return p0 + (k * PL_WAVES + wave) * RUN; };
     uint32_t bits[PL_LOADS / 8];                          // four pages of a load each
-    int n = 0, zero = 0;
 #pragma unroll
     for (int g = 0; g < PL_LOADS / 8; ++g) {
       bits[g] = 0;
@@ -205,47 +230,58 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       int4 c[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int p = first + (g * 8 + j) * LOAD;
+        const int p = first_of(g * 8 + j) + lane * 4;
         c[j] = make_int4(1, 1, 1, 1);
-        if (g * 8 + j < loads) {
-          if (p + 3 < a.n_pages) {
-            c[j] = *reinterpret_cast<const int4*>(a.refs + p);
-          } else {
-            if (p < a.n_pages) c[j].x = a.refs[p];
-            if (p + 1 < a.n_pages) c[j].y = a.refs[p + 1];
-            if (p + 2 < a.n_pages) c[j].z = a.refs[p + 2];
-          }
+        if (p + 3 < a.n_pages) {
+          c[j] = *reinterpret_cast<const int4*>(a.refs + p);
+        } else {
+          if (p < a.n_pages) c[j].x = a.refs[p];
+          if (p + 1 < a.n_pages) c[j].y = a.refs[p + 1];
+          if (p + 2 < a.n_pages) c[j].z = a.refs[p + 2];
         }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        bits[g] |= (uint32_t)((c[j].x == 0) | (c[j].y == 0) << 1 | (c[j].z == 0) << 2 | (c[j].w == 0) << 3) << (4 * j);
-      n += __popc(bits[g]);
+      for (int j = 0; j < 8; ++j) {
+        const bool f[4] = {c[j].x == 0, c[j].y == 0, c[j].z == 0, c[j].w == 0};
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          n += __popcll(__ballot(f[i]));
+          bits[g] |= (uint32_t)f[i] << (4 * j + i);
+        }
+        if (lane == 0) free_upto[(g * 8 + j) * PL_WAVES + wave] = n;
+      }
     }
-    int rank = n;
-    scan_two(rank, zero, found, unused, tmp);
-    rank = __builtin_amdgcn_readfirstlane(rank - n);    // of the wavefront's first free page
+    __syncthreads();
+    const bool mine = tid < loads * PL_WAVES;
+    int n = mine ? free_upto[tid] : 0, zero = 0;
+    scan_two(n, zero, found, unused, tmp);
+    if (mine) free_upto[tid] = n;
+    __syncthreads();
 #pragma unroll
     for (int g = 0; g < PL_LOADS / 8; ++g) {
+      if (g * 8 >= loads) continue;
 #pragma unroll 1
       for (int j = 0; j < 8; ++j) {
+        const int k = g * 8 + j;
         const uint32_t four = (bits[g] >> (4 * j)) & 15u;
-        if (__ballot(four != 0) == 0) continue;
-        const int c = __popc(four), upto_lane = wave_inclusive_scan(c);
-        int r = rank + upto_lane - c;
+        const int c = __popc(four), upto_lane = wave_inclusive_scan(c), all = __builtin_amdgcn_readlane(upto_lane, WAVE - 1);
+        int r = __builtin_amdgcn_readfirstlane(free_upto[k * PL_WAVES + wave]) - all;
+        if (all == 0 || r >= wanted) continue;          // wave-uniform
+        r += upto_lane - c;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (!((four >> i) & 1)) continue;
           if (r < wanted) {
-            const int p = first + (g * 8 + j) * LOAD + i;
+            const int p = first_of(k) + lane * 4 + i;
             a.refs[p] = 1;
             *entry_of(r) = p;
           }
           ++r;
         }
-        rank += __builtin_amdgcn_readlane(upto_lane, WAVE - 1);
       }
     }
+    __syncthreads();                                    // free_upto is read no more
   }
   for (int r = found + tid; r < wanted; r += PL_THREADS) *entry_of(r) = -1;
   int none = 0;

@@ -4,28 +4,53 @@
 //
 // A unit is a run of cache rows with the queries that see them: a segment with its states; a group of sequences with
 // its shared rows; a sequence with its own rows.  Its queries are cut into blocks of 256 (token, head of the group), its
-// rows into pieces of whole tiles.  The length of the pieces is found on the device, from all lengths of the ragged
-// batch, so that every compute unit gets as many tiles: a tile costs about the same where it is read from memory for
-// few queries and where 256 of them keep the matrix cores busy.  Pieces leave maximum, sum and accumulators in
-// fp32, which a second launch joins, in their order.
+// rows into pieces of whole tiles.  Three launches: one workgroup cuts the work, from all lengths of the ragged batch
+// (k_segment_plan); a workgroup for each piece, block and KV head (k_segment_attn), with up to 16 queries as in the attention of
+// single tokens (row_stream.hpp), with more as in that of prompts (attn_tiles.hpp), which leaves maximum, sum and
+// accumulators in fp32; and the pieces are joined in their order (k_segment_join).
 #include "attn_tiles.hpp"
+#include "row_stream.hpp"
 
 namespace ck {
 
 namespace {
 
-constexpr int SG_MIN_TILES = 2;                         // of a piece
 constexpr int SG_CUS = 256;                             // a workgroup fills a compute unit
-constexpr int SG_TRIES = 8;                             // times that the pieces are made longer by an eighth
+constexpr int SG_MIN_TILES = 2;                         // of a piece: 16 rows for each wavefront
+constexpr int SG_EXTRA = 512;                           // pieces that are more than blocks, over all heads, at most
+constexpr int SG_FEW = 16;                              // queries that stream rows instead of sharing tiles
 constexpr int SG_ROW = D + 4;                           // floats of a query row in a piece's results, see Partial
+constexpr int SG_PLAN_THREADS = 1024, SG_PLAN_WAVES = SG_PLAN_THREADS / 64;
+constexpr int SG_MODEL_UNITS = 2048;                    // units for which several cuts are compared
+constexpr int SG_CLASSES = 8;                           // of pieces, by how long they take
+
+// A piece of a block, as the planning workgroup hands it out.
+struct Piece {
+  int t0;                                               // rows [t0, t0 + n_tok) of q
+  short n_tok, flags;
+  int seq, lo, end;                                     // see rows [lo, end) of this sequence's cache
+  int row, n_tiles;                                     // of which the piece has n_tiles tiles from this row on
+  int result;                                           // row of results, over Hkv * G; -1: there is one piece, it writes the output
+  enum { SEVERAL = 1, LIMITED = 2 };                    // other blocks read the rows too; a query may see fewer rows
+};
+// Results to be joined: of the tokens of a block (cross attention) or of a unit.
+struct Whole {
+  int t0, n_tok, n_pieces;
+  int result, step;                                     // rows of results over Hkv * G: of the first piece, to the next
+  int pad[3];
+};
+struct Counts { int pieces, joins; };
 
 struct SegmentArgs {
   const bf16 *q, *K, *V;
   bf16* out;
+  Counts* counts;
+  Piece* pieces;
+  Whole* joins;                                         // blocks of several pieces, or units: groups, then sequences
   float* part;
   const int32_t *starts, *lengths, *shared;             // shared: only for groups of sequences
   Pages pages;
-  int S, n_segments, Hq, Hkv, n_rows, part_rows;
+  int S, n_segments, Hq, Hkv, n_rows, part_rows, most_pieces, most_joins;
   float scale_log2e;
 };
 
@@ -37,21 +62,16 @@ struct Unit {
   __device__ __forceinline__ int tiles() const { return lo < end ? (end - row0() + AT_TILE - 1) / AT_TILE : 0; }
 };
 
-// How the work of a call is cut; found by every wavefront for itself.
 template <int G, bool SHARED>
-struct Cut {
+struct Units {
   static constexpr int TOKENS = AT_ROWS / G;            // of a block
-  static constexpr int LISTS = SHARED ? 2 : 1;          // segments, then single sequences with rows of their own
   const SegmentArgs& a;
-  int length;                                           // tiles of a piece, at most
-  Unit held[LISTS];                                     // of the lists' first 64 units, one a lane
-
+  __device__ __forceinline__ int count() const { return a.n_segments + (SHARED ? a.S : 0); }
   __device__ __forceinline__ int bound(int t) const { return t < 0 ? 0 : (t < a.n_rows ? t : a.n_rows); }
-  __device__ __forceinline__ int count(int list) const { return list == 0 ? a.n_segments : a.S; }
-  __device__ __forceinline__ Unit load(int list, int i) const {
+  __device__ __forceinline__ Unit load(int i) const {
     Unit u = {0, 0, 0, 0, 0};
-    if (i >= count(list)) return u;
-    if (list == 0) {
+    if (i >= count()) return u;
+    if (i < a.n_segments) {
       u.begin = bound(a.starts[i]);
       u.tokens = max(0, bound(a.starts[i + 1]) - u.begin);
       u.seq = i;
@@ -63,6 +83,7 @@ struct Cut {
         u.end = a.pages.clamp_length(a.lengths[i]);
       }
     } else {
+      i -= a.n_segments;
       u.begin = u.seq = i;
       u.tokens = 1;
       u.end = a.pages.clamp_length(a.lengths[i]);
@@ -71,115 +92,237 @@ struct Cut {
     }
     return u;
   }
-  __device__ __forceinline__ Unit unit(int list, int i0) const {
-    return count(list) <= WAVE ? held[list] : load(list, i0 + (threadIdx.x & 63));
-  }
   __device__ __forceinline__ static int blocks(const Unit& u) { return (u.tokens + TOKENS - 1) / TOKENS; }
-  // of each block.  A segment without rows gets one, which writes zeros; where pieces are always joined, none.
-  __device__ __forceinline__ int pieces(const Unit& u) const {
-    const int n = (u.tiles() + length - 1) / length;
-    return SHARED ? n : max(n, 1);
-  }
-  // rows of results that the pieces of a unit leave, over Hkv * G
-  __device__ __forceinline__ int stored(const Unit& u) const {
-    const int n = pieces(u);
-    return SHARED || n > 1 ? n * u.tokens : 0;
-  }
-
-  __device__ __forceinline__ explicit Cut(const SegmentArgs& a_) : a(a_), length(1) {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    int all = 0;
-#pragma unroll
-    for (int list = 0; list < LISTS; ++list) {
-      held[list] = load(list, lane);
-      for (int i0 = 0; i0 < count(list); i0 += WAVE) {
-        const Unit u = unit(list, i0);
-        total += (int64_t)blocks(u) * u.tiles();
-        all += blocks(u);
-      }
-    }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-      total += __shfl_xor(total, o);
-      all += __shfl_xor(all, o);
-    }
-    const int64_t even = (total * a.Hkv + SG_CUS - 1) / SG_CUS;
-    length = __builtin_amdgcn_readfirstlane((int)(even < SG_MIN_TILES ? SG_MIN_TILES : (even < 1 << 24 ? even : 1 << 24)));
-    if (__builtin_amdgcn_readfirstlane(all) * a.Hkv > SG_CUS) return;
-    // Lengths that no piece divides make more pieces than fit, and the rest would run alone: longer ones then.
-    const int more = max(1, length / 8);
-    for (int tries = 0; tries < SG_TRIES; ++tries, length += more) {
-      int n = 0;
-#pragma unroll
-      for (int list = 0; list < LISTS; ++list)
-        for (int i0 = 0; i0 < count(list); i0 += WAVE) {
-          const Unit u = unit(list, i0);
-          n += blocks(u) * pieces(u);
-        }
-#pragma unroll
-      for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o);
-      if (__builtin_amdgcn_readfirstlane(n) * a.Hkv <= SG_CUS) break;
-    }
-  }
-
-  // A unit, its list, the rows of results before its own (over Hkv * G), and its pieces; rest: see find.
-  struct Place { Unit u; int list, rest, rows, n_pieces; };
-  __device__ __forceinline__ Place place(const Unit& u, int list, int lane, int rest, int rows) const {
-    auto get = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
-    const Unit one = {get(u.begin), get(u.tokens), get(u.seq), get(u.lo), get(u.end)};
-    return {one, list, rest, rows, pieces(one)};
-  }
-  // Of size(u) numbers for each unit, one after the other: the unit in which number x falls, and what is left of x there.
-  template <class Size>
-  __device__ __forceinline__ bool find(int x, Size size, Place* p) const {
-    int before = 0, rows = 0;
-#pragma unroll
-    for (int list = 0; list < LISTS; ++list)
-      for (int i0 = 0; i0 < count(list); i0 += WAVE) {
-        const Unit u = unit(list, i0);
-        const int n = size(u), upto = before + wave_inclusive_scan(n);
-        const int left = stored(u), left_upto = rows + wave_inclusive_scan(left);
-        const uint64_t beyond = __ballot(upto > x);
-        if (beyond) {
-          const int l = __builtin_ctzll(beyond);
-          const int rest = x - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
-          *p = place(u, list, l, rest, __builtin_amdgcn_readlane(left_upto, l) - __builtin_amdgcn_readlane(left, l));
-          return rest >= 0;
-        }
-        before = __builtin_amdgcn_readlane(upto, WAVE - 1);
-        rows = __builtin_amdgcn_readlane(left_upto, WAVE - 1);
-      }
-    return false;
-  }
-  // Unit i of a list.
-  __device__ __forceinline__ Place nth(int which, int i) const {
-    int rows = 0;
-    Place p = {};
-#pragma unroll
-    for (int list = 0; list < LISTS; ++list)
-      for (int i0 = 0; i0 < count(list) && list <= which; i0 += WAVE) {
-        const Unit u = unit(list, i0);
-        const int left = stored(u), left_upto = rows + wave_inclusive_scan(left);
-        if (list == which && i < i0 + WAVE) {
-          const int l = i - i0;
-          return place(u, list, l, 0, __builtin_amdgcn_readlane(left_upto, l) - __builtin_amdgcn_readlane(left, l));
-        }
-        rows = __builtin_amdgcn_readlane(left_upto, WAVE - 1);
-      }
-    return p;
-  }
 };
 
-// What a piece of a unit leaves for one KV head, of R = tokens * G query rows: maximum and sum of every row (and as
+// What the model below goes by, in microseconds.  A tile costs a workgroup 1.2 with up to two wavefronts of queries (its
+// share of the memory) and 0.18 more with each other one, 1.8 at most where other blocks read the same rows (from L2):
+// measured on 256 workgroups at 6400 and 3200 rows, 1.19 for 16, 32 and 64 queries, 1.35, 1.6, 1.85, 2.0, 2.2 and 2.15 for 96
+// to 256.  Beginning and end of a piece take 3; a row of results 0.05, written and read.
+__device__ __forceinline__ float tile_cost(int rows, int blocks) {
+  const float t = fmaf(0.18f, (float)max(0, (rows + 31) / 32 - 2), 1.2f);
+  return blocks > 1 ? fminf(t, 1.8f) : t;
+}
+constexpr float SG_PIECE_COST = 3.f, SG_ROW_COST = 0.05f;
+
+// Into how many pieces the rows of a unit are cut so that all work takes `within`, and how many compute units that takes.
+struct Choice { int pieces; float units; };
+template <bool SHARED>
+__device__ __forceinline__ Choice choose(int tiles, int blocks, int rows, int Hkv, float within) {
+  Choice best = {SHARED && tiles == 0 ? 0 : 1, 0.f};
+  if (blocks == 0 || tiles == 0) return best;
+  const float work = (float)tiles * tile_cost(rows, blocks), results = SG_ROW_COST * (float)rows;
+  const int most = max(1, tiles / SG_MIN_TILES);
+  const float whole = work + SG_PIECE_COST + (SHARED ? results : 0.f), room = within - SG_PIECE_COST - results;
+  int n = room > 0.f ? (int)fminf(ceilf(work * __builtin_amdgcn_rcpf(room)), (float)most) : most;
+  n = whole <= within ? 1 : max(1, n);
+  best = {most, 1e30f};
+#pragma unroll
+  for (int i = 0; i < 3; ++i, ++n) {
+    const float each = n == 1 ? whole : fmaf(work, __builtin_amdgcn_rcpf((float)n), SG_PIECE_COST + results);
+    const float fit = floorf(within * __builtin_amdgcn_rcpf(each));
+    const float units = fit >= 1.f ? (float)(n * blocks * Hkv) * __builtin_amdgcn_rcpf(fit) : 1e30f;
+    if (n <= most && units < best.units) best = {n, units};
+  }
+  return best;
+}
+
+// Inclusive prefix sums over the workgroup of three numbers a thread, with what earlier chunks left; tmp: LDS.
+__device__ __forceinline__ void scan_three(int (&x)[3], int (&before)[3], int4* tmp) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) x[k] = wave_inclusive_scan(x[k]);
+  __syncthreads();                                      // tmp may still be in use
+  if (lane == WAVE - 1) tmp[wave] = make_int4(x[0], x[1], x[2], 0);
+  __syncthreads();
+  int mine[3] = {before[0], before[1], before[2]};
+#pragma unroll
+  for (int w = 0; w < SG_PLAN_WAVES; ++w) {
+    const int4 t = tmp[w];
+    const int v[3] = {t.x, t.y, t.z};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      mine[k] += w < wave ? v[k] : 0;
+      before[k] += v[k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) x[k] += mine[k];
+}
+
+template <int G, bool SHARED>
+__global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentArgs a) {
+  __shared__ int2 held[SG_MODEL_UNITS];                 // tiles, tokens
+  __shared__ int4 tmp[SG_PLAN_WAVES];
+  __shared__ float2 sums[SG_PLAN_WAVES];
+  __shared__ int upto[SG_PLAN_THREADS];                 // pieces of blocks, up to and with a unit
+  __shared__ Unit chunk[SG_PLAN_THREADS];
+  __shared__ int2 cut[SG_PLAN_THREADS];                 // pieces, row of results (-1: none)
+  __shared__ int class_at[SG_CLASSES];
+  CK_FETCH_ARG(a.starts);
+  CK_FETCH_ARG(a.S);
+  CK_FETCH_ARG(a.pages.rows);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  using U = Units<G, SHARED>;
+  const U units{a};
+  const int n_units = units.count();
+  const bool model = n_units <= SG_MODEL_UNITS;
+  auto all_sum = [&](float2 v) {
+    v = make_float2(wave_sum(v.x), wave_sum(v.y));
+    __syncthreads();                                    // sums may still be in use
+    if (lane == 0) sums[wave] = v;
+    __syncthreads();
+    v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < SG_PLAN_WAVES; ++w) v = make_float2(v.x + sums[w].x, v.y + sums[w].y);
+    return v;
+  };
+
+  // ---- how long it takes at best: all compute units busy until the end ----
+  float2 work = make_float2(0.f, 0.f);                  // y: tiles
+  Unit first = {};
+  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
+    const Unit u = units.load(i0 + tid);
+    if (i0 == 0) first = u;
+    const int tiles = u.tiles(), blocks = U::blocks(u), rows = min(u.tokens * G, AT_ROWS);
+    if (model) held[min(i0 + tid, SG_MODEL_UNITS - 1)] = make_int2(tiles, u.tokens);
+    if (tiles > 0) {
+      work.x += (float)blocks * fmaf((float)tiles, tile_cost(rows, blocks), SG_PIECE_COST + (SHARED ? SG_ROW_COST * (float)rows : 0.f));
+      work.y += (float)blocks * (float)tiles;
+    }
+  }
+  work = all_sum(work);
+  const float least = fmaxf(work.x * (float)a.Hkv / SG_CUS, 6.f);
+
+  // ---- and how long it has to be given, so that the pieces fit: a wavefront tries one length, each a sixteenth longer ----
+  float within = least * 1.25f;
+  if (model) {
+    const float mine = least * (1.f + (float)wave / 16.f);
+    float2 need = make_float2(0.f, 0.f);
+    for (int i = lane; i < n_units; i += WAVE) {
+      const int2 u = held[i];
+      need.x += choose<SHARED>(u.x, (u.y + U::TOKENS - 1) / U::TOKENS, min(u.y * G, AT_ROWS), a.Hkv, mine).units;
+    }
+    need.x = wave_sum(need.x);
+    __syncthreads();
+    if (lane == 0) sums[wave] = need;
+    __syncthreads();
+    within = least * 2.f;
+#pragma unroll
+    for (int w = SG_PLAN_WAVES - 1; w >= 0; --w)
+      if (sums[w].x <= (float)SG_CUS) within = least * (1.f + (float)w / 16.f);
+  }
+
+  // ---- pieces of every unit, unless they are too many: then at least an even share each ----
+  auto chosen = [&](const Unit& u) {
+    return choose<SHARED>(u.tiles(), U::blocks(u), min(u.tokens * G, AT_ROWS), a.Hkv, within).pieces;
+  };
+  float2 extra = make_float2(0.f, 0.f);
+  int first_pieces = 0;
+  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
+    if (i0 + wave * WAVE >= n_units) break;             // wave-uniform
+    const Unit u = i0 == 0 ? first : units.load(i0 + tid);
+    const int n = chosen(u);
+    if (i0 == 0) first_pieces = n;
+    extra.x += (float)max(0, n - 1) * (float)U::blocks(u);
+  }
+  extra = all_sum(extra);
+  const bool shares = extra.x * (float)a.Hkv > SG_EXTRA;
+  const int length = max(SG_MIN_TILES, (int)fminf(ceilf(work.y * (float)a.Hkv / SG_CUS), 1e9f));   // tiles
+
+  // ---- numbers of pieces, rows of results and joins before each unit ----
+  int before[3] = {0, 0, 0};
+  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
+    const int i = i0 + tid, pieces_before = before[0];
+    const Unit u = i0 == 0 ? first : units.load(i);
+    int n = 0;
+    if (i < n_units && u.tokens > 0) {
+      if (shares)
+        n = max(SHARED ? 0 : 1, (u.tiles() + length - 1) / length);
+      else
+        n = i0 == 0 ? first_pieces : chosen(u);
+    }
+    const int blocks = U::blocks(u);
+    const bool stored = SHARED || n > 1;
+    const int mine[3] = {n * blocks, stored ? n * u.tokens : 0, !SHARED && stored ? blocks : 0};
+    int sum[3] = {mine[0], mine[1], mine[2]};
+    scan_three(sum, before, tmp);
+    upto[tid] = sum[0] - pieces_before;
+    chunk[tid] = u;
+    const int result = sum[1] - mine[1];
+    cut[tid] = make_int2(n, stored ? result : -1);
+    if (tid < SG_CLASSES) class_at[tid] = 0;
+    if constexpr (SHARED) {
+      if (i < n_units) a.joins[i] = {u.begin, u.tokens, n, result, u.tokens, {}};
+    } else {
+      for (int b = 0; b < mine[2]; ++b) {
+        const int at = sum[2] - mine[2] + b;
+        if (at < a.most_joins)
+          a.joins[at] = {u.begin + b * U::TOKENS, min(U::TOKENS, u.tokens - b * U::TOKENS), n, result + b * U::TOKENS, u.tokens, {}};
+      }
+    }
+    __syncthreads();
+    // Pieces of the chunk.  The blocks of a piece come one after the other: they read the same rows.
+    const int here = before[0] - pieces_before, in_chunk = min(SG_PLAN_THREADS, n_units - i0);
+    auto piece_of = [&](int x) {
+      int s = 0;
+      for (int len = in_chunk - 1; len > 0;) {          // the first with upto > x
+        const int half = len >> 1;
+        const bool right = upto[s + half] <= x;
+        s = right ? s + half + 1 : s;
+        len = right ? len - half - 1 : half;
+      }
+      const Unit v = chunk[s];
+      const int k = x - (s > 0 ? upto[s - 1] : 0), n_blocks = max(1, U::blocks(v)), n_pieces = max(1, cut[s].x);
+      const int piece = min(k / n_blocks, n_pieces - 1), block = k - k / n_blocks * n_blocks, tiles = v.tiles();
+      const int from = (int)((int64_t)tiles * piece / n_pieces), to = (int)((int64_t)tiles * (piece + 1) / n_pieces);
+      Piece p;
+      p.t0 = v.begin + block * U::TOKENS;
+      p.n_tok = (short)min(U::TOKENS, v.tokens - block * U::TOKENS);
+      p.flags = (n_blocks > 1 ? Piece::SEVERAL : 0) | (SHARED && i0 + s < a.n_segments ? Piece::LIMITED : 0);
+      p.seq = v.seq;
+      p.lo = v.lo;
+      p.end = v.end;
+      p.row = v.row0() + from * AT_TILE;
+      p.n_tiles = to - from;
+      p.result = cut[s].y < 0 ? -1 : cut[s].y + piece * v.tokens + block * U::TOKENS;
+      return p;
+    };
+    // Those that take longest go first, so that what runs at the end is short.  Which of a class comes first changes no
+    // result: where each leaves its results does not depend on it.
+    auto class_of = [&](const Piece& p) {
+      const float share = (float)p.n_tiles * tile_cost(p.n_tok * G, p.flags & Piece::SEVERAL ? 2 : 1) / within;
+      return max(0, min(SG_CLASSES - 1, SG_CLASSES - 1 - (int)(share * SG_CLASSES)));
+    };
+    if (here > SG_CUS / a.Hkv && n_units <= SG_PLAN_THREADS && here <= SG_PLAN_THREADS) {
+      Piece p;
+      int c = 0, rank = 0;
+      if (tid < here) {
+        p = piece_of(tid);
+        c = class_of(p);
+        rank = atomicAdd(&class_at[c], 1);
+      }
+      __syncthreads();
+      for (int k = 0; k < c; ++k) rank += class_at[k];
+      if (tid < here && rank < a.most_pieces) a.pieces[rank] = p;
+    } else {
+      for (int x = tid; x < here; x += SG_PLAN_THREADS)
+        if (pieces_before + x < a.most_pieces) a.pieces[pieces_before + x] = piece_of(x);
+    }
+    __syncthreads();
+  }
+  if (tid == 0) *a.counts = {min(before[0], a.most_pieces), min(before[2], a.most_joins)};
+}
+
+// What a piece of R query rows (token, head of the group) leaves for one KV head: maximum and sum of every row (and as
 // much room again), then its 128 channels four by four, i = 0 .. 15 outermost: those of both halves of a wavefront
 // beside each other, so that a wavefront writes 1 KB at a time and a reader of few rows whole lines.
 struct Partial {
   float* base;
   int R;
-  bool there;                                           // of the workspace
-  __device__ __forceinline__ Partial(const SegmentArgs& a, const Unit& u, int G, int rows, int piece, int h) : R(u.tokens * G) {
-    const int64_t first = (int64_t)rows * a.Hkv * G + ((int64_t)piece * a.Hkv + h) * R;
+  bool there;                                           // in the workspace
+  __device__ __forceinline__ Partial(const SegmentArgs& a, int G, int result, int n_tok, int h) : R(n_tok * G) {
+    const int64_t first = (int64_t)result * a.Hkv * G + (int64_t)h * R;
     there = first >= 0 && first + R <= a.part_rows;
     base = a.part + (there ? first : 0) * SG_ROW;
   }
@@ -209,223 +352,383 @@ __device__ __forceinline__ int wave_least(int v) {
   return __builtin_amdgcn_readfirstlane(v);
 }
 
+// LDS of the two ways
+struct FewBuffers {
+  int rows[AT_WAVES][2][WAVE];
+  union {
+    __attribute__((aligned(16))) bf16 stage[AT_WAVES][STAGE_ELEMS];
+    __attribute__((aligned(16))) float red[AT_WAVES][SG_FEW * SR_PART];
+  };
+};
+union SegmentLds {
+  TileBuffers tiles;
+  FewBuffers few;
+};
+
+// Up to 16 queries: the rows of a piece in one contiguous run for each wavefront.
+template <int G>
+__device__ __forceinline__ void attend_few(const SegmentArgs& a, const Piece& pc, int h, FewBuffers& lds) {
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_rows = pc.n_tok * G;
+  const int first = max(pc.lo, pc.row), n_pos = max(0, min(pc.end, pc.row + pc.n_tiles * AT_TILE) - first);
+  const int run = ((n_pos + AT_WAVES - 1) / AT_WAVES + SR_STEP - 1) / SR_STEP * SR_STEP;
+  const int w_begin = first + min(wave * run, n_pos), w_end = first + min((wave + 1) * run, n_pos);
+  const int n_steps = (w_end - w_begin + SR_STEP - 1) / SR_STEP;
+  const int mine = col < n_rows ? col : 0;
+  const bf16* q = a.q + ((int64_t)(pc.t0 + mine / G) * a.Hq + h * G + mine % G) * D + kg * 8;
+  bf16x8 qb[4];
+#pragma unroll
+  for (int sl = 0; sl < 4; ++sl) qb[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + sl * 32));
+  struct Found { int page, slot; };
+  auto look_up = [&](int group) -> Found {
+    const int p = w_begin + group * WAVE + lane;
+    const Pages::Entry e = a.pages.entry(pc.seq, p < w_end ? p : -1);
+    return {a.pages.table[e.at], e.slot};
+  };
+  int(*rows)[WAVE] = lds.rows[wave];
+  auto put_rows = [&](int group, const Found& f) { rows[group & 1][lane] = a.pages.place(f.page, h, f.slot); };
+  auto step_rows = [&](int t) { return *reinterpret_cast<const int4*>(&rows[(t >> 2) & 1][(t & 3) * 16 + kg * 4]); };
+  const bf16 *K = a.K + col * 8, *V = a.V + col * 8;
+  auto fetch = [&](int t, StepBf16& r) {
+    const int4 tr = step_rows(t);
+    const int w[4] = {tr.x, tr.y, tr.z, tr.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = (int64_t)(w[i] < 0 ? 0 : w[i]) * D;
+      r.k[i] = load_once(K + at);
+      r.v[i] = load_once(V + at);
+    }
+  };
+  StateBf16<SG_FEW> state;
+  state.clear();
+  const Stage16 stage(lds.stage[wave], lane);
+  // Two register sets in turn, whose loads go on behind the end, as in the attention of single tokens.
+  if (n_steps > 0) {                                    // wave-uniform
+    put_rows(0, look_up(0));
+    Found next = look_up(1);
+    wave_lds_order();
+    StepBf16 sets[2];
+    fetch(0, sets[0]);
+    for (int group = 0;; ++group) {
+      wave_lds_order();
+      put_rows(group + 1, next);
+      wave_lds_order();
+      next = look_up(group + 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int t = group * 4 + j;
+        fetch(t + 1, sets[(j + 1) & 1]);
+        state.add(sets[j & 1], step_rows(t), qb, stage, a.scale_log2e);
+        if (t + 1 >= n_steps) goto reduced;
+      }
+    }
+  }
+reduced:
+  __syncthreads();                                      // nobody turns rows any more
+  state.leave(lds.red[wave], n_rows);
+  __syncthreads();
+  const int result = pc.result;
+  const Partial to(a, G, result, pc.n_tok, h);
+  if (result >= 0 && !to.there) return;
+  for (int e = tid; e < n_rows * (D / 4); e += AT_WAVES * 64) {
+    const int row = e / (D / 4), c4 = e % (D / 4);
+    float2 ml[AT_WAVES];
+    float mx = NO_ROW_YET;
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) {
+      ml[w] = *reinterpret_cast<const float2*>(&lds.red[w][row * SR_PART]);
+      mx = fmaxf(mx, ml[w].x);
+    }
+    float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < AT_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[w].x - mx);
+      const float2* acc = reinterpret_cast<const float2*>(&lds.red[w][row * SR_PART + 2 + c4 * 4]);
+      const float2 a0 = acc[0], a1 = acc[1];
+      l = fmaf(ml[w].y, f, l);
+      x[0] = fmaf(a0.x, f, x[0]);
+      x[1] = fmaf(a0.y, f, x[1]);
+      x[2] = fmaf(a1.x, f, x[2]);
+      x[3] = fmaf(a1.y, f, x[3]);
+    }
+    if (result >= 0) {
+      if (c4 == 0) *to.stats(row) = make_float2(mx, l);
+      *to.four(c4 >> 1, row, c4 & 1) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+      const float inv = l > 0.f ? 1.0f / l : 0.f;
+      *reinterpret_cast<uint2*>(a.out + ((int64_t)(pc.t0 + row / G) * a.Hq + h * G + row % G) * D + c4 * 4) =
+          four_bf16(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    }
+  }
+}
+
 template <int G, bool EIGHTS, bool SHARED>
 __global__ __launch_bounds__(AT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_segment_attn(const SegmentArgs a) {
-  __shared__ TileBuffers lds;
+  __shared__ SegmentLds lds;
   const int tid = threadIdx.x, lane = tid & 63, col = tid & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.x % a.Hkv, x = blockIdx.x / a.Hkv;
-  using Cuts = Cut<G, SHARED>;
-  const Cuts cut(a);
-  typename Cuts::Place at;
-  if (!cut.find(x, [&](const Unit& u) { return Cuts::blocks(u) * cut.pieces(u); }, &at)) return;
-  const Unit& u = at.u;
-  // the blocks of a piece one after the other: they read the same rows
-  const int n_blocks = Cuts::blocks(u), piece = at.rest / n_blocks, block = at.rest - piece * n_blocks;
-  if (piece >= at.n_pieces) return;
-  const int tok0 = block * Cuts::TOKENS, n_tok = min(Cuts::TOKENS, u.tokens - tok0);
-  const int tiles = u.tiles();
-  const int tile0 = (int)((int64_t)tiles * piece / at.n_pieces), tile1 = (int)((int64_t)tiles * (piece + 1) / at.n_pieces);
-  const int row0 = u.row0() + tile0 * AT_TILE;
+  const int n_pieces = a.counts->pieces;
+  const int4* from = reinterpret_cast<const int4*>(a.pieces + min(x, a.most_pieces - 1));
+  const int4 lo = from[0], hi = from[1];
+  if (x >= n_pieces) return;
+  auto all = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int sizes = all(lo.y);
+  const Piece pc = {all(lo.x), (short)sizes, (short)(sizes >> 16), all(lo.z), all(lo.w), all(hi.x), all(hi.y), all(hi.z), all(hi.w)};
 
-  // ---- what the queries see ----
+  // ---- what the queries see: of shared rows, as far as their own sequences go, and share ----
   const int row = wave * 32 + col, token = row / G;     // of the block
-  const bool there = token < n_tok;
-  const int t = u.begin + tok0 + (there ? token : 0);
-  const int64_t q_at = ((int64_t)t * a.Hq + h * G + row % G) * D;
-  int upto = u.end, least = u.end, my_least = u.end;
-  if (SHARED && at.list == 0) {                         // as far as their own sequences go, and share
-    auto limit = [&](int s) { return max(0, min(min(a.shared[s], a.pages.clamp_length(a.lengths[s])), u.end)); };
+  const bool there = token < pc.n_tok;
+  const int t = pc.t0 + (there ? token : 0);
+  int upto = pc.end, least = pc.end, my_least = pc.end;
+  if (SHARED && (pc.flags & Piece::LIMITED)) {
+    auto limit = [&](int s) { return max(0, min(min(a.shared[s], a.pages.clamp_length(a.lengths[s])), pc.end)); };
     upto = limit(t);
-    my_least = wave_least(there ? upto : u.end);
-    for (int i = lane; i < n_tok; i += WAVE) least = min(least, limit(u.begin + tok0 + i));
+    my_least = wave_least(there ? upto : pc.end);
+    for (int i = lane; i < pc.n_tok; i += WAVE) least = min(least, limit(pc.t0 + i));
     least = wave_least(least);
   }
-  const int from_whole = u.lo > row0 ? 1 : 0;
-  SegmentView view = {u.seq,
-                      u.end,
-                      tile1 - tile0,
-                      row0,
-                      u.lo,
-                      (there ? upto : 0) - 1,
-                      Tiles(from_whole, max(0, least - row0) / AT_TILE),
-                      Tiles(from_whole, max(0, my_least - row0) / AT_TILE),
-                      0,
-                      wave * 32 < n_tok * G ? tile1 - tile0 : 0};
+  if (pc.n_tok * G <= SG_FEW && least == pc.end) {
+    attend_few<G>(a, pc, h, lds.few);
+    return;
+  }
+
+  const int from_whole = pc.lo > pc.row ? 1 : 0;
+  const SegmentView view = {pc.seq,
+                            pc.end,
+                            pc.n_tiles,
+                            pc.row,
+                            pc.lo,
+                            (there ? upto : 0) - 1,
+                            Tiles(from_whole, max(0, least - pc.row) / AT_TILE),
+                            Tiles(from_whole, max(0, my_least - pc.row) / AT_TILE),
+                            0,
+                            wave * 32 < pc.n_tok * G ? pc.n_tiles : 0};
   QueryState state;
-  attend_tiles<EIGHTS>(view, a.K, a.V, a.pages, h, a.scale_log2e, a.q + q_at, n_blocks == 1, lds, state);
+  attend_tiles<EIGHTS>(view, a.K, a.V, a.pages, h, a.scale_log2e, a.q + ((int64_t)t * a.Hq + h * G + row % G) * D,
+                       (pc.flags & Piece::SEVERAL) == 0, lds.tiles, state);
 
   const float l = xor32(state.l, OpSum());
-  if (SHARED || at.n_pieces > 1) {
-    const Partial to(a, u, G, at.rows, piece, h);
+  if (pc.result >= 0) {
+    const Partial to(a, G, pc.result, pc.n_tok, h);
     if (!there || !to.there) return;
-    const int r = tok0 * G + row, half = lane >> 5;
-    if (half == 0) *to.stats(r) = make_float2(state.nothing() ? AT_NEG_BIG : state.m, l);
+    const int half = lane >> 5;
+    if (half == 0) *to.stats(row) = make_float2(state.nothing() ? AT_NEG_BIG : state.m, l);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const floatx16& acc = state.acc[i >> 2];
       const int e = 4 * (i & 3);
-      *to.four(i, r, half) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+      *to.four(i, row, half) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
     }
     return;
   }
-  write_outputs(state, l, lds, [&](int to) -> bf16* {
+  write_outputs(state, l, lds.tiles, [&](int to) -> bf16* {
     const int tok = to / G;
-    return tok < n_tok ? a.out + ((int64_t)(u.begin + tok0 + tok) * a.Hq + h * G + to % G) * D : nullptr;
+    return tok < pc.n_tok ? a.out + ((int64_t)(pc.t0 + tok) * a.Hq + h * G + to % G) * D : nullptr;
   });
 }
 
-// Pieces joined: a wavefront has the G heads of one token and KV head.
-template <int G>
-struct Joined {
-  static constexpr int N = G > 1 ? G / 2 : 1;           // of a lane: four channels each
+// Pieces joined: ROWS query rows of one KV head a workgroup, a quarter of the pieces each wavefront, then those four.
+// Workgroups of a wavefront for all pieces: the shared rows of 16 sequences in 17 pieces took 12.5 us.
+constexpr int SG_JOIN_WAVES = 4;
+constexpr int SG_JOIN_ROWS = 8;                         // of a block of a segment
+
+struct Source {                                         // pieces that have results of the rows
+  int n, result, step, n_tok, row;
+};
+template <int ROWS>
+struct JoinBuffers {
+  float4 x[SG_JOIN_WAVES][ROWS * 32];
+  float2 stats[SG_JOIN_WAVES][ROWS];
+};
+// to(row): where the output of a row goes, nullptr: nowhere
+template <int ROWS, int G, class To>
+__device__ __forceinline__ void join_rows(const SegmentArgs& a, const Source& s0, const Source& s1, int h, int n_rows,
+                                          JoinBuffers<ROWS>& lds, To to) {
+  constexpr int N = ROWS > 1 ? ROWS / 2 : 1;            // of a lane: four channels each
+  constexpr int BATCH = N < 4 ? 4 / N * 2 : 2;          // pieces whose loads are under way together
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = s0.n + s1.n;
   float m[N], l[N];
   float4 x[N];
-  __device__ __forceinline__ Joined() {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      m[k] = AT_NEG_BIG;
-      l[k] = 0.f;
-      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+  for (int k = 0; k < N; ++k) {
+    m[k] = AT_NEG_BIG;
+    l[k] = 0.f;
+    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  __device__ __forceinline__ static int channels(int k) { return (((threadIdx.x & 63) + 64 * k) / (2 * G)) & 15; }
-  __device__ __forceinline__ static int head(int k) { return ((threadIdx.x & 63) + 64 * k) % (2 * G) / 2; }
-  __device__ __forceinline__ static int half(int) { return threadIdx.x & 1; }
-  __device__ __forceinline__ void add(const SegmentArgs& a, const Unit& u, int rows, int n, int h, int token) {
-    constexpr int BATCH = 8 / N;                        // pieces whose loads are under way together
-    for (int p0 = 0; p0 < n; p0 += BATCH) {
-      float2 st[BATCH][N];
-      float4 f[BATCH][N];
+  // number e = lane + 64 k of the rows' 32 pieces of four channels: i, row and half, see Partial
+  auto row_of = [&](int k) { return min((lane + 64 * k) % (2 * ROWS) / 2, n_rows - 1); };
+  auto four_of = [&](int k) { return ((lane + 64 * k) / (2 * ROWS)) & 15; };
+  for (int p0 = wave; p0 < n; p0 += SG_JOIN_WAVES * BATCH) {
+    float2 st[BATCH][N];
+    float4 f[BATCH][N];
 #pragma unroll
-      for (int p = 0; p < BATCH; ++p) {                 // the last one again behind the end
-        const Partial from(a, u, G, rows, min(p0 + p, n - 1), h);
+    for (int b = 0; b < BATCH; ++b) {                   // the last one again behind the end
+      const int p = min(p0 + SG_JOIN_WAVES * b, n - 1);
+      const Source& s = p < s0.n ? s0 : s1;
+      const Partial from(a, G, s.result + (p < s0.n ? p : p - s0.n) * s.step, s.n_tok, h);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const int row = from.there ? token * G + head(k) : 0;
-          st[p][k] = *from.stats(row);
-          f[p][k] = *from.four(channels(k), row, half(k));
-        }
+      for (int k = 0; k < N; ++k) {
+        const int row = from.there ? s.row + row_of(k) : 0;
+        st[b][k] = *from.stats(row);
+        f[b][k] = *from.four(four_of(k), row, lane & 1);
       }
-      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int p = 0; p < BATCH; ++p) {
-        if (p0 + p >= n) break;                         // uniform
+    for (int b = 0; b < BATCH; ++b) {
+      if (p0 + SG_JOIN_WAVES * b >= n) break;           // uniform
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          const float mx = fmaxf(m[k], st[p][k].x);
-          const float old = __builtin_amdgcn_exp2f(m[k] - mx), add = __builtin_amdgcn_exp2f(st[p][k].x - mx);
-          m[k] = mx;
-          l[k] = l[k] * old + st[p][k].y * add;
-          x[k].x = x[k].x * old + f[p][k].x * add;
-          x[k].y = x[k].y * old + f[p][k].y * add;
-          x[k].z = x[k].z * old + f[p][k].z * add;
-          x[k].w = x[k].w * old + f[p][k].w * add;
-        }
+      for (int k = 0; k < N; ++k) {
+        const float mx = fmaxf(m[k], st[b][k].x);
+        const float old = __builtin_amdgcn_exp2f(m[k] - mx), add = __builtin_amdgcn_exp2f(st[b][k].x - mx);
+        m[k] = mx;
+        l[k] = l[k] * old + st[b][k].y * add;
+        x[k].x = x[k].x * old + f[b][k].x * add;
+        x[k].y = x[k].y * old + f[b][k].y * add;
+        x[k].z = x[k].z * old + f[b][k].z * add;
+        x[k].w = x[k].w * old + f[b][k].w * add;
       }
     }
   }
-  __device__ __forceinline__ void write(const SegmentArgs& a, int t, int h) const {
+  __syncthreads();                                      // of an earlier turn
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (G == 1 && (threadIdx.x & 63) >= 32) continue;
-      const float inv = l[k] > 0.f ? 1.0f / l[k] : 0.f;
-      *reinterpret_cast<uint2*>(a.out + ((int64_t)t * a.Hq + h * G + head(k)) * D + 8 * channels(k) + 4 * half(k)) =
-          four_bf16(x[k].x * inv, x[k].y * inv, x[k].z * inv, x[k].w * inv);
-    }
+  for (int k = 0; k < N; ++k) {
+    const int e = lane + 64 * k;
+    if (e >= ROWS * 32) continue;
+    lds.x[wave][e] = x[k];
+    if (four_of(k) == 0) lds.stats[wave][e % (2 * ROWS) / 2] = make_float2(m[k], l[k]);
   }
-};
+  __syncthreads();
+  const int row = tid % (2 * ROWS) / 2;
+  if (tid >= ROWS * 32 || row >= n_rows) return;
+  float mx = AT_NEG_BIG, sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < SG_JOIN_WAVES; ++w) mx = fmaxf(mx, lds.stats[w][row].x);
+#pragma unroll
+  for (int w = 0; w < SG_JOIN_WAVES; ++w) {
+    const float f = __builtin_amdgcn_exp2f(lds.stats[w][row].x - mx);
+    const float4 v = lds.x[w][tid];
+    sum = fmaf(lds.stats[w][row].y, f, sum);
+    y[0] = fmaf(v.x, f, y[0]);
+    y[1] = fmaf(v.y, f, y[1]);
+    y[2] = fmaf(v.z, f, y[2]);
+    y[3] = fmaf(v.w, f, y[3]);
+  }
+  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  bf16* at = to(row);
+  *reinterpret_cast<uint2*>(at + 8 * (tid / (2 * ROWS)) + 4 * (tid & 1)) = four_bf16(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+}
 
-constexpr int SG_JOIN_WAVES = 4;
 template <int G, bool SHARED>
 __global__ __launch_bounds__(SG_JOIN_WAVES * 64) void k_segment_join(const SegmentArgs a) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  using Cuts = Cut<G, SHARED>;
-  const Cuts cut(a);
-  typename Cuts::Place at;
-  for (int64_t i = (int64_t)blockIdx.x * SG_JOIN_WAVES + wave;; i += (int64_t)gridDim.x * SG_JOIN_WAVES) {
-    const int x = (int)(i / a.Hkv), h = (int)(i - (int64_t)x * a.Hkv);
-    Joined<G> sum;
-    if constexpr (SHARED) {                             // sequence x: what its group shares, then its own rows
-      if (x >= a.S) return;
-      const int g = find_sequence(a.starts, a.n_segments, x);
-      if (g >= 0) {
-        at = cut.nth(0, g);
-        sum.add(a, at.u, at.rows, at.n_pieces, h, x - at.u.begin);
-      }
-      at = cut.nth(1, x);
-      sum.add(a, at.u, at.rows, at.n_pieces, h, 0);
-      sum.write(a, x, h);
-    } else {
-      if (!cut.find(x, [&](const Unit& u) { return cut.pieces(u) > 1 ? u.tokens : 0; }, &at)) return;
-      sum.add(a, at.u, at.rows, at.n_pieces, h, at.rest);
-      sum.write(a, at.u.begin + at.rest, h);
+  constexpr int TOKENS = AT_ROWS / G;
+  if constexpr (SHARED) {                               // a sequence and KV head: what its group shares, then its own rows
+    __shared__ JoinBuffers<G> lds;
+    const int s = blockIdx.x / a.Hkv, h = blockIdx.x - s * a.Hkv;
+    const Whole own = a.joins[a.n_segments + s];
+    const int g = __builtin_amdgcn_readfirstlane(find_sequence(a.starts, a.n_segments, s));
+    Source shared = {};
+    if (g >= 0) {
+      const Whole w = a.joins[g];
+      const int token = s - w.t0, block = token / TOKENS;
+      shared = {w.n_pieces, w.result + block * TOKENS, w.step, min(TOKENS, w.n_tok - block * TOKENS), (token - block * TOKENS) * G};
+    }
+    join_rows<G, G>(a, shared, Source{own.n_pieces, own.result, own.step, 1, 0}, h, G, lds,
+                    [&](int row) { return a.out + ((int64_t)s * a.Hq + h * G + row) * D; });
+  } else {                                              // eight rows of a block
+    __shared__ JoinBuffers<SG_JOIN_ROWS> lds;
+    constexpr int PARTS = AT_ROWS / SG_JOIN_ROWS;
+    const int n = a.counts->joins * a.Hkv * PARTS;
+    for (int i = blockIdx.x; i < n; i += gridDim.x) {
+      const int j = i / (a.Hkv * PARTS), rest = i - j * (a.Hkv * PARTS), h = rest / PARTS, row0 = rest % PARTS * SG_JOIN_ROWS;
+      const Whole w = a.joins[j];
+      const int n_rows = min(SG_JOIN_ROWS, w.n_tok * G - row0);
+      if (n_rows <= 0) continue;
+      join_rows<SG_JOIN_ROWS, G>(a, Source{w.n_pieces, w.result, w.step, w.n_tok, row0}, Source{}, h, n_rows, lds, [&](int row) {
+        const int r = row0 + row;
+        return a.out + ((int64_t)(w.t0 + r / G) * a.Hq + h * G + r % G) * D;
+      });
     }
   }
 }
 
-template <bool EIGHTS, bool SHARED>
-void launch_segments_g(int G, unsigned groups, unsigned joins, const SegmentArgs& a, hipStream_t st) {
-  const dim3 grid(groups), block(AT_WAVES * 64), join(joins), join_block(SG_JOIN_WAVES * 64);
+template <int G, bool SHARED>
+void launch_segments_g(unsigned groups, unsigned joins, bool eights, const SegmentArgs& a, hipStream_t st) {
+  const dim3 grid(groups), block(AT_WAVES * 64);
+  hipLaunchKernelGGL((k_segment_plan<G, SHARED>), dim3(1), dim3(SG_PLAN_THREADS), 0, st, a);
+  if (eights)
+    hipLaunchKernelGGL((k_segment_attn<G, true, SHARED>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_segment_attn<G, false, SHARED>), grid, block, 0, st, a);
+  if (joins) hipLaunchKernelGGL((k_segment_join<G, SHARED>), dim3(joins), dim3(SG_JOIN_WAVES * 64), 0, st, a);
+}
+template <bool SHARED>
+void launch_segments_all(int G, unsigned groups, unsigned joins, bool eights, const SegmentArgs& a, hipStream_t st) {
   switch (G) {
-    case 1: hipLaunchKernelGGL((k_segment_attn<1, EIGHTS, SHARED>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_segment_attn<2, EIGHTS, SHARED>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_segment_attn<4, EIGHTS, SHARED>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_segment_attn<8, EIGHTS, SHARED>), grid, block, 0, st, a); break;
-  }
-  if (joins == 0) return;
-  switch (G) {
-    case 1: hipLaunchKernelGGL((k_segment_join<1, SHARED>), join, join_block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_segment_join<2, SHARED>), join, join_block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_segment_join<4, SHARED>), join, join_block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_segment_join<8, SHARED>), join, join_block, 0, st, a); break;
+    case 1: launch_segments_g<1, SHARED>(groups, joins, eights, a, st); break;
+    case 2: launch_segments_g<2, SHARED>(groups, joins, eights, a, st); break;
+    case 4: launch_segments_g<4, SHARED>(groups, joins, eights, a, st); break;
+    default: launch_segments_g<8, SHARED>(groups, joins, eights, a, st); break;
   }
 }
 
-// Rows of results.  Of every unit the pieces but the last are whole ones of total / SG_CUS tiles or more, so there are
-// at most SG_CUS of those, over all blocks and heads, and twice as many of units that have more than one.
-int64_t split_rows(const Dims& dm, int64_t n_rows) {
-  const int64_t most = n_rows * dm.G < AT_ROWS ? n_rows * dm.G : AT_ROWS;
-  return 2 * SG_CUS * most;
-}
-size_t row_bytes(int64_t rows) { return (size_t)rows * SG_ROW * sizeof(float); }
+// What a workspace holds, for n_segments segments with n_rows tokens (and S sequences with rows of their own).
+struct Space {
+  int64_t pieces, joins, rows;
+  Space(const Dims& dm, int64_t n_rows, int64_t n_segments, bool shared) {
+    // blocks there can be, as one of each segment may be short, and the pieces that are more than those
+    const int64_t blocks = n_rows / (AT_ROWS / dm.G) + (n_rows < n_segments ? n_rows : n_segments);
+    pieces = blocks + (shared ? dm.S : 0) + SG_EXTRA / dm.Hkv;
+    joins = shared ? n_segments + dm.S : SG_EXTRA / dm.Hkv + 1;
+    // A unit that is cut has at most twice as many pieces as are more than its blocks.
+    const int64_t most = n_rows * dm.G < AT_ROWS ? n_rows * dm.G : AT_ROWS;
+    rows = 2 * SG_EXTRA * most + (shared ? 2ll * dm.S * dm.Hq : 0);
+  }
+  static size_t padded(size_t n) { return (n + 255) & ~(size_t)255; }
+  size_t joins_at() const { return 256 + padded((size_t)pieces * sizeof(Piece)); }
+  size_t part_at() const { return joins_at() + padded((size_t)joins * sizeof(Whole)); }
+  size_t bytes() const { return part_at() + (size_t)rows * SG_ROW * sizeof(float); }
+};
 
-hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv, int64_t part_rows, float softmax_scale,
-                           hipStream_t st) {
+hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv, const Space& space, void* workspace,
+                           float softmax_scale, hipStream_t st) {
+  char* ws = static_cast<char*>(workspace);
+  a.counts = reinterpret_cast<Counts*>(ws);
+  a.pieces = reinterpret_cast<Piece*>(ws + 256);
+  a.joins = reinterpret_cast<Whole*>(ws + space.joins_at());
+  a.part = reinterpret_cast<float*>(ws + space.part_at());
+  a.most_pieces = (int)space.pieces;
+  a.most_joins = (int)space.joins;
+  a.part_rows = (int)space.rows;
   a.K = static_cast<const bf16*>(kv.K);
   a.V = static_cast<const bf16*>(kv.V);
   a.pages = Pages(kv, dm.Hkv);
   a.S = dm.S;
   a.Hq = dm.Hq;
   a.Hkv = dm.Hkv;
-  a.part_rows = (int)part_rows;
   a.scale_log2e = softmax_scale * 1.4426950408889634f;
-  // blocks there can be, as one of each segment may be short, and the pieces that are more than those
-  const int64_t blocks = a.n_rows / (AT_ROWS / dm.G) + (a.n_rows < a.n_segments ? a.n_rows : a.n_segments);
-  const int64_t units = blocks + (a.shared ? dm.S : 0);
-  const bool cut = a.pages.rows > SG_MIN_TILES * AT_TILE;
-  const unsigned groups = (unsigned)(units * dm.Hkv + (cut ? SG_CUS : 0));
-  const int64_t items = (int64_t)a.n_rows * dm.Hkv;
-  const int64_t joins = (items + SG_JOIN_WAVES - 1) / SG_JOIN_WAVES;
+  const unsigned groups = (unsigned)(space.pieces * dm.Hkv);
   const bool eights = kv.page_size % 8 == 0;
   if (a.shared) {
-    eights ? launch_segments_g<true, true>(dm.G, groups, (unsigned)joins, a, st)
-           : launch_segments_g<false, true>(dm.G, groups, (unsigned)joins, a, st);
+    launch_segments_all<true>(dm.G, groups, (unsigned)dm.HP, eights, a, st);
   } else {
-    const unsigned some = cut ? (unsigned)(joins < 4 * SG_CUS ? joins : 4 * SG_CUS) : 0;
-    eights ? launch_segments_g<true, false>(dm.G, groups, some, a, st)
-           : launch_segments_g<false, false>(dm.G, groups, some, a, st);
+    const int64_t parts = space.joins * dm.Hkv * (AT_ROWS / SG_JOIN_ROWS);
+    const bool cut = a.pages.rows > 2 * SG_MIN_TILES * AT_TILE - AT_TILE;   // otherwise no unit is
+    launch_segments_all<false>(dm.G, groups, cut ? (unsigned)(parts < 8 * SG_CUS ? parts : 8 * SG_CUS) : 0, eights, a, st);
   }
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t cross_workspace_bytes(const Dims& dm, int64_t n_rows) { return row_bytes(split_rows(dm, n_rows)); }
+size_t cross_workspace_bytes(const Dims& dm, int64_t n_rows) { return Space(dm, n_rows, dm.S, false).bytes(); }
 
-// ... and of every unit one: the shared rows of a sequence, and its own
-size_t shared_workspace_bytes(const Dims& dm) { return row_bytes(split_rows(dm, dm.S) + 2ll * dm.S * dm.Hq); }
+size_t shared_workspace_bytes(const Dims& dm) { return Space(dm, dm.S, dm.S, true).bytes(); }
 
 hipError_t launch_cross_attn(const Dims& dm, const void* q, int64_t n_rows, const int32_t* q_starts,
                              const ck_paged_kv& kv, const int32_t* lengths, float softmax_scale, void* out,
@@ -433,12 +736,11 @@ hipError_t launch_cross_attn(const Dims& dm, const void* q, int64_t n_rows, cons
   SegmentArgs a = {};
   a.q = static_cast<const bf16*>(q);
   a.out = static_cast<bf16*>(out);
-  a.part = static_cast<float*>(workspace);
   a.starts = q_starts;
   a.lengths = lengths;
   a.n_segments = dm.S;
   a.n_rows = (int)n_rows;
-  return launch_segments(dm, a, kv, split_rows(dm, n_rows), softmax_scale, st);
+  return launch_segments(dm, a, kv, Space(dm, n_rows, dm.S, false), workspace, softmax_scale, st);
 }
 
 hipError_t launch_shared_attn(const Dims& dm, const void* q, const ck_paged_kv& kv, const int32_t* lengths,
@@ -447,13 +749,12 @@ hipError_t launch_shared_attn(const Dims& dm, const void* q, const ck_paged_kv& 
   SegmentArgs a = {};
   a.q = static_cast<const bf16*>(q);
   a.out = static_cast<bf16*>(out);
-  a.part = static_cast<float*>(workspace);
   a.starts = group_starts;
   a.lengths = lengths;
   a.shared = shared_rows;
   a.n_segments = n_groups;
   a.n_rows = dm.S;
-  return launch_segments(dm, a, kv, split_rows(dm, dm.S) + 2ll * dm.S * dm.Hq, softmax_scale, st);
+  return launch_segments(dm, a, kv, Space(dm, dm.S, n_groups, true), workspace, softmax_scale, st);
 }
 
 }  // namespace ck

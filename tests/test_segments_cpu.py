@@ -83,7 +83,7 @@ def test_shapes_that_are_refused(bad, want):
     (dict(slots=None), EINVALID), (dict(n=0), EINVALID), (dict(n=-1), EINVALID), (dict(n=(1 << 24) + 1), EUNSUPPORTED),
     (dict(width=0), EINVALID), (dict(pages=0), EINVALID), (dict(size=0), EINVALID), (dict(size=-3), EINVALID),
     (dict(size=2 ** 20, width=2 ** 11), EUNSUPPORTED), (dict(pages=2 ** 28), EUNSUPPORTED),
-    (dict(sh=shape(S=8193)), EUNSUPPORTED), (dict(sh=shape(S=8192), size=1, width=2 ** 18), EUNSUPPORTED)])
+    (dict(pages=2 ** 30 + 1, size=1), EUNSUPPORTED), (dict(sh=shape(S=8193)), EUNSUPPORTED), (dict(sh=shape(S=8192), size=1, width=2 ** 18), EUNSUPPORTED)])
 def test_plan_refuses(bad, want):
     assert code(plan, **bad) == want
 
