@@ -14,7 +14,7 @@ namespace ck {
 namespace {
 
 constexpr int PL_THREADS = 1024, PL_WAVES = PL_THREADS / 64;
-constexpr int PL_LOADS = 32, PL_FIRST_LOADS = 8;        // of 4 counts a lane, for the pages that are looked at together
+constexpr int PL_LOADS = 32, PL_FIRST_LOADS = 2;        // of 4 counts a lane, for the pages that are looked at together
 constexpr int PL_ITEMS = 4;                             // of a thread at a time
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
 constexpr int PL_OWN_ROWS = 8192;
@@ -23,7 +23,7 @@ constexpr int PL_SLOT_ROWS = PL_THREADS;                // of a workgroup of tha
 struct PlanArgs {
   const int32_t *n_new, *parent, *shared_rows;
   int32_t *lengths, *table, *refs, *q_starts, *slots, *lacking;
-  int S, per_seq, n_pages, n_rows;
+  int S, per_seq, n_pages, n_rows;                      // S * per_seq < 2^31
   Divider size;
   __device__ __forceinline__ int pages_of(int rows) const {
     const int n = size.quotient(rows);
@@ -82,7 +82,7 @@ __device__ __forceinline__ void write_slots(const PlanArgs& a, const int* ends, 
       const int64_t r = (int64_t)a.lengths[s] - (ends[s] - (int)t);
       const int e = r >= 0 ? a.size.quotient((int)r) : a.per_seq;
       if (e < a.per_seq) {
-        const int page = a.table[(int64_t)s * a.per_seq + e];
+        const int page = a.table[(uint32_t)(s * a.per_seq + e)];
         if (a.is_page(page)) slot = page * (int)a.size.d + ((int)r - e * (int)a.size.d);
       }
     }
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   if (taken > 0) {
     for_items(taken,
               [&](int s, int e) -> Entry {
-                return {a.table + (int64_t)s * a.per_seq + e, a.table[(int64_t)a.parent[s] * a.per_seq + e]};
+                return {a.table + (uint32_t)(s * a.per_seq + e), a.table[(uint32_t)(a.parent[s] * a.per_seq + e)]};
               },
               [&](const Entry& x) {
                 const bool is = a.is_page(x.page);
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
     __syncthreads();
     for_items(given,
               [&](int s, int i) -> Entry {
-                int32_t* at = a.table + (int64_t)s * a.per_seq + a.pages_of(after(s, a.n_new[s])) + i;
+                int32_t* at = a.table + (uint32_t)(s * a.per_seq + a.pages_of(after(s, a.n_new[s])) + i);
                 return {at, *at};
               },
               [&](const Entry& x) {
@@ -213,28 +213,29 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   __syncthreads();
   auto entry_of = [&](int r) {
     const int s = first_beyond(upto, a.S, r);
-    return a.table + (int64_t)s * a.per_seq + a.pages_of(rows[s]) + (r - (s > 0 ? upto[s - 1] : 0));
+    return a.table + (uint32_t)(s * a.per_seq + a.pages_of(rows[s]) + (r - (s > 0 ? upto[s - 1] : 0)));
   };
-  // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.  Few at first:
-  // most calls need few pages.
+  // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.  Few runs at
+  // first: most calls need few pages (64 tokens, 5 pages of 16384: 1.7 us with two runs for each wavefront, 5.8 with eight).
   int found = 0;                                        // free pages so far
   constexpr int RUN = WAVE * 4;
-  int loads = PL_FIRST_LOADS;
-  for (int p0 = 0; p0 < a.n_pages && found < wanted; p0 += loads * PL_WAVES * RUN, loads = PL_LOADS) {
+  for (int p0 = 0, loads = PL_FIRST_LOADS; p0 < a.n_pages && found < wanted;) {
+    const int left = (a.n_pages - p0 + RUN - 1) / RUN - wave;   // runs that are this wavefront's
+    const int mine = max(0, min(loads, (left + PL_WAVES - 1) / PL_WAVES));
     auto first_of = [&](int k) { return p0 + (k * PL_WAVES + wave) * RUN; };
-    uint32_t bits[PL_LOADS / 8];                          // four pages of a load each
+    uint32_t bits[PL_LOADS / 8];                          // four pages of a run each
 #pragma unroll
     for (int g = 0; g < PL_LOADS / 8; ++g) {
       bits[g] = 0;
-      if (g * 8 >= loads) continue;
       int4 c[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        if (g * 8 + j >= mine) continue;                // wave-uniform, as below
         const int p = first_of(g * 8 + j) + lane * 4;
-        c[j] = make_int4(1, 1, 1, 1);
         if (p + 3 < a.n_pages) {
           c[j] = *reinterpret_cast<const int4*>(a.refs + p);
         } else {
+          c[j] = make_int4(1, 1, 1, 1);
           if (p < a.n_pages) c[j].x = a.refs[p];
           if (p + 1 < a.n_pages) c[j].y = a.refs[p + 1];
           if (p + 2 < a.n_pages) c[j].z = a.refs[p + 2];
@@ -242,6 +243,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
+        if (g * 8 + j >= mine) continue;
         const bool f[4] = {c[j].x == 0, c[j].y == 0, c[j].z == 0, c[j].w == 0};
         int n = 0;
 #pragma unroll
@@ -252,23 +254,26 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
         if (lane == 0) free_upto[(g * 8 + j) * PL_WAVES + wave] = n;
       }
     }
+    if (lane == 0)
+      for (int k = mine; k < loads; ++k) free_upto[k * PL_WAVES + wave] = 0;
     __syncthreads();
-    const bool mine = tid < loads * PL_WAVES;
-    int n = mine ? free_upto[tid] : 0, zero = 0;
+    const bool run = tid < loads * PL_WAVES;
+    int n = run ? free_upto[tid] : 0, zero = 0;
+    const int n_run = n;
     scan_two(n, zero, found, unused, tmp);
-    if (mine) free_upto[tid] = n;
+    if (run) free_upto[tid] = n - n_run;                // before the run
     __syncthreads();
 #pragma unroll
     for (int g = 0; g < PL_LOADS / 8; ++g) {
-      if (g * 8 >= loads) continue;
+      if (g * 8 >= mine) continue;
 #pragma unroll 1
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < min(8, mine - g * 8); ++j) {
         const int k = g * 8 + j;
+        int r = __builtin_amdgcn_readfirstlane(free_upto[k * PL_WAVES + wave]);
+        if (r >= wanted) break;
         const uint32_t four = (bits[g] >> (4 * j)) & 15u;
-        const int c = __popc(four), upto_lane = wave_inclusive_scan(c), all = __builtin_amdgcn_readlane(upto_lane, WAVE - 1);
-        int r = __builtin_amdgcn_readfirstlane(free_upto[k * PL_WAVES + wave]) - all;
-        if (all == 0 || r >= wanted) continue;          // wave-uniform
-        r += upto_lane - c;
+        const int c = __popc(four);
+        r += wave_inclusive_scan(c) - c;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if (!((four >> i) & 1)) continue;
@@ -282,6 +287,8 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       }
     }
     __syncthreads();                                    // free_upto is read no more
+    p0 += loads * PL_WAVES * RUN;
+    loads = PL_LOADS;
   }
   for (int r = found + tid; r < wanted; r += PL_THREADS) *entry_of(r) = -1;
   int none = 0;

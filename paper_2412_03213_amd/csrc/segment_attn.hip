@@ -21,7 +21,8 @@ constexpr int SG_EXTRA = 512;                           // pieces that are more 
 constexpr int SG_FEW = 16;                              // queries that stream rows instead of sharing tiles
 constexpr int SG_ROW = D + 4;                           // floats of a query row in a piece's results, see Partial
 constexpr int SG_PLAN_THREADS = 1024, SG_PLAN_WAVES = SG_PLAN_THREADS / 64;
-constexpr int SG_MODEL_UNITS = 2048;                    // units for which several cuts are compared
+constexpr int SG_MODEL_UNITS = SG_PLAN_THREADS;         // units for which several cuts are compared
+constexpr int SG_TRIES = 8;                             // of them
 constexpr int SG_CLASSES = 8;                           // of pieces, by how long they take
 
 // A piece of a block, as the planning workgroup hands it out.
@@ -153,6 +154,7 @@ __device__ __forceinline__ void scan_three(int (&x)[3], int (&before)[3], int4* 
 template <int G, bool SHARED>
 __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentArgs a) {
   __shared__ int2 held[SG_MODEL_UNITS];                 // tiles, tokens
+  __shared__ int tried[SG_TRIES][SG_MODEL_UNITS];       // pieces of the units
   __shared__ int4 tmp[SG_PLAN_WAVES];
   __shared__ float2 sums[SG_PLAN_WAVES];
   __shared__ int upto[SG_PLAN_THREADS];                 // pieces of blocks, up to and with a unit
@@ -194,40 +196,46 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
   work = all_sum(work);
   const float least = fmaxf(work.x * (float)a.Hkv / SG_CUS, 6.f);
 
-  // ---- and how long it has to be given, so that the pieces fit: a wavefront tries one length, each a sixteenth longer ----
-  float within = least * 1.25f;
+  // ---- and how long it has to be given, so that the pieces fit: a wavefront tries one length ----
+  float within = least * 1.25f, extra = 0.f;            // extra: pieces that are more than blocks
+  int winner = 0;
   if (model) {
-    const float mine = least * (1.f + (float)wave / 16.f);
+    auto length_of = [&](int w) { return least * (w < 4 ? 1.f + (float)w / 16.f : (float)(w + 1) / 4.f); };
     float2 need = make_float2(0.f, 0.f);
-    for (int i = lane; i < n_units; i += WAVE) {
-      const int2 u = held[i];
-      need.x += choose<SHARED>(u.x, (u.y + U::TOKENS - 1) / U::TOKENS, min(u.y * G, AT_ROWS), a.Hkv, mine).units;
+    if (wave < SG_TRIES) {
+      const float mine = length_of(wave);
+      for (int i = lane; i < n_units; i += WAVE) {
+        const int2 u = held[i];
+        const int blocks = (u.y + U::TOKENS - 1) / U::TOKENS;
+        const Choice c = choose<SHARED>(u.x, blocks, min(u.y * G, AT_ROWS), a.Hkv, mine);
+        need = make_float2(need.x + c.units, need.y + (float)max(0, c.pieces - 1) * (float)blocks);
+        tried[wave][i] = c.pieces;
+      }
+      need = make_float2(wave_sum(need.x), wave_sum(need.y));
     }
-    need.x = wave_sum(need.x);
-    __syncthreads();
+    __syncthreads();                                    // sums may still be in use
     if (lane == 0) sums[wave] = need;
     __syncthreads();
-    within = least * 2.f;
+    winner = SG_TRIES - 1;
 #pragma unroll
-    for (int w = SG_PLAN_WAVES - 1; w >= 0; --w)
-      if (sums[w].x <= (float)SG_CUS) within = least * (1.f + (float)w / 16.f);
+    for (int w = SG_TRIES - 1; w >= 0; --w) winner = sums[w].x <= (float)SG_CUS ? w : winner;
+    within = length_of(winner);
+    extra = sums[winner].y;
   }
 
   // ---- pieces of every unit, unless they are too many: then at least an even share each ----
   auto chosen = [&](const Unit& u) {
     return choose<SHARED>(u.tiles(), U::blocks(u), min(u.tokens * G, AT_ROWS), a.Hkv, within).pieces;
   };
-  float2 extra = make_float2(0.f, 0.f);
-  int first_pieces = 0;
-  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
-    if (i0 + wave * WAVE >= n_units) break;             // wave-uniform
-    const Unit u = i0 == 0 ? first : units.load(i0 + tid);
-    const int n = chosen(u);
-    if (i0 == 0) first_pieces = n;
-    extra.x += (float)max(0, n - 1) * (float)U::blocks(u);
+  if (!model) {
+    float2 sum = make_float2(0.f, 0.f);
+    for (int i = tid; i < n_units; i += SG_PLAN_THREADS) {
+      const Unit u = units.load(i);
+      sum.x += (float)max(0, chosen(u) - 1) * (float)U::blocks(u);
+    }
+    extra = all_sum(sum).x;
   }
-  extra = all_sum(extra);
-  const bool shares = extra.x * (float)a.Hkv > SG_EXTRA;
+  const bool shares = extra * (float)a.Hkv > SG_EXTRA;
   const int length = max(SG_MIN_TILES, (int)fminf(ceilf(work.y * (float)a.Hkv / SG_CUS), 1e9f));   // tiles
 
   // ---- numbers of pieces, rows of results and joins before each unit ----
@@ -240,7 +248,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       if (shares)
         n = max(SHARED ? 0 : 1, (u.tiles() + length - 1) / length);
       else
-        n = i0 == 0 ? first_pieces : chosen(u);
+        n = model ? tried[winner][i] : chosen(u);
     }
     const int blocks = U::blocks(u);
     const bool stored = SHARED || n > 1;
@@ -252,15 +260,6 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
     const int result = sum[1] - mine[1];
     cut[tid] = make_int2(n, stored ? result : -1);
     if (tid < SG_CLASSES) class_at[tid] = 0;
-    if constexpr (SHARED) {
-      if (i < n_units) a.joins[i] = {u.begin, u.tokens, n, result, u.tokens, {}};
-    } else {
-      for (int b = 0; b < mine[2]; ++b) {
-        const int at = sum[2] - mine[2] + b;
-        if (at < a.most_joins)
-          a.joins[at] = {u.begin + b * U::TOKENS, min(U::TOKENS, u.tokens - b * U::TOKENS), n, result + b * U::TOKENS, u.tokens, {}};
-      }
-    }
     __syncthreads();
     // Pieces of the chunk.  The blocks of a piece come one after the other: they read the same rows.
     const int here = before[0] - pieces_before, in_chunk = min(SG_PLAN_THREADS, n_units - i0);
@@ -275,7 +274,8 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       const Unit v = chunk[s];
       const int k = x - (s > 0 ? upto[s - 1] : 0), n_blocks = max(1, U::blocks(v)), n_pieces = max(1, cut[s].x);
       const int piece = min(k / n_blocks, n_pieces - 1), block = k - k / n_blocks * n_blocks, tiles = v.tiles();
-      const int from = (int)((int64_t)tiles * piece / n_pieces), to = (int)((int64_t)tiles * (piece + 1) / n_pieces);
+      const int each = tiles / n_pieces, more = tiles - each * n_pieces;   // the first ones have one more
+      const int from = piece * each + min(piece, more);
       Piece p;
       p.t0 = v.begin + block * U::TOKENS;
       p.n_tok = (short)min(U::TOKENS, v.tokens - block * U::TOKENS);
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       p.lo = v.lo;
       p.end = v.end;
       p.row = v.row0() + from * AT_TILE;
-      p.n_tiles = to - from;
+      p.n_tiles = each + (piece < more ? 1 : 0);
       p.result = cut[s].y < 0 ? -1 : cut[s].y + piece * v.tokens + block * U::TOKENS;
       return p;
     };
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       const float share = (float)p.n_tiles * tile_cost(p.n_tok * G, p.flags & Piece::SEVERAL ? 2 : 1) / within;
       return max(0, min(SG_CLASSES - 1, SG_CLASSES - 1 - (int)(share * SG_CLASSES)));
     };
-    if (here > SG_CUS / a.Hkv && n_units <= SG_PLAN_THREADS && here <= SG_PLAN_THREADS) {
+    if (here > SG_CUS / a.Hkv && model && here <= SG_PLAN_THREADS) {
       Piece p;
       int c = 0, rank = 0;
       if (tid < here) {
@@ -309,7 +309,16 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       for (int x = tid; x < here; x += SG_PLAN_THREADS)
         if (pieces_before + x < a.most_pieces) a.pieces[pieces_before + x] = piece_of(x);
     }
-    __syncthreads();
+    if constexpr (SHARED) {
+      if (i < n_units) a.joins[i] = {u.begin, u.tokens, n, result, u.tokens, {}};
+    } else {
+      for (int b = 0; b < mine[2]; ++b) {
+        const int at = sum[2] - mine[2] + b;
+        if (at < a.most_joins)
+          a.joins[at] = {u.begin + b * U::TOKENS, min(U::TOKENS, u.tokens - b * U::TOKENS), n, result + b * U::TOKENS, u.tokens, {}};
+      }
+    }
+    if (i0 + SG_PLAN_THREADS < n_units) __syncthreads();
   }
   if (tid == 0) *a.counts = {min(before[0], a.most_pieces), min(before[2], a.most_joins)};
 }
@@ -719,7 +728,7 @@ hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv
   } else {
     const int64_t parts = space.joins * dm.Hkv * (AT_ROWS / SG_JOIN_ROWS);
     const bool cut = a.pages.rows > 2 * SG_MIN_TILES * AT_TILE - AT_TILE;   // otherwise no unit is
-    launch_segments_all<false>(dm.G, groups, cut ? (unsigned)(parts < 8 * SG_CUS ? parts : 8 * SG_CUS) : 0, eights, a, st);
+    launch_segments_all<false>(dm.G, groups, cut ? (unsigned)(parts < 4 * SG_CUS ? parts : 4 * SG_CUS) : 0, eights, a, st);
   }
   return hipGetLastError();
 }
