@@ -690,7 +690,9 @@ int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_st
  *              Any numbers, also within a page; taken as at least 0 and at most lengths[s].
  * workspace    ck_workspace_bytes(sh, CK_WS_SHARED_ATTN, 0, 0); calls that share one must be ordered (its contents
  *              on entry do not matter).
- * CK_BF16: products as in ck_prompt_attn.  CK_F32 (check mode): every sequence reads its own table.
+ * CK_BF16: products as in ck_prompt_attn.  Where S times the rows that the table has room for are few (160 MB of keys and
+ * values) every sequence reads all of its rows through its own table, with the products of ck_paged_decode_attn; so it
+ * does in CK_F32 (check mode).
  * Lengths, groups and tables are read on the device: a captured call may be replayed with others.  The order of the
  * sums depends on the lengths of the whole batch.
  */

@@ -200,6 +200,14 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.host_copy_rows = _host("copy_rows")
     lib.copy_rows_entry = ctypes.cast(lib.ck_copy_rows, P).value
     lib.paged_decode_attn_entry = ctypes.cast(lib.ck_paged_decode_attn, P).value
+    lib.host_plan_pages = _host("plan_pages")
+    lib.plan_pages_entry = ctypes.cast(lib.ck_plan_pages, P).value
+    lib.host_store_rows = _host("store_rows")
+    lib.store_rows_entry = ctypes.cast(lib.ck_store_rows, P).value
+    lib.host_shared_decode_attn = _host("shared_decode_attn")
+    lib.shared_decode_attn_entry = ctypes.cast(lib.ck_shared_decode_attn, P).value
+    lib.host_cross_attn = _host("cross_attn")
+    lib.cross_attn_entry = ctypes.cast(lib.ck_cross_attn, P).value
     _lib = lib
     return lib
 
@@ -747,6 +755,12 @@ def ck_plan_pages(sh: Shape, n_new, lengths, page_table, page_refs, page_size: i
     place; q_starts, lacking [1] and slots (None: not asked for) are written."""
     lib = load_library()
     dev, stream = _device(n_new), _stream(n_new)
+    rc = lib.host_plan_pages(lib.plan_pages_entry, sh, n_new, lengths, page_table, page_refs, page_size,
+                             q_starts, lacking, slots, parent, shared_rows, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return
     if not all(isinstance(t, torch.Tensor) and t.dim() == d for t, d in ((page_table, 2), (page_refs, 1))):
         raise ValueError("page_table must be int32 [S, pages_per_seq], page_refs int32 [n_pages]")
     width, pages, n = page_table.shape[1], page_refs.shape[0], 0 if slots is None else slots.shape[0]
@@ -766,6 +780,11 @@ def ck_store_rows(sh: Shape, k, v, slots, kv):
     """k, v: token rows [n, Hkv, d], views of one projection's output among them; slots int32 [n]."""
     lib = load_library()
     dev, stream = _device(k), _stream(k)
+    rc = lib.host_store_rows(lib.store_rows_entry, sh, kv, k, v, slots, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return
     n = k.shape[0] if isinstance(k, torch.Tensor) else sh.S
     kp, ks = _rows(k, "k", n, sh.Hkv, sh, dev)
     vp, vs = _rows(v, "v", n, sh.Hkv, sh, dev)
@@ -793,6 +812,12 @@ def ck_shared_decode_attn(sh: Shape, q, kv, lengths, group_starts, shared_rows, 
     if workspace is None:
         workspace = shared_decode_workspace(sh, q.device)
     dev, stream = _device(q), _stream(q)
+    rc = lib.host_shared_decode_attn(lib.shared_decode_attn_entry, sh, kv, q, lengths, group_starts, shared_rows,
+                                     out, workspace, softmax_scale, stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return workspace
     groups = group_starts.shape[0] - 1 if isinstance(group_starts, torch.Tensor) else 1
     ws, ws_bytes = _scratch(workspace, dev)
     _check(lib.ck_shared_decode_attn(ctypes.byref(sh.c()), _dense(q, "q", sh.S, sh, dev), _kv(sh, kv, dev),
@@ -812,6 +837,12 @@ def ck_cross_attn(sh: Shape, q, q_starts, kv, lengths, out, softmax_scale=None, 
     if workspace is None:
         workspace = cross_workspace(sh, n, q.device)
     dev, stream = _device(q), _stream(q)
+    rc = lib.host_cross_attn(lib.cross_attn_entry, sh, kv, q, q_starts, lengths, out, workspace, softmax_scale,
+                             stream)
+    if rc is not None:
+        if rc != 0:
+            _check(rc)
+        return workspace
     ws, ws_bytes = _scratch(workspace, dev)
     _check(lib.ck_cross_attn(ctypes.byref(sh.c()), _dense(q, "q", n, sh, dev), n,
                              _ints(q_starts, "q_starts", (sh.S + 1,), dev), _kv(sh, kv, dev),

@@ -1094,7 +1094,7 @@ int ck_shared_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* 
   if (q == out) return fail(CK_EINVALID, "out is q");
   if ((rc = check_paged(kv, "kv", dm, dm.S))) return rc;
   if ((rc = check_workspace(workspace, workspace_bytes, shared_bytes(dm)))) return rc;
-  if (dm.dtype != CK_BF16)                              // check mode: every sequence reads its own table
+  if (ck::shared_reads_each(dm, *kv))                   // little to share, and the check mode: through its own table
     return hip_result(ck::launch_paged_attn(dm, q, *kv, lengths, 0, -1, nullptr, nullptr, 0, 0, softmax_scale, out,
                                             workspace, (hipStream_t)stream),
                       "paged attention launch");

@@ -407,6 +407,7 @@ hipError_t launch_cross_attn(const Dims& dm, const void* q, int64_t n_rows, cons
                              const ck_paged_kv& kv, const int32_t* lengths, float softmax_scale, void* out,
                              void* workspace, hipStream_t st);
 size_t shared_workspace_bytes(const Dims& dm);
+bool shared_reads_each(const Dims& dm, const ck_paged_kv& kv);   // ck_shared_decode_attn as the attention of single tokens
 hipError_t launch_shared_attn(const Dims& dm, const void* q, const ck_paged_kv& kv, const int32_t* lengths,
                               int n_groups, const int32_t* group_starts, const int32_t* shared_rows,
                               float softmax_scale, void* out, void* workspace, hipStream_t st);

@@ -1,5 +1,5 @@
 // The calls that are made once per layer and step, for the Python binding without ctypes in between:
-// ck_decode_step and the four on caches in pages.
+// ck_decode_step and those on caches in pages.
 //
 // ck_decode_step is made once per layer and generated token, and at small batches its marshalling (fifteen tensors, two method
 // calls and two ctypes conversions each) took longer than the kernel: 9.9 us from call to call
@@ -340,6 +340,123 @@ PyObject* copy_rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
   return PyLong_FromLong(rc);
 }
 
+// plan_pages(entry, shape, n_new, lengths, page_table, page_refs, page_size, q_starts, lacking, slots, parent, shared_rows,
+//            stream)
+PyObject* plan_pages(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 13) {
+    PyErr_SetString(PyExc_TypeError, "plan_pages: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  int64_t stream, table_size[2], n_pages, n_rows = 0;
+  int32_t page_size;
+  void *n_new, *lengths, *table, *refs, *starts, *lacking, *slots = nullptr, *parent, *shared;
+  if (!types[0] || !as_int(a[0], &c.entry) || c.entry == 0 || !as_shape(a[1], &c.sh) || a[2] == Py_None ||
+      PyLong_Check(a[2]) || !as_device(a[2], &c.device) || !as_tuple(PyObject_GetAttr(a[4], s_size), 2, table_size) ||
+      !as_tuple(PyObject_GetAttr(a[5], s_size), 1, &n_pages) ||
+      (a[9] != Py_None && !as_tuple(PyObject_GetAttr(a[9], s_size), 1, &n_rows)))
+    return not_plain();
+  if (table_size[1] > INT32_MAX || n_pages > INT32_MAX || (a[9] != Py_None && n_rows == 0)) return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t per_seq[1] = {sh.S}, n_starts[1] = {(int64_t)sh.S + 1}, one[1] = {1}, entries[2] = {sh.S, table_size[1]};
+  PyObject* const i32 = types[INT32];
+  const bool ok = as_dense(c, a[2], i32, 1, per_seq, &n_new) && as_dense(c, a[3], i32, 1, per_seq, &lengths) &&
+                  as_dense(c, a[4], i32, 2, entries, &table) && as_dense(c, a[5], i32, 1, &n_pages, &refs) &&
+                  as_i32(a[6], &page_size) && as_dense(c, a[7], i32, 1, n_starts, &starts) &&
+                  as_dense(c, a[8], i32, 1, one, &lacking) && as_dense(c, a[9], i32, 1, &n_rows, &slots, true) &&
+                  as_dense(c, a[10], i32, 1, per_seq, &parent, true) &&
+                  as_dense(c, a[11], i32, 1, per_seq, &shared, true) && as_int(a[12], &stream);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_plan_pages)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, (const int32_t*)n_new, (int32_t*)lengths, (int32_t*)table, (int32_t)table_size[1], (int32_t*)refs,
+          (int32_t)n_pages, page_size, (const int32_t*)parent, (const int32_t*)shared, (int32_t*)starts, (int32_t*)slots,
+          n_rows, (int32_t*)lacking, reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// store_rows(entry, shape, cache, k, v, slots, stream)
+PyObject* store_rows(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 7) {
+    PyErr_SetString(PyExc_TypeError, "store_rows: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  int64_t stream, size[3], s_k, s_v;
+  void *k, *v, *slots;
+  if (!as_call(a, a[3], &c) || !as_tuple(PyObject_GetAttr(a[3], s_size), 3, size)) return not_plain();
+  const int64_t rows[3] = {size[0], c.sh.Hkv, c.sh.d}, per_row[1] = {size[0]};
+  const bool ok = as_rows(c, a[3], rows, &k, &s_k) && as_rows(c, a[4], rows, &v, &s_v) &&
+                  as_dense(c, a[5], types[INT32], 1, per_row, &slots) && as_int(a[6], &stream);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_store_rows)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&c.sh, k, v, s_k, s_v, size[0], (const int32_t*)slots, c.kv,
+          reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// shared_decode_attn(entry, shape, cache, q, lengths, group_starts, shared_rows, out, workspace, scale, stream)
+PyObject* shared_decode_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 11) {
+    PyErr_SetString(PyExc_TypeError, "shared_decode_attn: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  int64_t stream, n_starts, ws_bytes;
+  void *q, *lengths, *starts, *shared, *out, *ws;
+  double scale;
+  if (!as_call(a, a[3], &c) || !as_tuple(PyObject_GetAttr(a[5], s_size), 1, &n_starts) ||
+      !as_tuple(PyObject_GetAttr(a[8], s_size), 1, &ws_bytes) || n_starts < 1 || n_starts > INT32_MAX)
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t rows[3] = {sh.S, sh.Hq, sh.d}, per_seq[1] = {sh.S};
+  const bool ok = as_dense(c, a[3], c.type, 3, rows, &q) && as_dense(c, a[4], types[INT32], 1, per_seq, &lengths) &&
+                  as_dense(c, a[5], types[INT32], 1, &n_starts, &starts) &&
+                  as_dense(c, a[6], types[INT32], 1, per_seq, &shared) && as_dense(c, a[7], c.type, 3, rows, &out) &&
+                  as_dense(c, a[8], types[UINT8], 1, &ws_bytes, &ws) && as_float(a[9], &scale) && as_int(a[10], &stream);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_shared_decode_attn)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, q, c.kv, (const int32_t*)lengths, (int32_t)(n_starts - 1), (const int32_t*)starts, (const int32_t*)shared,
+          (float)scale, out, ws, (size_t)ws_bytes, reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+// cross_attn(entry, shape, cache, q, q_starts, lengths, out, workspace, scale, stream)
+PyObject* cross_attn(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 10) {
+    PyErr_SetString(PyExc_TypeError, "cross_attn: wrong number of arguments");
+    return nullptr;
+  }
+  Common c;
+  int64_t stream, size[3], ws_bytes;
+  void *q, *starts, *lengths, *out, *ws;
+  double scale;
+  if (!as_call(a, a[3], &c) || !as_tuple(PyObject_GetAttr(a[3], s_size), 3, size) ||
+      !as_tuple(PyObject_GetAttr(a[7], s_size), 1, &ws_bytes))
+    return not_plain();
+  const ck_shape& sh = c.sh;
+  const int64_t rows[3] = {size[0], sh.Hq, sh.d}, n_starts[1] = {(int64_t)sh.S + 1}, per_seq[1] = {sh.S};
+  const bool ok = as_dense(c, a[3], c.type, 3, rows, &q) && as_dense(c, a[4], types[INT32], 1, n_starts, &starts, true) &&
+                  as_dense(c, a[5], types[INT32], 1, per_seq, &lengths) && as_dense(c, a[6], c.type, 3, rows, &out) &&
+                  as_dense(c, a[7], types[UINT8], 1, &ws_bytes, &ws) && as_float(a[8], &scale) && as_int(a[9], &stream);
+  if (!ok) return not_plain();
+  const auto fn = reinterpret_cast<decltype(&ck_cross_attn)>(static_cast<uintptr_t>(c.entry));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = fn(&sh, q, size[0], (const int32_t*)starts, c.kv, (const int32_t*)lengths, (float)scale, out, ws, (size_t)ws_bytes,
+          reinterpret_cast<void*>(static_cast<uintptr_t>(stream)));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
 #define CK_METHOD(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
     {"decode_step", CK_METHOD(decode_step), "ck_decode_step on plain tensors; None if an argument is of another kind"},
@@ -347,6 +464,10 @@ PyMethodDef methods[] = {
     {"paged_decode_attn", CK_METHOD(paged_decode_attn), "ck_paged_decode_attn, likewise"},
     {"prompt_attn", CK_METHOD(prompt_attn), "ck_prompt_attn, likewise"},
     {"copy_rows", CK_METHOD(copy_rows), "ck_copy_rows, likewise"},
+    {"plan_pages", CK_METHOD(plan_pages), "ck_plan_pages, likewise"},
+    {"store_rows", CK_METHOD(store_rows), "ck_store_rows, likewise"},
+    {"shared_decode_attn", CK_METHOD(shared_decode_attn), "ck_shared_decode_attn, likewise"},
+    {"cross_attn", CK_METHOD(cross_attn), "ck_cross_attn, likewise"},
     {"set_types", CK_METHOD(set_types), "torch's bfloat16, float32, int32 and uint8"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ckhost", nullptr, -1, methods,

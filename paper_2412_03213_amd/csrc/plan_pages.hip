@@ -13,12 +13,16 @@ namespace ck {
 
 namespace {
 
-constexpr int PL_THREADS = 1024, PL_WAVES = PL_THREADS / 64;
-constexpr int PL_LOADS = 32, PL_FIRST_LOADS = 2;        // of 4 counts a lane, for the pages that are looked at together
+// Threads of the planning workgroup.  Prefix sums are done by every wavefront for itself, over all of them: four are done
+// sooner where there are few sequences and the table is small: a token for each of 64 sequences 6.8 us, not 7.6; 16500 pages
+// given back 53, not 30.
+constexpr int PL_FEW = 256, PL_MANY = 1024, PL_FEW_ENTRIES = 16384;
+constexpr int PL_LOADS = 32;                            // runs of 256 pages that a wavefront looks at together, at most
+constexpr int PL_FIRST_RUNS = 32;                       // ... and the workgroup to begin with
 constexpr int PL_ITEMS = 4;                             // of a thread at a time
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
 constexpr int PL_OWN_ROWS = 8192;
-constexpr int PL_SLOT_ROWS = PL_THREADS;                // of a workgroup of that launch
+constexpr int PL_SLOT_ROWS = PL_MANY;                // of a workgroup of that launch
 
 struct PlanArgs {
   const int32_t *n_new, *parent, *shared_rows;
@@ -33,6 +37,7 @@ struct PlanArgs {
 };
 
 // Inclusive prefix sums over the workgroup of two numbers a thread, with what earlier chunks left; tmp: LDS.
+template <int WAVES>
 __device__ __forceinline__ void scan_two(int& x, int& y, int& x_before, int& y_before, int2* tmp) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   x = wave_inclusive_scan(x);
@@ -42,7 +47,7 @@ __device__ __forceinline__ void scan_two(int& x, int& y, int& x_before, int& y_b
   __syncthreads();
   int2 mine = make_int2(x_before, y_before), all = mine;
 #pragma unroll
-  for (int w = 0; w < PL_WAVES; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const int2 t = tmp[w];
     if (w < wave) mine = make_int2(mine.x + t.x, mine.y + t.y);
     all = make_int2(all.x + t.x, all.y + t.y);
@@ -98,12 +103,14 @@ __device__ __forceinline__ void memory_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
-__global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
+  constexpr int WAVES = THREADS / 64;
   extern __shared__ int lds[];
   int* const rows = lds;                                // [S]: of every sequence, before it gives back or gets tokens
   int* const upto = lds + a.S;                          // [S]: prefix sums
-  __shared__ int2 tmp[PL_WAVES];
-  __shared__ int free_upto[PL_LOADS * PL_WAVES];        // free pages of a run; then up to its end
+  __shared__ int2 tmp[WAVES];
+  __shared__ int free_upto[PL_LOADS * WAVES];                    // free pages of a run; then before it
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ps = (int)a.size.d;
   auto after = [&](int s, int n) {                      // rows of a sequence after the call
@@ -113,24 +120,24 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   // Items of all sequences, numbered through upto[]: get(sequence, item of it) asks for what put takes.  Several at a
   // time: an item is a chain of look-ups, one after the other.
   auto for_items = [&](int total, auto get, auto put) {
-    for (int r0 = tid; r0 < total; r0 += PL_ITEMS * PL_THREADS) {
+    for (int r0 = tid; r0 < total; r0 += PL_ITEMS * THREADS) {
       decltype(get(0, 0)) x[PL_ITEMS];
       int r[PL_ITEMS], s[PL_ITEMS];
 #pragma unroll
-      for (int u = 0; u < PL_ITEMS; ++u) r[u] = min(r0 + u * PL_THREADS, total - 1);   // the last one again behind the end
+      for (int u = 0; u < PL_ITEMS; ++u) r[u] = min(r0 + u * THREADS, total - 1);   // the last one again behind the end
       first_beyond<PL_ITEMS>(upto, a.S, r, s);
 #pragma unroll
       for (int u = 0; u < PL_ITEMS; ++u) x[u] = get(s[u], r[u] - (s[u] > 0 ? upto[s[u] - 1] : 0));
 #pragma unroll
       for (int u = 0; u < PL_ITEMS; ++u)
-        if (r0 + u * PL_THREADS < total) put(x[u]);
+        if (r0 + u * THREADS < total) put(x[u]);
     }
   };
   struct Entry { int32_t* at; int page; };
 
   // ---- sequences without rows take over whole pages of a parent, as it stands before the call ----
   int taken = 0, unused = 0, less = 0;
-  for (int s0 = 0; s0 < a.S; s0 += PL_THREADS) {
+  for (int s0 = 0; s0 < a.S; s0 += THREADS) {
     const int s = s0 + tid;
     int pages = 0, zero = 0;
     if (s < a.S) {
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       rows[s] = old + pages * ps;
     }
     if (a.parent) {
-      scan_two(pages, zero, taken, unused, tmp);
+      scan_two<WAVES>(pages, zero, taken, unused, tmp);
       if (s < a.S) upto[s] = pages;
     }
   }
@@ -167,12 +174,12 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   // ---- pages that hold no row any more are given back ----
   if (less) {
     int given = 0;
-    for (int s0 = 0; s0 < a.S; s0 += PL_THREADS) {
+    for (int s0 = 0; s0 < a.S; s0 += THREADS) {
       const int s = s0 + tid;
       int n = 0, zero = 0;
       if (s < a.S && a.n_new[s] < 0)
         n = max(0, min(a.pages_of(rows[s]), a.per_seq) - a.pages_of(after(s, a.n_new[s])));
-      scan_two(n, zero, given, unused, tmp);
+      scan_two<WAVES>(n, zero, given, unused, tmp);
       if (s < a.S) upto[s] = n;
     }
     __syncthreads();
@@ -190,7 +197,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
 
   // ---- pages for new rows ----
   int wanted = 0, tokens = 0, behind = 0;               // behind: pages that the table has no entry for
-  for (int s0 = 0; s0 < a.S; s0 += PL_THREADS) {
+  for (int s0 = 0; s0 < a.S; s0 += THREADS) {
     const int s = s0 + tid;
     int n = 0, add = 0;
     if (s < a.S) {
@@ -203,7 +210,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       }
       a.lengths[s] = now;
     }
-    scan_two(n, add, wanted, tokens, tmp);
+    scan_two<WAVES>(n, add, wanted, tokens, tmp);
     if (s < a.S) {
       upto[s] = n;
       a.q_starts[s + 1] = add;
@@ -219,10 +226,10 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
   // first: most calls need few pages (64 tokens, 5 pages of 16384: 1.7 us with two runs for each wavefront, 5.8 with eight).
   int found = 0;                                        // free pages so far
   constexpr int RUN = WAVE * 4;
-  for (int p0 = 0, loads = PL_FIRST_LOADS; p0 < a.n_pages && found < wanted;) {
+  for (int p0 = 0, loads = PL_FIRST_RUNS / WAVES; p0 < a.n_pages && found < wanted;) {
     const int left = (a.n_pages - p0 + RUN - 1) / RUN - wave;   // runs that are this wavefront's
-    const int mine = max(0, min(loads, (left + PL_WAVES - 1) / PL_WAVES));
-    auto first_of = [&](int k) { return p0 + (k * PL_WAVES + wave) * RUN; };
+    const int mine = max(0, min(loads, (left + WAVES - 1) / WAVES));
+    auto first_of = [&](int k) { return p0 + (k * WAVES + wave) * RUN; };
     uint32_t bits[PL_LOADS / 8];                          // four pages of a run each
 #pragma unroll
     for (int g = 0; g < PL_LOADS / 8; ++g) {
@@ -251,16 +258,16 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
           n += __popcll(__ballot(f[i]));
           bits[g] |= (uint32_t)f[i] << (4 * j + i);
         }
-        if (lane == 0) free_upto[(g * 8 + j) * PL_WAVES + wave] = n;
+        if (lane == 0) free_upto[(g * 8 + j) * WAVES + wave] = n;
       }
     }
     if (lane == 0)
-      for (int k = mine; k < loads; ++k) free_upto[k * PL_WAVES + wave] = 0;
+      for (int k = mine; k < loads; ++k) free_upto[k * WAVES + wave] = 0;
     __syncthreads();
-    const bool run = tid < loads * PL_WAVES;
+    const bool run = tid < loads * WAVES;
     int n = run ? free_upto[tid] : 0, zero = 0;
     const int n_run = n;
-    scan_two(n, zero, found, unused, tmp);
+    scan_two<WAVES>(n, zero, found, unused, tmp);
     if (run) free_upto[tid] = n - n_run;                // before the run
     __syncthreads();
 #pragma unroll
@@ -269,7 +276,7 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
 #pragma unroll 1
       for (int j = 0; j < min(8, mine - g * 8); ++j) {
         const int k = g * 8 + j;
-        int r = __builtin_amdgcn_readfirstlane(free_upto[k * PL_WAVES + wave]);
+        int r = __builtin_amdgcn_readfirstlane(free_upto[k * WAVES + wave]);
         if (r >= wanted) break;
         const uint32_t four = (bits[g] >> (4 * j)) & 15u;
         const int c = __popc(four);
@@ -287,28 +294,28 @@ __global__ __launch_bounds__(PL_THREADS) void k_plan_pages(const PlanArgs a) {
       }
     }
     __syncthreads();                                    // free_upto is read no more
-    p0 += loads * PL_WAVES * RUN;
+    p0 += loads * WAVES * RUN;
     loads = PL_LOADS;
   }
-  for (int r = found + tid; r < wanted; r += PL_THREADS) *entry_of(r) = -1;
+  for (int r = found + tid; r < wanted; r += THREADS) *entry_of(r) = -1;
   int none = 0;
-  scan_two(behind, none, unused, none, tmp);
-  if (tid == PL_THREADS - 1) *a.lacking = behind + max(0, wanted - found);
+  scan_two<WAVES>(behind, none, unused, none, tmp);
+  if (tid == THREADS - 1) *a.lacking = behind + max(0, wanted - found);
   if (!a.slots || a.n_rows > PL_OWN_ROWS) return;
 
   // ---- slots ----
   memory_barrier();
-  for (int s = tid; s < a.S; s += PL_THREADS) upto[s] = a.q_starts[s + 1];
+  for (int s = tid; s < a.S; s += THREADS) upto[s] = a.q_starts[s + 1];
   __syncthreads();
-  write_slots(a, upto, tid, a.n_rows, PL_THREADS);
+  write_slots(a, upto, tid, a.n_rows, THREADS);
 }
 
-__global__ __launch_bounds__(PL_THREADS) void k_plan_slots(const PlanArgs a) {
+__global__ __launch_bounds__(PL_MANY) void k_plan_slots(const PlanArgs a) {
   extern __shared__ int ends[];
-  for (int s = threadIdx.x; s < a.S; s += PL_THREADS) ends[s] = a.q_starts[s + 1];
+  for (int s = threadIdx.x; s < a.S; s += PL_MANY) ends[s] = a.q_starts[s + 1];
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * PL_SLOT_ROWS;
-  write_slots(a, ends, t0 + threadIdx.x, min(t0 + PL_SLOT_ROWS, (int64_t)a.n_rows), PL_THREADS);
+  write_slots(a, ends, t0 + threadIdx.x, min(t0 + PL_SLOT_ROWS, (int64_t)a.n_rows), PL_MANY);
 }
 
 }  // namespace
@@ -332,9 +339,12 @@ hipError_t launch_plan_pages(int S, const int32_t* n_new, int32_t* lengths, int3
   a.n_pages = n_pages;
   a.n_rows = (int)n_rows;
   a.size = Divider((uint32_t)page_size);
-  hipLaunchKernelGGL(k_plan_pages, dim3(1), dim3(PL_THREADS), (size_t)S * 2 * sizeof(int), st, a);
+  if (S <= PL_FEW && (int64_t)S * pages_per_seq <= PL_FEW_ENTRIES && n_rows <= 4 * PL_FEW)
+    hipLaunchKernelGGL(k_plan_pages<PL_FEW>, dim3(1), dim3(PL_FEW), (size_t)S * 2 * sizeof(int), st, a);
+  else
+    hipLaunchKernelGGL(k_plan_pages<PL_MANY>, dim3(1), dim3(PL_MANY), (size_t)S * 2 * sizeof(int), st, a);
   if (a.slots && n_rows > PL_OWN_ROWS)
-    hipLaunchKernelGGL(k_plan_slots, dim3((unsigned)((n_rows + PL_SLOT_ROWS - 1) / PL_SLOT_ROWS)), dim3(PL_THREADS),
+    hipLaunchKernelGGL(k_plan_slots, dim3((unsigned)((n_rows + PL_SLOT_ROWS - 1) / PL_SLOT_ROWS)), dim3(PL_MANY),
                        (size_t)S * sizeof(int), st, a);
   return hipGetLastError();
 }

@@ -20,8 +20,9 @@ constexpr int SG_MIN_TILES = 2;                         // of a piece: 16 rows f
 constexpr int SG_EXTRA = 512;                           // pieces that are more than blocks, over all heads, at most
 constexpr int SG_FEW = 16;                              // queries that stream rows instead of sharing tiles
 constexpr int SG_ROW = D + 4;                           // floats of a query row in a piece's results, see Partial
-constexpr int SG_PLAN_THREADS = 1024, SG_PLAN_WAVES = SG_PLAN_THREADS / 64;
-constexpr int SG_MODEL_UNITS = SG_PLAN_THREADS;         // units for which several cuts are compared
+// Threads of the planning workgroup, a unit each: most of its steps are done by every wavefront for itself (sums over all
+// of them), which four do in 4.2 us, sixteen in 6.
+constexpr int SG_FEW_UNITS = 256, SG_MANY_UNITS = 1024;
 constexpr int SG_TRIES = 8;                             // of them
 constexpr int SG_CLASSES = 8;                           // of pieces, by how long they take
 
@@ -96,23 +97,29 @@ struct Units {
   __device__ __forceinline__ static int blocks(const Unit& u) { return (u.tokens + TOKENS - 1) / TOKENS; }
 };
 
-// What the model below goes by, in microseconds.  A tile costs a workgroup 1.2 with up to two wavefronts of queries (its
-// share of the memory) and 0.18 more with each other one, 1.8 at most where other blocks read the same rows (from L2):
-// measured on 256 workgroups at 6400 and 3200 rows, 1.19 for 16, 32 and 64 queries, 1.35, 1.6, 1.85, 2.0, 2.2 and 2.15 for 96
-// to 256.  Beginning and end of a piece take 3; a row of results 0.05, written and read.
+// What the model below goes by, in microseconds.  Beginning and end of a piece take 3, a row of results 0.08, written and
+// read.  A tile of its own for each of 256 workgroups takes 1.2 with up to two wavefronts of queries (their share of the
+// memory) and 0.18 more with each other one, 1.8 at most where other blocks read the same rows (from L2); measured: 1.19 for
+// 16, 32 and 64 queries, 1.35, 1.6, 1.85, 2.0, 2.2 and 2.15 for 96 to 256.  With few workgroups on the chip it takes 0.46 for 16
+// queries, 0.85 for 32, 1.0 for 96, 1.41 for 256.
 __device__ __forceinline__ float tile_cost(int rows, int blocks) {
   const float t = fmaf(0.18f, (float)max(0, (rows + 31) / 32 - 2), 1.2f);
   return blocks > 1 ? fminf(t, 1.8f) : t;
 }
-constexpr float SG_PIECE_COST = 3.f, SG_ROW_COST = 0.05f;
+__device__ __forceinline__ float tile_cost_alone(int rows) {
+  return rows <= SG_FEW ? 0.46f : fmaf(0.08f, (float)((rows + 31) / 32), 0.77f);
+}
+constexpr float SG_PIECE_COST = 3.f, SG_ROW_COST = 0.08f;
+constexpr float SG_JOIN_COST = 10.f;                    // of the join, where there is none without a cut
 
-// Into how many pieces the rows of a unit are cut so that all work takes `within`, and how many compute units that takes.
+// Into how many pieces the rows of a unit are cut so that all work takes `within`, and how many compute units that takes;
+// load: the share of that time for which the whole chip is busy.
 struct Choice { int pieces; float units; };
 template <bool SHARED>
-__device__ __forceinline__ Choice choose(int tiles, int blocks, int rows, int Hkv, float within) {
+__device__ __forceinline__ Choice choose(int tiles, int blocks, int rows, int Hkv, float within, float load) {
   Choice best = {SHARED && tiles == 0 ? 0 : 1, 0.f};
   if (blocks == 0 || tiles == 0) return best;
-  const float work = (float)tiles * tile_cost(rows, blocks), results = SG_ROW_COST * (float)rows;
+  const float work = (float)tiles * fmaxf(tile_cost_alone(rows), load * tile_cost(rows, blocks)), results = SG_ROW_COST * (float)rows;
   const int most = max(1, tiles / SG_MIN_TILES);
   const float whole = work + SG_PIECE_COST + (SHARED ? results : 0.f), room = within - SG_PIECE_COST - results;
   int n = room > 0.f ? (int)fminf(ceilf(work * __builtin_amdgcn_rcpf(room)), (float)most) : most;
@@ -123,12 +130,13 @@ __device__ __forceinline__ Choice choose(int tiles, int blocks, int rows, int Hk
     const float each = n == 1 ? whole : fmaf(work, __builtin_amdgcn_rcpf((float)n), SG_PIECE_COST + results);
     const float fit = floorf(within * __builtin_amdgcn_rcpf(each));
     const float units = fit >= 1.f ? (float)(n * blocks * Hkv) * __builtin_amdgcn_rcpf(fit) : 1e30f;
-    if (n <= most && units < best.units) best = {n, units};
+    if (n <= most && units < 0.95f * best.units) best = {n, units};   // more pieces have to spare something
   }
   return best;
 }
 
 // Inclusive prefix sums over the workgroup of three numbers a thread, with what earlier chunks left; tmp: LDS.
+template <int WAVES>
 __device__ __forceinline__ void scan_three(int (&x)[3], int (&before)[3], int4* tmp) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -138,7 +146,7 @@ __device__ __forceinline__ void scan_three(int (&x)[3], int (&before)[3], int4* 
   __syncthreads();
   int mine[3] = {before[0], before[1], before[2]};
 #pragma unroll
-  for (int w = 0; w < SG_PLAN_WAVES; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const int4 t = tmp[w];
     const int v[3] = {t.x, t.y, t.z};
 #pragma unroll
@@ -151,15 +159,17 @@ __device__ __forceinline__ void scan_three(int (&x)[3], int (&before)[3], int4* 
   for (int k = 0; k < 3; ++k) x[k] += mine[k];
 }
 
-template <int G, bool SHARED>
-__global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentArgs a) {
-  __shared__ int2 held[SG_MODEL_UNITS];                 // tiles, tokens
-  __shared__ int tried[SG_TRIES][SG_MODEL_UNITS];       // pieces of the units
-  __shared__ int4 tmp[SG_PLAN_WAVES];
-  __shared__ float2 sums[SG_PLAN_WAVES];
-  __shared__ int upto[SG_PLAN_THREADS];                 // pieces of blocks, up to and with a unit
-  __shared__ Unit chunk[SG_PLAN_THREADS];
-  __shared__ int2 cut[SG_PLAN_THREADS];                 // pieces, row of results (-1: none)
+template <int G, bool SHARED, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_segment_plan(const SegmentArgs a) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ int2 held[THREADS];                        // tiles, tokens
+  __shared__ int tried[SG_TRIES][THREADS];              // pieces of the units
+  __shared__ float2 needed[SG_TRIES];
+  __shared__ int4 tmp[WAVES];
+  __shared__ float2 sums[WAVES];
+  __shared__ int upto[THREADS];                 // pieces of blocks, up to and with a unit
+  __shared__ Unit chunk[THREADS];
+  __shared__ int2 cut[THREADS];                 // pieces, row of results (-1: none)
   __shared__ int class_at[SG_CLASSES];
   CK_FETCH_ARG(a.starts);
   CK_FETCH_ARG(a.S);
@@ -168,7 +178,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
   using U = Units<G, SHARED>;
   const U units{a};
   const int n_units = units.count();
-  const bool model = n_units <= SG_MODEL_UNITS;
+  const bool model = n_units <= THREADS;                // several cuts are compared
   auto all_sum = [&](float2 v) {
     v = make_float2(wave_sum(v.x), wave_sum(v.y));
     __syncthreads();                                    // sums may still be in use
@@ -176,18 +186,18 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
     __syncthreads();
     v = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < SG_PLAN_WAVES; ++w) v = make_float2(v.x + sums[w].x, v.y + sums[w].y);
+    for (int w = 0; w < WAVES; ++w) v = make_float2(v.x + sums[w].x, v.y + sums[w].y);
     return v;
   };
 
   // ---- how long it takes at best: all compute units busy until the end ----
   float2 work = make_float2(0.f, 0.f);                  // y: tiles
   Unit first = {};
-  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
+  for (int i0 = 0; i0 < n_units; i0 += THREADS) {
     const Unit u = units.load(i0 + tid);
     if (i0 == 0) first = u;
     const int tiles = u.tiles(), blocks = U::blocks(u), rows = min(u.tokens * G, AT_ROWS);
-    if (model) held[min(i0 + tid, SG_MODEL_UNITS - 1)] = make_int2(tiles, u.tokens);
+    if (model) held[tid] = make_int2(tiles, u.tokens);
     if (tiles > 0) {
       work.x += (float)blocks * fmaf((float)tiles, tile_cost(rows, blocks), SG_PIECE_COST + (SHARED ? SG_ROW_COST * (float)rows : 0.f));
       work.y += (float)blocks * (float)tiles;
@@ -201,35 +211,40 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
   int winner = 0;
   if (model) {
     auto length_of = [&](int w) { return least * (w < 4 ? 1.f + (float)w / 16.f : (float)(w + 1) / 4.f); };
-    float2 need = make_float2(0.f, 0.f);
-    if (wave < SG_TRIES) {
-      const float mine = length_of(wave);
+    for (int w = wave; w < SG_TRIES; w += WAVES) {
+      const float mine = length_of(w);
+      float2 need = make_float2(0.f, 0.f);
       for (int i = lane; i < n_units; i += WAVE) {
         const int2 u = held[i];
         const int blocks = (u.y + U::TOKENS - 1) / U::TOKENS;
-        const Choice c = choose<SHARED>(u.x, blocks, min(u.y * G, AT_ROWS), a.Hkv, mine);
+        const Choice c = choose<SHARED>(u.x, blocks, min(u.y * G, AT_ROWS), a.Hkv, mine, least / mine);
         need = make_float2(need.x + c.units, need.y + (float)max(0, c.pieces - 1) * (float)blocks);
-        tried[wave][i] = c.pieces;
+        tried[w][i] = c.pieces;
       }
       need = make_float2(wave_sum(need.x), wave_sum(need.y));
+      if (lane == 0) needed[w] = need;
     }
-    __syncthreads();                                    // sums may still be in use
-    if (lane == 0) sums[wave] = need;
     __syncthreads();
     winner = SG_TRIES - 1;
+    int uncut = -1;
 #pragma unroll
-    for (int w = SG_TRIES - 1; w >= 0; --w) winner = sums[w].x <= (float)SG_CUS ? w : winner;
+    for (int w = SG_TRIES - 1; w >= 0; --w) {
+      const bool fits = needed[w].x <= (float)SG_CUS;
+      winner = fits ? w : winner;
+      uncut = fits && needed[w].y == 0.f ? w : uncut;
+    }
+    if (!SHARED && uncut >= 0 && length_of(uncut) - length_of(winner) < SG_JOIN_COST) winner = uncut;
     within = length_of(winner);
-    extra = sums[winner].y;
+    extra = needed[winner].y;
   }
 
   // ---- pieces of every unit, unless they are too many: then at least an even share each ----
   auto chosen = [&](const Unit& u) {
-    return choose<SHARED>(u.tiles(), U::blocks(u), min(u.tokens * G, AT_ROWS), a.Hkv, within).pieces;
+    return choose<SHARED>(u.tiles(), U::blocks(u), min(u.tokens * G, AT_ROWS), a.Hkv, within, least / within).pieces;
   };
   if (!model) {
     float2 sum = make_float2(0.f, 0.f);
-    for (int i = tid; i < n_units; i += SG_PLAN_THREADS) {
+    for (int i = tid; i < n_units; i += THREADS) {
       const Unit u = units.load(i);
       sum.x += (float)max(0, chosen(u) - 1) * (float)U::blocks(u);
     }
@@ -240,7 +255,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
 
   // ---- numbers of pieces, rows of results and joins before each unit ----
   int before[3] = {0, 0, 0};
-  for (int i0 = 0; i0 < n_units; i0 += SG_PLAN_THREADS) {
+  for (int i0 = 0; i0 < n_units; i0 += THREADS) {
     const int i = i0 + tid, pieces_before = before[0];
     const Unit u = i0 == 0 ? first : units.load(i);
     int n = 0;
@@ -254,7 +269,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
     const bool stored = SHARED || n > 1;
     const int mine[3] = {n * blocks, stored ? n * u.tokens : 0, !SHARED && stored ? blocks : 0};
     int sum[3] = {mine[0], mine[1], mine[2]};
-    scan_three(sum, before, tmp);
+    scan_three<WAVES>(sum, before, tmp);
     upto[tid] = sum[0] - pieces_before;
     chunk[tid] = u;
     const int result = sum[1] - mine[1];
@@ -262,7 +277,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
     if (tid < SG_CLASSES) class_at[tid] = 0;
     __syncthreads();
     // Pieces of the chunk.  The blocks of a piece come one after the other: they read the same rows.
-    const int here = before[0] - pieces_before, in_chunk = min(SG_PLAN_THREADS, n_units - i0);
+    const int here = before[0] - pieces_before, in_chunk = min(THREADS, n_units - i0);
     auto piece_of = [&](int x) {
       int s = 0;
       for (int len = in_chunk - 1; len > 0;) {          // the first with upto > x
@@ -294,19 +309,27 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
       const float share = (float)p.n_tiles * tile_cost(p.n_tok * G, p.flags & Piece::SEVERAL ? 2 : 1) / within;
       return max(0, min(SG_CLASSES - 1, SG_CLASSES - 1 - (int)(share * SG_CLASSES)));
     };
-    if (here > SG_CUS / a.Hkv && model && here <= SG_PLAN_THREADS) {
-      Piece p;
-      int c = 0, rank = 0;
-      if (tid < here) {
-        p = piece_of(tid);
-        c = class_of(p);
-        rank = atomicAdd(&class_at[c], 1);
+    constexpr int EACH = SG_MANY_UNITS / THREADS;       // pieces of a thread
+    if (here > SG_CUS / a.Hkv && model && here <= SG_MANY_UNITS) {
+      Piece p[EACH];
+      int c[EACH], rank[EACH];
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        c[k] = -1;
+        if (tid + k * THREADS >= here) break;
+        p[k] = piece_of(tid + k * THREADS);
+        c[k] = class_of(p[k]);
+        rank[k] = atomicAdd(&class_at[c[k]], 1);
       }
       __syncthreads();
-      for (int k = 0; k < c; ++k) rank += class_at[k];
-      if (tid < here && rank < a.most_pieces) a.pieces[rank] = p;
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        if (c[k] < 0) break;
+        for (int i = 0; i < c[k]; ++i) rank[k] += class_at[i];
+        if (rank[k] < a.most_pieces) a.pieces[rank[k]] = p[k];
+      }
     } else {
-      for (int x = tid; x < here; x += SG_PLAN_THREADS)
+      for (int x = tid; x < here; x += THREADS)
         if (pieces_before + x < a.most_pieces) a.pieces[pieces_before + x] = piece_of(x);
     }
     if constexpr (SHARED) {
@@ -318,7 +341,7 @@ __global__ __launch_bounds__(SG_PLAN_THREADS) void k_segment_plan(const SegmentA
           a.joins[at] = {u.begin + b * U::TOKENS, min(U::TOKENS, u.tokens - b * U::TOKENS), n, result + b * U::TOKENS, u.tokens, {}};
       }
     }
-    if (i0 + SG_PLAN_THREADS < n_units) __syncthreads();
+    if (i0 + THREADS < n_units) __syncthreads();
   }
   if (tid == 0) *a.counts = {min(before[0], a.most_pieces), min(before[2], a.most_joins)};
 }
@@ -472,20 +495,50 @@ reduced:
   }
 }
 
-template <int G, bool EIGHTS, bool SHARED>
+// Block x of the segments, all of its rows; by every wavefront for itself.
+template <int G>
+__device__ __forceinline__ bool whole_block(const SegmentArgs& a, int x, Piece* p) {
+  using U = Units<G, false>;
+  const U units{a};
+  int before = 0;
+  for (int i0 = 0; i0 < a.n_segments; i0 += WAVE) {
+    const Unit u = units.load(i0 + (threadIdx.x & 63));
+    const int n = U::blocks(u), upto = before + wave_inclusive_scan(n);
+    const uint64_t beyond = __ballot(upto > x);
+    if (beyond) {
+      const int l = __builtin_ctzll(beyond);
+      auto get = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      const Unit v = {get(u.begin), get(u.tokens), get(u.seq), 0, get(u.end)};
+      const int block = x - (get(upto) - get(n));
+      *p = {v.begin + block * U::TOKENS, (short)min(U::TOKENS, v.tokens - block * U::TOKENS),
+            (short)(U::blocks(v) > 1 ? Piece::SEVERAL : 0), v.seq, 0, v.end, 0, v.tiles(), -1};
+      return block >= 0;
+    }
+    before = __builtin_amdgcn_readlane(upto, WAVE - 1);
+  }
+  return false;
+}
+
+// DIRECT: without a plan, a block and KV head for each workgroup.
+template <int G, bool EIGHTS, bool SHARED, bool DIRECT>
 __global__ __launch_bounds__(AT_WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void k_segment_attn(const SegmentArgs a) {
   __shared__ SegmentLds lds;
   const int tid = threadIdx.x, lane = tid & 63, col = tid & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.x % a.Hkv, x = blockIdx.x / a.Hkv;
-  const int n_pieces = a.counts->pieces;
-  const int4* from = reinterpret_cast<const int4*>(a.pieces + min(x, a.most_pieces - 1));
-  const int4 lo = from[0], hi = from[1];
-  if (x >= n_pieces) return;
-  auto all = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  const int sizes = all(lo.y);
-  const Piece pc = {all(lo.x), (short)sizes, (short)(sizes >> 16), all(lo.z), all(lo.w), all(hi.x), all(hi.y), all(hi.z), all(hi.w)};
+  Piece pc;
+  if constexpr (DIRECT) {
+    if (!whole_block<G>(a, x, &pc)) return;
+  } else {
+    const int n_pieces = a.counts->pieces;
+    const int4* from = reinterpret_cast<const int4*>(a.pieces + min(x, a.most_pieces - 1));
+    const int4 lo = from[0], hi = from[1];
+    if (x >= n_pieces) return;
+    auto all = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int sizes = all(lo.y);
+    pc = {all(lo.x), (short)sizes, (short)(sizes >> 16), all(lo.z), all(lo.w), all(hi.x), all(hi.y), all(hi.z), all(hi.w)};
+  }
 
   // ---- what the queries see: of shared rows, as far as their own sequences go, and share ----
   const int row = wave * 32 + col, token = row / G;     // of the block
@@ -542,7 +595,7 @@ void k_segment_attn(const SegmentArgs a) {
 // Pieces joined: ROWS query rows of one KV head a workgroup, a quarter of the pieces each wavefront, then those four.
 // Workgroups of a wavefront for all pieces: the shared rows of 16 sequences in 17 pieces took 12.5 us.
 constexpr int SG_JOIN_WAVES = 4;
-constexpr int SG_JOIN_ROWS = 8;                         // of a block of a segment
+constexpr int SG_JOIN_ROWS = 8, SG_JOIN_PARTS = 8;      // of a block of a segment, that so many workgroups share
 
 struct Source {                                         // pieces that have results of the rows
   int n, result, step, n_tok, row;
@@ -649,35 +702,43 @@ __global__ __launch_bounds__(SG_JOIN_WAVES * 64) void k_segment_join(const Segme
     }
     join_rows<G, G>(a, shared, Source{own.n_pieces, own.result, own.step, 1, 0}, h, G, lds,
                     [&](int row) { return a.out + ((int64_t)s * a.Hq + h * G + row) * D; });
-  } else {                                              // eight rows of a block
+  } else {                                              // rows of a block, eight at a time
     __shared__ JoinBuffers<SG_JOIN_ROWS> lds;
-    constexpr int PARTS = AT_ROWS / SG_JOIN_ROWS;
-    const int n = a.counts->joins * a.Hkv * PARTS;
-    for (int i = blockIdx.x; i < n; i += gridDim.x) {
-      const int j = i / (a.Hkv * PARTS), rest = i - j * (a.Hkv * PARTS), h = rest / PARTS, row0 = rest % PARTS * SG_JOIN_ROWS;
-      const Whole w = a.joins[j];
-      const int n_rows = min(SG_JOIN_ROWS, w.n_tok * G - row0);
-      if (n_rows <= 0) continue;
-      join_rows<SG_JOIN_ROWS, G>(a, Source{w.n_pieces, w.result, w.step, w.n_tok, row0}, Source{}, h, n_rows, lds, [&](int row) {
+    const int i = blockIdx.x, j = i / a.Hkv, h = i - j * a.Hkv;
+    const Whole w = a.joins[min(j, a.most_joins - 1)];
+    if (j >= a.counts->joins) return;
+    for (int row0 = blockIdx.y * SG_JOIN_ROWS; row0 < w.n_tok * G; row0 += SG_JOIN_PARTS * SG_JOIN_ROWS)
+      join_rows<SG_JOIN_ROWS, G>(a, Source{w.n_pieces, w.result, w.step, w.n_tok, row0}, Source{}, h,
+                                 min(SG_JOIN_ROWS, w.n_tok * G - row0), lds, [&](int row) {
         const int r = row0 + row;
         return a.out + ((int64_t)(w.t0 + r / G) * a.Hq + h * G + r % G) * D;
       });
-    }
   }
 }
 
 template <int G, bool SHARED>
-void launch_segments_g(unsigned groups, unsigned joins, bool eights, const SegmentArgs& a, hipStream_t st) {
+void launch_segments_g(unsigned groups, dim3 joins, bool eights, const SegmentArgs& a, hipStream_t st) {
   const dim3 grid(groups), block(AT_WAVES * 64);
-  hipLaunchKernelGGL((k_segment_plan<G, SHARED>), dim3(1), dim3(SG_PLAN_THREADS), 0, st, a);
-  if (eights)
-    hipLaunchKernelGGL((k_segment_attn<G, true, SHARED>), grid, block, 0, st, a);
+  if (a.n_segments + (SHARED ? a.S : 0) <= SG_FEW_UNITS)
+    hipLaunchKernelGGL((k_segment_plan<G, SHARED, SG_FEW_UNITS>), dim3(1), dim3(SG_FEW_UNITS), 0, st, a);
   else
-    hipLaunchKernelGGL((k_segment_attn<G, false, SHARED>), grid, block, 0, st, a);
-  if (joins) hipLaunchKernelGGL((k_segment_join<G, SHARED>), dim3(joins), dim3(SG_JOIN_WAVES * 64), 0, st, a);
+    hipLaunchKernelGGL((k_segment_plan<G, SHARED, SG_MANY_UNITS>), dim3(1), dim3(SG_MANY_UNITS), 0, st, a);
+  if (eights)
+    hipLaunchKernelGGL((k_segment_attn<G, true, SHARED, false>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_segment_attn<G, false, SHARED, false>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((k_segment_join<G, SHARED>), joins, dim3(SG_JOIN_WAVES * 64), 0, st, a);
+}
+template <int G>
+void launch_direct(unsigned groups, bool eights, const SegmentArgs& a, hipStream_t st) {
+  const dim3 grid(groups), block(AT_WAVES * 64);
+  if (eights)
+    hipLaunchKernelGGL((k_segment_attn<G, true, false, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_segment_attn<G, false, false, true>), grid, block, 0, st, a);
 }
 template <bool SHARED>
-void launch_segments_all(int G, unsigned groups, unsigned joins, bool eights, const SegmentArgs& a, hipStream_t st) {
+void launch_segments_all(int G, unsigned groups, dim3 joins, bool eights, const SegmentArgs& a, hipStream_t st) {
   switch (G) {
     case 1: launch_segments_g<1, SHARED>(groups, joins, eights, a, st); break;
     case 2: launch_segments_g<2, SHARED>(groups, joins, eights, a, st); break;
@@ -688,10 +749,10 @@ void launch_segments_all(int G, unsigned groups, unsigned joins, bool eights, co
 
 // What a workspace holds, for n_segments segments with n_rows tokens (and S sequences with rows of their own).
 struct Space {
-  int64_t pieces, joins, rows;
+  int64_t blocks, pieces, joins, rows;
   Space(const Dims& dm, int64_t n_rows, int64_t n_segments, bool shared) {
     // blocks there can be, as one of each segment may be short, and the pieces that are more than those
-    const int64_t blocks = n_rows / (AT_ROWS / dm.G) + (n_rows < n_segments ? n_rows : n_segments);
+    blocks = n_rows / (AT_ROWS / dm.G) + (n_rows < n_segments ? n_rows : n_segments);
     pieces = blocks + (shared ? dm.S : 0) + SG_EXTRA / dm.Hkv;
     joins = shared ? n_segments + dm.S : SG_EXTRA / dm.Hkv + 1;
     // A unit that is cut has at most twice as many pieces as are more than its blocks.
@@ -703,6 +764,20 @@ struct Space {
   size_t part_at() const { return joins_at() + padded((size_t)joins * sizeof(Whole)); }
   size_t bytes() const { return part_at() + (size_t)rows * SG_ROW * sizeof(float); }
 };
+
+// Whether every block is left to one workgroup, whatever the lengths are: the plan and the join cost 8 to 9 us, which cutting
+// and sorting have to spare.  The host knows the table's width and takes it for the longest sequence, and that segments
+// are not empty.  us, direct / planned, 8 heads of G = 4, lengths of 0.1 to 1 and 0.7 to 1 of N rows:
+//   1 sequence, 64 tokens (8 blocks)      256 rows - and 12 / 19, 768 - and 24 / 20
+//   8 of 20 tokens (64)                   1024 rows 22 / 25, 1536 30 / 26
+//   16 of 20 (128)                        1536 30 / 31, 2048 38 / 35
+//   64 of 16 (512)                        4000 108 / 124; 3000 rows of 0.7 to 1 118 / 139
+//   24 of 200 (600 full blocks)           768 43 / 39, 4000 140 / 121; 3000 rows of 0.7 to 1 214 / 218
+bool goes_direct(const Dims& dm, int64_t n_rows, int64_t rows) {
+  const int64_t full = n_rows / (AT_ROWS / dm.G) * dm.Hkv, segments = (n_rows < dm.S ? n_rows : dm.S) * dm.Hkv;
+  const int64_t blocks = full > segments ? full : segments;
+  return rows <= (blocks < 64 || full >= SG_CUS ? 768 : (blocks < SG_CUS ? 1536 : 4096));
+}
 
 hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv, const Space& space, void* workspace,
                            float softmax_scale, hipStream_t st) {
@@ -723,13 +798,20 @@ hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv
   a.scale_log2e = softmax_scale * 1.4426950408889634f;
   const unsigned groups = (unsigned)(space.pieces * dm.Hkv);
   const bool eights = kv.page_size % 8 == 0;
-  if (a.shared) {
-    launch_segments_all<true>(dm.G, groups, (unsigned)dm.HP, eights, a, st);
-  } else {
-    const int64_t parts = space.joins * dm.Hkv * (AT_ROWS / SG_JOIN_ROWS);
-    const bool cut = a.pages.rows > 2 * SG_MIN_TILES * AT_TILE - AT_TILE;   // otherwise no unit is
-    launch_segments_all<false>(dm.G, groups, cut ? (unsigned)(parts < 4 * SG_CUS ? parts : 4 * SG_CUS) : 0, eights, a, st);
+  if (!a.shared && goes_direct(dm, a.n_rows, a.pages.rows)) {
+    const unsigned blocks = (unsigned)(space.blocks * dm.Hkv);
+    switch (dm.G) {
+      case 1: launch_direct<1>(blocks, eights, a, st); break;
+      case 2: launch_direct<2>(blocks, eights, a, st); break;
+      case 4: launch_direct<4>(blocks, eights, a, st); break;
+      default: launch_direct<8>(blocks, eights, a, st); break;
+    }
+    return hipGetLastError();
   }
+  if (a.shared)
+    launch_segments_all<true>(dm.G, groups, dim3((unsigned)dm.HP), eights, a, st);
+  else
+    launch_segments_all<false>(dm.G, groups, dim3((unsigned)(space.joins * dm.Hkv), SG_JOIN_PARTS), eights, a, st);
   return hipGetLastError();
 }
 
@@ -750,6 +832,15 @@ hipError_t launch_cross_attn(const Dims& dm, const void* q, int64_t n_rows, cons
   a.n_segments = dm.S;
   a.n_rows = (int)n_rows;
   return launch_segments(dm, a, kv, Space(dm, n_rows, dm.S, false), workspace, softmax_scale, st);
+}
+
+// Whether reading the shared rows once for each sequence takes no longer than cutting and joining, by the table's width.  us
+// of the two, S sequences of N shared and 64 rows, 8 heads, G = 4: S = 4, N = 2048 (34 MB) 10.4 and 16.3, 8192 (135 MB) 18.1
+// and 19.8, 16384 (269 MB) 30.5 and 25.6; S = 16, N = 2048 (137 MB) 16.4 and 17.8, 4096 (272 MB) 24 and 20; S = 64,
+// N = 256 (80 MB) 11 and 22, 1024 (281 MB) 22 and 24; one head, G = 8, S = 64, N = 4096 (136 MB) 19 and 25.
+bool shared_reads_each(const Dims& dm, const ck_paged_kv& kv) {
+  const double rows = (double)dm.HP * kv.page_size * kv.pages_per_seq;
+  return dm.dtype != CK_BF16 || rows * (4 * D) <= 160e6;
 }
 
 hipError_t launch_shared_attn(const Dims& dm, const void* q, const ck_paged_kv& kv, const int32_t* lengths,

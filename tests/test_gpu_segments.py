@@ -29,10 +29,19 @@ def close(got, want, tol, what):
     assert worst <= 0, f"{what}: off by {np.abs(got - want).max():.3g}, {worst:.3g} more than allowed"
 
 
+# Tables with room for short sequences are served by one launch; for long ones the work is planned, cut and joined.
+FORMS = ["short", "long"]
+
+
+def width_of(form, page, S=1, Hkv=1):
+    """Entries of a table: none more than needed, or room for 5000 rows and 160 MB of a batch."""
+    return 0 if form == "short" else max(5000, int(161e6 / (512 * S * Hkv))) // page + 1
+
+
 # ---------------------------------------------------------------- cross attention
-def run_cross(lens, news, Hkv, G, page, cache=None, seed=0, pad=0, before=0, qscale=1.5, starts=None, width=0):
+def run_cross(lens, news, Hkv, G, page, cache=None, seed=0, pad=0, before=0, qscale=1.5, form="short"):
     S = len(lens)
-    c = cache or Cache(lens, Hkv, page, BF, seed, DEV, width=width)
+    c = cache or Cache(lens, Hkv, page, BF, seed, DEV, width=width_of(form, page))
     starts = (before + np.concatenate([[0], np.cumsum(news)])).tolist()
     T = max(1, starts[-1] + pad)
     g = torch.Generator().manual_seed(seed + 1)
@@ -54,48 +63,61 @@ def run_cross(lens, news, Hkv, G, page, cache=None, seed=0, pad=0, before=0, qsc
     return out
 
 
+@pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("G", [1, 2, 4, 8])
 @pytest.mark.parametrize("lens,news,page", [([1], [1], 1), ([0, 1, 2], [3, 1, 2], 16), ([64], [64], 64),
                                             ([65, 63, 130], [1, 65, 9], 7), ([200, 0, 300], [17, 5, 0], 40),
                                             ([129], [300], 32), ([7, 1000], [40, 3], 256), ([0, 0], [1, 2], 8)])
-def test_cross(lens, news, page, G):
-    run_cross(lens, news, 2, G, page)
+def test_cross(lens, news, page, G, form):
+    run_cross(lens, news, 2, G, page, form=form)
 
 
 @pytest.mark.parametrize("Hkv,G", [(1, 1), (3, 2), (8, 4), (16, 1)])
 @pytest.mark.parametrize("page", [24, 9])
 def test_cross_heads_and_pieces(Hkv, G, page):
     # several pieces of each, blocks that are not full, a sequence whose only block has one token
-    run_cross([2500, 300, 1], [30, 1, 5], Hkv, G, page)
+    run_cross([2500, 300, 1], [30, 1, 5], Hkv, G, page, form="long")
 
 
-def test_cross_rows_outside_the_sequences_are_left():
-    run_cross([700, 30], [9, 4], 2, 4, 16, pad=5, before=3)
+@pytest.mark.parametrize("form", FORMS)
+def test_cross_rows_outside_the_sequences_are_left(form):
+    run_cross([700, 30], [9, 4], 2, 4, 16, pad=5, before=3, form=form)
 
 
-def test_cross_more_sequences_than_lanes():
-    run_cross([(7 * s) % 197 for s in range(131)], [(3 * s) % 5 for s in range(131)], 1, 2, 16)
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("S", [131, 300, 1100])
+def test_cross_more_sequences_than_lanes_and_threads(S, form):
+    run_cross([(7 * s) % 197 for s in range(S)], [(3 * s) % 5 for s in range(S)], 1, 2, 16, form=form)
 
 
 def test_cross_more_blocks_than_fit_and_a_long_sequence():
     run_cross([150, 9000, 70], [700, 2, 900], 8, 1, 64)
 
 
-def test_cross_large_scores():
-    run_cross([3000], [20], 1, 4, 32, qscale=40.0)
+def test_cross_many_pieces_of_many_tokens():
+    # 200 tokens of 4 heads are four blocks, each in several pieces
+    run_cross([8000, 40], [200, 3], 1, 4, 32)
 
 
-def test_cross_pages_that_are_missing():
+@pytest.mark.parametrize("form", FORMS)
+def test_cross_large_scores(form):
+    run_cross([700], [20], 1, 4, 32, qscale=40.0, form=form)
+    run_cross([3000], [3], 1, 4, 32, qscale=40.0, form=form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_cross_pages_that_are_missing(form):
     lens = [500, 260]
-    c = Cache(lens, 2, 16, BF, 5, DEV)
+    c = Cache(lens, 2, 16, BF, 5, DEV, width=width_of(form, 16))
     c.table[0, 3:9] = -1
     c.table[1, :] = 10 ** 6                                # nothing is left of it
     run_cross(lens, [20, 20], 2, 2, 16, cache=c)
 
 
-def test_cross_infinite_values_reach_every_query_of_their_sequence_only():
-    lens, news = [700, 300], [11, 6]
-    c = Cache(lens, 1, 24, BF, 6, DEV)
+@pytest.mark.parametrize("form", FORMS)
+def test_cross_infinite_values_reach_every_query_of_their_sequence_only(form):
+    lens = [700, 300]
+    c = Cache(lens, 1, 24, BF, 6, DEV, width=width_of(form, 24))
     for s, r, ch in ((0, 3, 5), (0, 699, 7), (1, 299, 9)):
         v = c.rows_v[s][0, r].clone()
         v[ch] = math.inf
@@ -130,10 +152,11 @@ def test_cross_one_token_for_each_sequence(dtype):
                 close(out[s, h * G:(h + 1) * G], ref, tol, f"sequence {s} head {h}")
 
 
-def test_cross_twice_the_same_and_from_a_graph():
+@pytest.mark.parametrize("form", FORMS)
+def test_cross_twice_the_same_and_from_a_graph(form):
     """Bit-equal from run to run; two captured calls on one workspace replay with the lengths of that time."""
-    lens, news, Hkv, G = [3000, 64, 700], [40, 300, 1], 2, 4
-    c = Cache(lens, Hkv, 16, BF, 8, DEV)
+    lens, Hkv, G = [3000 if form == "long" else 700, 64, 650], 2, 4
+    c = Cache(lens, Hkv, 16, BF, 8, DEV, width=width_of(form, 16))
     sh, kv, T = shape(3, Hkv, G), c.kv(), 341
     q = torch.randn(T, Hkv * G, D, device=DEV).to(BF)
     starts, n, out = i32([0, 40, 340, 341]), i32(lens), torch.empty_like(q)
@@ -146,7 +169,7 @@ def test_cross_twice_the_same_and_from_a_graph():
         ck.ck_cross_attn(sh, q, starts, kv, n, out, workspace=ws)
     with torch.cuda.graph(second):
         ck.ck_cross_attn(sh, q, starts, kv, n, other, softmax_scale=0.05, workspace=ws)
-    for new in (lens, [3000, 0, 650], [17, 64, 1], lens):
+    for new in (lens, [lens[0], 0, 600], [17, 64, 1], lens):
         n.copy_(i32(new))
         out.fill_(float("nan"))
         graph.replay()
@@ -161,10 +184,10 @@ def test_cross_twice_the_same_and_from_a_graph():
 
 
 # ---------------------------------------------------------------- rows that a batch shares
-def shared_cache(groups, lens, shares, Hkv, page, dtype=BF, seed=0):
+def shared_cache(groups, lens, shares, Hkv, page, dtype=BF, seed=0, form="long"):
     """A cache whose sequences [groups[g], groups[g + 1]) begin with the first one's rows, in its pages where whole ones
     are shared, whose own copies hold NaN."""
-    c = Cache(lens, Hkv, page, dtype, seed, DEV)
+    c = Cache(lens, Hkv, page, dtype, seed, DEV, width=width_of(form, page, len(lens), Hkv))
     for a, b in zip(groups[:-1], groups[1:]):
         for s in range(a + 1, b):
             n = max(0, min(shares[s], lens[s]))
@@ -182,9 +205,9 @@ def shared_cache(groups, lens, shares, Hkv, page, dtype=BF, seed=0):
     return c
 
 
-def run_shared(groups, lens, shares, Hkv, G, page, dtype=BF, cache=None, seed=0, qscale=1.5):
+def run_shared(groups, lens, shares, Hkv, G, page, dtype=BF, cache=None, seed=0, qscale=1.5, form="long"):
     S = len(lens)
-    c = cache or shared_cache(groups, lens, shares, Hkv, page, dtype, seed)
+    c = cache or shared_cache(groups, lens, shares, Hkv, page, dtype, seed, form)
     g = torch.Generator().manual_seed(seed + 1)
     q = (torch.randn(S, Hkv * G, D, generator=g) * qscale).to(dtype)
     out = torch.full((S, Hkv * G, D), float("nan"), dtype=dtype, device=DEV)
@@ -218,10 +241,17 @@ def test_shared(case, page, G):
     run_shared(groups, lens, shares, 2, G, page)
 
 
+@pytest.mark.parametrize("case", CASES)
+def test_shared_little(case):
+    groups, lens, shares = case
+    run_shared(groups, lens, shares, 2, 4, 16, form="short")
+
+
 @pytest.mark.parametrize("case", CASES[2:5])
 def test_shared_in_fp32(case):
     groups, lens, shares = case
     run_shared(groups, lens, shares, 2, 4, 16, F32)
+    run_shared(groups, lens, shares, 2, 4, 16, F32, form="short")
 
 
 @pytest.mark.parametrize("Hkv,G", [(1, 8), (3, 4), (8, 2)])
@@ -236,8 +266,14 @@ def test_shared_more_queries_than_a_block():
     run_shared([0, 40, 41], lens, [700 - s for s in range(40)] + [9], 1, 8, 32)
 
 
-def test_shared_more_sequences_and_groups_than_lanes():
-    S = 150
+def test_shared_few_queries_that_see_different_numbers_of_shared_rows():
+    # two sequences of four heads: as many queries as would stream the rows, were they the same for all
+    run_shared([0, 2], [900, 700], [890, 500], 2, 4, 16)
+    run_shared([0, 2], [900, 890], [890, 890], 2, 4, 16)
+
+
+@pytest.mark.parametrize("S", [150, 600, 900])
+def test_shared_more_sequences_and_groups_than_lanes_and_threads(S):
     lens = [100 + (s * 31) % 90 for s in range(S)]
     groups = list(range(0, S, 2)) + [S]
     run_shared(groups, lens, [90 if s % 2 == 0 else 71 for s in range(S)], 1, 2, 16)
@@ -250,7 +286,7 @@ def test_shared_large_scores():
 def test_shared_equals_attention_of_each_sequence():
     """The same rows as the attention of single tokens, but for roundings."""
     lens, groups, shares = [800, 1500, 900, 400], [0, 4], [800, 800, 800, 400]
-    c = shared_cache(groups, lens, shares, 2, 24)
+    c = shared_cache(groups, lens, shares, 2, 24, form="long")
     q = torch.randn(4, 8, D, device=DEV).to(BF)
     a, b, sh = torch.empty_like(q), torch.empty_like(q), shape(4, 2, 4)
     ck.ck_shared_decode_attn(sh, q, c.kv(), i32(lens), i32(groups), i32(shares), a)
