@@ -1,6 +1,6 @@
 // Page tables, reference counts and slots of new rows from the requests of a batch.
 //
-// Integers only, and little of them: what counts is the chain of steps that wait for each other.  One workgroup takes
+// Integers only, and few: what counts is the chain of steps that wait for each other.  One workgroup takes
 // all of them, so that a step waits for a barrier and not for a launch: pages taken over from parents, pages given back,
 // pages given out, slots.  Each step is a list of items (sequence, entry of its table); a prefix sum over the sequences
 // numbers them, and a thread finds the sequence of its item by binary search in LDS.  So a sequence with many
@@ -14,15 +14,16 @@ namespace ck {
 namespace {
 
 // Threads of the planning workgroup.  Prefix sums are done by every wavefront for itself, over all of them: four are done
-// sooner where there are few sequences and the table is small: a token for each of 64 sequences 6.8 us, not 7.6; 16500 pages
-// given back 53, not 30.
+// sooner where there are few sequences and the table is small (16500 pages given back take four 53 us, sixteen 30).
 constexpr int PL_FEW = 256, PL_MANY = 1024, PL_FEW_ENTRIES = 16384;
 constexpr int PL_LOADS = 32;                            // runs of 256 pages that a wavefront looks at together, at most
-constexpr int PL_FIRST_RUNS = 32;                       // ... and the workgroup to begin with
+// ... and the workgroup to begin with, four times as many in each turn.  A token for each of 64 sequences (5 pages of 16384)
+// and taken back, two calls in a graph: 12.3 us, 14.3 with 32 runs and then 512; 18.1 and 17.0 where no page is free.
+constexpr int PL_FIRST_RUNS = 16;
 constexpr int PL_ITEMS = 4;                             // of a thread at a time
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
 constexpr int PL_OWN_ROWS = 8192;
-constexpr int PL_SLOT_ROWS = PL_MANY;                // of a workgroup of that launch
+constexpr int PL_SLOT_ROWS = PL_MANY;                   // of a workgroup of that launch
 
 struct PlanArgs {
   const int32_t *n_new, *parent, *shared_rows;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   int* const rows = lds;                                // [S]: of every sequence, before it gives back or gets tokens
   int* const upto = lds + a.S;                          // [S]: prefix sums
   __shared__ int2 tmp[WAVES];
-  __shared__ int free_upto[PL_LOADS * WAVES];                    // free pages of a run; then before it
+  __shared__ int free_upto[PL_LOADS * WAVES];           // free pages of a run; then before it
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ps = (int)a.size.d;
   auto after = [&](int s, int n) {                      // rows of a sequence after the call
@@ -222,8 +223,7 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
     const int s = first_beyond(upto, a.S, r);
     return a.table + (uint32_t)(s * a.per_seq + a.pages_of(rows[s]) + (r - (s > 0 ? upto[s - 1] : 0)));
   };
-  // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.  Few runs at
-  // first: most calls need few pages (64 tokens, 5 pages of 16384: 1.7 us with two runs for each wavefront, 5.8 with eight).
+  // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.
   int found = 0;                                        // free pages so far
   constexpr int RUN = WAVE * 4;
   for (int p0 = 0, loads = PL_FIRST_RUNS / WAVES; p0 < a.n_pages && found < wanted;) {
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
     }
     __syncthreads();                                    // free_upto is read no more
     p0 += loads * WAVES * RUN;
-    loads = PL_LOADS;
+    loads = min(4 * loads, PL_LOADS);
   }
   for (int r = found + tid; r < wanted; r += THREADS) *entry_of(r) = -1;
   int none = 0;

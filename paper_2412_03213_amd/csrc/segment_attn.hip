@@ -23,7 +23,7 @@ constexpr int SG_ROW = D + 4;                           // floats of a query row
 // Threads of the planning workgroup, a unit each: most of its steps are done by every wavefront for itself (sums over all
 // of them), which four do in 4.2 us, sixteen in 6.
 constexpr int SG_FEW_UNITS = 256, SG_MANY_UNITS = 1024;
-constexpr int SG_TRIES = 8;                             // of them
+constexpr int SG_TRIES = 8;                             // cuts that are compared
 constexpr int SG_CLASSES = 8;                           // of pieces, by how long they take
 
 // A piece of a block, as the planning workgroup hands it out.
@@ -101,7 +101,8 @@ struct Units {
 // read.  A tile of its own for each of 256 workgroups takes 1.2 with up to two wavefronts of queries (their share of the
 // memory) and 0.18 more with each other one, 1.8 at most where other blocks read the same rows (from L2); measured: 1.19 for
 // 16, 32 and 64 queries, 1.35, 1.6, 1.85, 2.0, 2.2 and 2.15 for 96 to 256.  With few workgroups on the chip it takes 0.46 for 16
-// queries, 0.85 for 32, 1.0 for 96, 1.41 for 256.
+// queries, 0.85 for 32, 1.0 for 96, 1.41 for 256.  What this leads to, against even pieces, as many as compute units: 16
+// sequences with 131072 shared rows 101 us, not 148, 64 with 32768 109, not 118.
 __device__ __forceinline__ float tile_cost(int rows, int blocks) {
   const float t = fmaf(0.18f, (float)max(0, (rows + 31) / 32 - 2), 1.2f);
   return blocks > 1 ? fminf(t, 1.8f) : t;

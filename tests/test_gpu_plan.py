@@ -336,3 +336,56 @@ def test_a_shared_prompt_and_an_encoder_from_requests_to_answers():
     ck.ck_plan_pages(sh, i32([INT_MIN] * S), lengths, kv.page_table, refs, size, starts, lacking)
     ck.ck_plan_pages(sh2, i32([INT_MIN] * 2), n2, table, refs, size, starts2, lacking)
     assert int(refs.abs().sum()) == 0
+
+
+def test_calls_with_and_without_the_native_marshalling(monkeypatch):
+    """The same results, and refusals of what the native form leaves to the general one."""
+    g = torch.Generator().manual_seed(5)
+    lib, sh = ck.load_library(), shape(2, 2, 4)
+    rnd = lambda *s: torch.randn(*s, generator=g).to(BF).to(DEV)
+    K, V, q, k = rnd(20, 2, 16, D), rnd(20, 2, 16, D), rnd(7, 8, D), rnd(7, 2, D)
+    results = []
+    for native in (True, False):
+        if not native:
+            for name in ("plan_pages", "store_rows", "shared_decode_attn", "cross_attn"):
+                monkeypatch.setattr(lib, "host_" + name, lambda *args: None)
+        kv = ck.PagedKV(K.clone(), V.clone(), torch.full((2, 8), -1, dtype=torch.int32, device=DEV))
+        n, refs, starts, lacking, slots = i32([0, 0]), i32([0] * 20), i32([0] * 3), i32([0]), i32([0] * 7)
+        ck.ck_plan_pages(sh, i32([40, 50]), n, kv.page_table, refs, 16, starts, lacking)
+        ck.ck_plan_pages(sh, i32([3, 4]), n, kv.page_table, refs, 16, starts, lacking, slots=slots,
+                         parent=i32([-1, -1]), shared_rows=i32([0, 0]))
+        ck.ck_store_rows(sh, k, k, slots, kv)
+        a, b, c = torch.empty_like(q), torch.empty_like(q[:2]), torch.empty_like(q[:2])
+        ck.ck_cross_attn(sh, q, starts, kv, n, a)
+        ck.ck_cross_attn(sh, q[:2], None, kv, n, b)
+        ck.ck_shared_decode_attn(sh, q[:2], kv, n, i32([0, 2]), i32([0, 0]), c, softmax_scale=0.1)
+        results.append((n, kv.page_table, refs, starts, lacking, slots, kv.K, kv.V, a, b, c))
+        with pytest.raises(ck.ClusterKVError):
+            ck.ck_cross_attn(sh, q, starts, kv, n, q)
+        with pytest.raises(ck.ClusterKVError):
+            ck.ck_shared_decode_attn(sh, q[:2], kv, n, i32([0, 1, 2, 2]), i32([0, 0]), c)
+        with pytest.raises(ck.ClusterKVError):
+            ck.ck_plan_pages(sh, n, n, kv.page_table, refs, 0, starts, lacking)
+        with pytest.raises(ck.ClusterKVError):
+            ck.ck_plan_pages(sh, n, n, kv.page_table, refs, 16, starts, lacking, parent=n)
+        with pytest.raises(ValueError):
+            ck.ck_store_rows(sh, k, k[:3], slots, kv)
+        with pytest.raises(ValueError):
+            ck.ck_plan_pages(sh, n, n, kv.page_table[:1], refs, 16, starts, lacking)
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+
+
+def test_tensors_on_another_device_are_refused(monkeypatch):
+    """A device that is not the current one."""
+    from paper_2412_03213_amd import binding
+    sh, n, starts, one = shape(1, 1, 4), i32([1]), i32([0, 1]), i32([0])
+    kv = ck.PagedKV(torch.zeros(2, 1, 4, D, dtype=BF, device=DEV), torch.zeros(2, 1, 4, D, dtype=BF, device=DEV))
+    q, k, refs = torch.zeros(1, 4, D, dtype=BF, device=DEV), torch.zeros(1, 1, D, dtype=BF, device=DEV), i32([0, 0])
+    sh2 = ck.Shape(1, 4, 1, 4, 1)
+    kv1 = ck.PagedKV(kv.K, kv.V, i32([[0]]))
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    for call in (lambda: ck.ck_plan_pages(sh, n, n, i32([[0]]), refs, 4, starts, one),
+                 lambda: ck.ck_store_rows(sh, k, k, n, kv1), lambda: ck.ck_cross_attn(sh2, q, starts, kv1, n, q.clone()),
+                 lambda: ck.ck_shared_decode_attn(sh2, q, kv1, n, starts, n, q.clone())):
+        with pytest.raises(ValueError, match="current"):
+            call()

@@ -128,7 +128,14 @@ def test_workspaces():
         assert ck.ck_workspace_bytes(sh, binding.CK_WS_CROSS_ATTN, 0) == 0
 
 
-def test_tensors_of_other_shapes_types_and_places_are_refused():
+NATIVE = ("plan_pages", "store_rows", "shared_decode_attn", "cross_attn")
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_host_tensors_are_refused(native, monkeypatch):
+    if not native:
+        for name in NATIVE:
+            monkeypatch.setattr(ck.load_library(), "host_" + name, lambda *args: None)
     bf = torch.bfloat16
     K = torch.zeros(8, 2, 16, 128, dtype=bf)
     table = torch.zeros(2, 4, dtype=torch.int32)
@@ -140,7 +147,7 @@ def test_tensors_of_other_shapes_types_and_places_are_refused():
                  lambda: ck.ck_cross_attn(SH, q, starts, cache, n, out, workspace=ws),
                  lambda: ck.ck_store_rows(SH, k, k, n, cache),
                  lambda: ck.ck_plan_pages(SH, n, n, table, refs, 16, starts, one)):
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match="host"):
             call()
 
 
