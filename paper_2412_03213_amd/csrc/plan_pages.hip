@@ -14,13 +14,16 @@ namespace ck {
 namespace {
 
 // Threads of the planning workgroup.  Prefix sums are done by every wavefront for itself, over all of them: four are done
-// sooner where there are few sequences and the table is small (16500 pages given back take four 53 us, sixteen 30).
-constexpr int PL_FEW = 256, PL_MANY = 1024, PL_FEW_ENTRIES = 16384;
+// sooner where there are few sequences and few pages to take over or give back, for which the host has the table's size.  Tokens
+// given and taken back, two calls in a graph, four / sixteen, us: 64 sequences 11.2 / 13.6, 100 with a table of 502 entries each
+// 14.4 / 15.8, 12000 pages taken over and 16500 given back 94 / 71.
+constexpr int PL_FEW = 256, PL_MANY = 1024, PL_FEW_ENTRIES = 65536;
 constexpr int PL_LOADS = 32;                            // runs of 256 pages that a wavefront looks at together, at most
 // ... and the workgroup to begin with, four times as many in each turn.  A token for each of 64 sequences (5 pages of 16384)
-// and taken back, two calls in a graph: 12.3 us, 14.3 with 32 runs and then 512; 18.1 and 17.0 where no page is free.
+// and taken back, two calls in a graph: 11.2 us, 11.8 with 32 runs, 10.9 with 8; 14.0, 14.7 and 16.1 where no page is free.
 constexpr int PL_FIRST_RUNS = 16;
 constexpr int PL_ITEMS = 4;                             // of a thread at a time
+constexpr int PL_LIST = 2048;                           // free pages that are given out together
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
 constexpr int PL_OWN_ROWS = 8192;
 constexpr int PL_SLOT_ROWS = PL_MANY;                   // of a workgroup of that launch
@@ -111,6 +114,8 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   int* const rows = lds;                                // [S]: of every sequence, before it gives back or gets tokens
   int* const upto = lds + a.S;                          // [S]: prefix sums
   __shared__ int2 tmp[WAVES];
+  __shared__ int behind;                                // pages that the table has no entry for
+  __shared__ int list[PL_LIST];                         // free pages
   __shared__ int free_upto[PL_LOADS * WAVES];           // free pages of a run; then before it
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ps = (int)a.size.d;
@@ -135,6 +140,22 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
     }
   };
   struct Entry { int32_t* at; int page; };
+
+  // the counts of pages p to p + 3; behind the last there are no free ones
+  auto counts_of = [&](int p) {
+    int4 c = make_int4(1, 1, 1, 1);
+    if (p + 3 < a.n_pages) return *reinterpret_cast<const int4*>(a.refs + p);
+    if (p < a.n_pages) c.x = a.refs[p];
+    if (p + 1 < a.n_pages) c.y = a.refs[p + 1];
+    if (p + 2 < a.n_pages) c.z = a.refs[p + 2];
+    return c;
+  };
+  // Those that are looked at first are asked for before it is known whether pages are wanted.
+  constexpr int RUN = WAVE * 4, FIRST = PL_FIRST_RUNS / WAVES;
+  int4 counts[FIRST];
+#pragma unroll
+  for (int k = 0; k < FIRST; ++k) counts[k] = counts_of((k * WAVES + wave) * RUN + lane * 4);
+  if (tid == 0) behind = 0;
 
   // ---- sequences without rows take over whole pages of a parent, as it stands before the call ----
   int taken = 0, unused = 0, less = 0;
@@ -197,7 +218,7 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   }
 
   // ---- pages for new rows ----
-  int wanted = 0, tokens = 0, behind = 0;               // behind: pages that the table has no entry for
+  int wanted = 0, tokens = 0;
   for (int s0 = 0; s0 < a.S; s0 += THREADS) {
     const int s = s0 + tid;
     int n = 0, add = 0;
@@ -206,7 +227,8 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
       if (m > 0) {
         const int have = a.pages_of(rows[s]), need = a.pages_of(now);
         n = max(0, min(need, a.per_seq) - have);
-        behind += max(0, need - max(have, a.per_seq));
+        const int none = need - max(have, a.per_seq);
+        if (none > 0) atomicAdd(&behind, none);
         add = m;
       }
       a.lengths[s] = now;
@@ -225,8 +247,8 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   };
   // Free pages, by runs of 256 that go to the wavefronts in turn, so that all of them have some to give out.
   int found = 0;                                        // free pages so far
-  constexpr int RUN = WAVE * 4;
-  for (int p0 = 0, loads = PL_FIRST_RUNS / WAVES; p0 < a.n_pages && found < wanted;) {
+  const bool unchanged = taken == 0 && !less;           // since the counts were asked for
+  for (int p0 = 0, loads = FIRST; p0 < a.n_pages && found < wanted;) {
     const int left = (a.n_pages - p0 + RUN - 1) / RUN - wave;   // runs that are this wavefront's
     const int mine = max(0, min(loads, (left + WAVES - 1) / WAVES));
     auto first_of = [&](int k) { return p0 + (k * WAVES + wave) * RUN; };
@@ -238,15 +260,10 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (g * 8 + j >= mine) continue;                // wave-uniform, as below
-        const int p = first_of(g * 8 + j) + lane * 4;
-        if (p + 3 < a.n_pages) {
-          c[j] = *reinterpret_cast<const int4*>(a.refs + p);
-        } else {
-          c[j] = make_int4(1, 1, 1, 1);
-          if (p < a.n_pages) c[j].x = a.refs[p];
-          if (p + 1 < a.n_pages) c[j].y = a.refs[p + 1];
-          if (p + 2 < a.n_pages) c[j].z = a.refs[p + 2];
-        }
+        if (g * 8 + j < FIRST && p0 == 0 && unchanged)
+          c[j] = counts[(g * 8 + j) % FIRST];
+        else
+          c[j] = counts_of(first_of(g * 8 + j) + lane * 4);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -266,41 +283,45 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
     __syncthreads();
     const bool run = tid < loads * WAVES;
     int n = run ? free_upto[tid] : 0, zero = 0;
-    const int n_run = n;
+    const int n_run = n, found_before = found;
     scan_two<WAVES>(n, zero, found, unused, tmp);
     if (run) free_upto[tid] = n - n_run;                // before the run
     __syncthreads();
+    // their numbers in order, so many at a time, then the entries that get them
+    const int end = min(found, wanted);
+    for (int r0 = found_before; r0 < end; r0 += PL_LIST) {
 #pragma unroll
-    for (int g = 0; g < PL_LOADS / 8; ++g) {
-      if (g * 8 >= mine) continue;
+      for (int g = 0; g < PL_LOADS / 8; ++g) {
+        if (g * 8 >= mine) continue;
 #pragma unroll 1
-      for (int j = 0; j < min(8, mine - g * 8); ++j) {
-        const int k = g * 8 + j;
-        int r = __builtin_amdgcn_readfirstlane(free_upto[k * WAVES + wave]);
-        if (r >= wanted) break;
-        const uint32_t four = (bits[g] >> (4 * j)) & 15u;
-        const int c = __popc(four);
-        r += wave_inclusive_scan(c) - c;
+        for (int j = 0; j < min(8, mine - g * 8); ++j) {
+          const int k = g * 8 + j;
+          int r = __builtin_amdgcn_readfirstlane(free_upto[k * WAVES + wave]) - r0;
+          if (r >= PL_LIST || r + r0 >= end) break;
+          const uint32_t four = (bits[g] >> (4 * j)) & 15u;
+          const int c = __popc(four);
+          r += wave_inclusive_scan(c) - c;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (!((four >> i) & 1)) continue;
-          if (r < wanted) {
-            const int p = first_of(k) + lane * 4 + i;
-            a.refs[p] = 1;
-            *entry_of(r) = p;
+          for (int i = 0; i < 4; ++i) {
+            if (!((four >> i) & 1)) continue;
+            if ((uint32_t)r < (uint32_t)PL_LIST) list[r] = first_of(k) + lane * 4 + i;
+            ++r;
           }
-          ++r;
         }
       }
+      __syncthreads();
+      for (int r = r0 + tid; r < min(end, r0 + PL_LIST); r += THREADS) {
+        const int p = list[r - r0];
+        a.refs[p] = 1;
+        *entry_of(r) = p;
+      }
+      __syncthreads();                                  // list and free_upto are read no more
     }
-    __syncthreads();                                    // free_upto is read no more
     p0 += loads * WAVES * RUN;
     loads = min(4 * loads, PL_LOADS);
   }
   for (int r = found + tid; r < wanted; r += THREADS) *entry_of(r) = -1;
-  int none = 0;
-  scan_two<WAVES>(behind, none, unused, none, tmp);
-  if (tid == THREADS - 1) *a.lacking = behind + max(0, wanted - found);
+  if (tid == 0) *a.lacking = behind + max(0, wanted - found);
   if (!a.slots || a.n_rows > PL_OWN_ROWS) return;
 
   // ---- slots ----
