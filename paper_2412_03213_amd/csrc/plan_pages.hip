@@ -24,8 +24,9 @@ constexpr int PL_LOADS = 32;                            // runs of 256 pages tha
 constexpr int PL_FIRST_RUNS = 16;
 constexpr int PL_ITEMS = 4;                             // of a thread at a time
 constexpr int PL_LIST = 2048;                           // free pages that are given out together
-// Rows whose slots the planning workgroup writes itself; more are left to a launch of their own.
-constexpr int PL_OWN_ROWS = 8192;
+// Rows whose slots the planning workgroup writes itself; more are left to a launch of their own (two calls, us: 2400 rows
+// 13.1 and 13.6, 4000 14.1 and 13.7, 16000 21.6 and 14.8).
+constexpr int PL_OWN_ROWS = 3000;
 constexpr int PL_SLOT_ROWS = PL_MANY;                   // of a workgroup of that launch
 
 struct PlanArgs {
