@@ -23,6 +23,7 @@ constexpr float AT_NEG_BIG = -FLT_MAX;                  // no row yet: below no 
 constexpr int AT_WAVES = 8;
 constexpr int AT_ROWS = AT_WAVES * 32;                  // query rows (token, head of the group) of a workgroup
 constexpr int AT_TILE = 64;                             // cache rows of a tile
+constexpr int AT_PLACES = 1024;                         // of rows, that are looked up together
 constexpr int AT_BUFFERS = 3;                           // tiles of keys, and of values, in LDS: loads run two tiles ahead
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -88,6 +89,7 @@ struct Tiles {
 struct TileBuffers {
   __attribute__((aligned(1024))) char k[AT_BUFFERS][AT_TILE * D * 2];
   __attribute__((aligned(1024))) char v[AT_BUFFERS][AT_TILE * D * 2];
+  int places[2][AT_PLACES];                             // of the tiles of a run, in turn
   __attribute__((aligned(8))) uint8_t odd[4][8];        // of tile t % 4; bit r: row r had a value not finite
 };
 
@@ -131,16 +133,35 @@ __device__ __forceinline__ void attend_tiles(const View& view, const bf16* K, co
   constexpr float NOTHING = AT_NEG_BIG, LAZY = 8.f;
 
   // ---- where rows are ----
-  // Page numbers are looked up by whole wavefronts: EIGHTS: lane 8 i + j for rows 8 j of tile i of the next eight
-  // tiles; else lane r for row r of the next tile.  Every wavefront has them all: its own rows, and what is missing.
-  constexpr int AT_ONCE = EIGHTS ? 8 : 1;
+  // Every wavefront has the places of all rows of a tile: its own, and what is missing.  EIGHTS: looked up by whole wavefronts,
+  // lane 8 i + j for rows 8 j of tile i of the next eight.  Else for 16 tiles at a time, a run ahead, kept in LDS: the
+  // compiler counts its own loads only, so to wait for a page number is to wait for every tile that is under way, which is
+  // not for each tile (24 ragged sequences of 220 tokens, pages of 20 rows: 63 us, 67 with a look-up by tile; 8192 tokens with EIGHTS
+  // from LDS too: 502, not 499).
   int next_page, next_slot, place = -1;
-  auto look_up = [&](int t) {                           // t: a multiple of AT_ONCE; tiles behind the last have no rows
-    const int tile = EIGHTS ? t + (lane >> 3) : t;
-    const int r = view.first_row(tile) + (EIGHTS ? (lane & 7) * 8 : lane);
-    const Pages::Entry e = pages.entry(view.seq, tile < n_tiles && r < view.end ? r : -1);
-    next_page = pages.table[e.at];
-    next_slot = e.slot;
+  struct Places { int all, own[2]; } next;              // of a tile: of row `lane`, and of the lane's own two
+  constexpr int RUN = EIGHTS ? 8 : AT_PLACES / 64;      // tiles
+  auto look_up = [&](int run) {                         // tiles behind the last have no rows
+    if constexpr (EIGHTS) {
+      const int tile = run * RUN + (lane >> 3), r = view.first_row(tile) + (lane & 7) * 8;
+      const Pages::Entry e = pages.entry(view.seq, tile < n_tiles && r < view.end ? r : -1);
+      next_page = pages.table[e.at];
+      next_slot = e.slot;
+    } else {
+#pragma unroll
+      for (int u = 0; u < AT_PLACES / (AT_WAVES * 64); ++u) {
+        const int e = u * AT_WAVES * 64 + tid, tile = run * RUN + e / 64;
+        if (tile >= n_tiles) break;
+        const int r = view.first_row(tile) + e % 64;
+        const Pages::Entry at = pages.entry(view.seq, r < view.end ? r : -1);
+        lds.places[run & 1][e] = pages.place(pages.table[at.at], h, at.slot);
+      }
+    }
+  };
+  auto places_of = [&](int t) -> Places {               // from LDS
+    const int* at = lds.places[t / RUN & 1] + t % RUN * 64;
+    const int* mine = at + wave * 8 + (lane >> 4);
+    return {at[lane], {mine[0], mine[4]}};
   };
   // Rows of a tile that are not there, as bits, of the last four tiles asked for (the newest first).
   uint64_t gone[4] = {0, 0, 0, 0};
@@ -162,9 +183,9 @@ __device__ __forceinline__ void attend_tiles(const View& view, const bf16* K, co
     }
   };
   auto rows_of = [&](int t) {                           // in turn: t = 0, 1, 2, ..
-    if ((t & (AT_ONCE - 1)) == 0) {
-      place = pages.place(next_page, h, next_slot);
-      look_up(t + AT_ONCE);
+    if (t % RUN == 0) {
+      if constexpr (EIGHTS) place = pages.place(next_page, h, next_slot);
+      look_up(t / RUN + 1);
     }
     Rows r;
     gone[3] = gone[2];
@@ -175,9 +196,11 @@ __device__ __forceinline__ void attend_tiles(const View& view, const bf16* K, co
       gone[0] = __ballot((none >> (lane >> 3)) & 1);    // bit j of none is rows 8 j .. 8 j + 7
       r.at[0] = max(__builtin_amdgcn_readlane(place, (t & 7) * 8 + wave), 0);
     } else {
-      gone[0] = __ballot(place < 0);
+      const bool is = t < n_tiles;
+      gone[0] = is ? __ballot(next.all < 0) : ~0ull;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) r.at[i] = max(__shfl(place, wave * 8 + 4 * i + (lane >> 4)), 0);
+      for (int i = 0; i < 2; ++i) r.at[i] = is ? max(next.own[i], 0) : 0;
+      next = places_of(t + 1);
     }
     return r;
   };
@@ -321,11 +344,15 @@ __device__ __forceinline__ void attend_tiles(const View& view, const bf16* K, co
   // values of t + 2, whose buffers were read for tile t - 1; what was asked for before that has to be there at its end.
   // Tiles behind the last one are asked for too (rows that the pool has): no conditions.
   if (n_tiles > 0) {
-    look_up(0);
 #pragma unroll
     for (int sl = 0; sl < 8; ++sl)
       q[sl] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + sl * 16 + half * 8));
+    look_up(0);
     __builtin_amdgcn_s_waitcnt(0);                      // the queries: no wait for them inside the loop
+    if constexpr (!EIGHTS) {
+      group_barrier();
+      next = places_of(0);
+    }
     Rows v_rows, k_rows = rows_of(0);
     bring(K, k_rows, own_k);
     auto request = [&](int t, uint32_t v_buffer, uint32_t k_buffer) {   // keys of tile t, values of t - 1
