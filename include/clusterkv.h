@@ -686,8 +686,9 @@ int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_st
  * group_starts [dev] int32 [n_groups + 1] ascending, n_groups <= S: group g is sequences [group_starts[g],
  *              group_starts[g + 1]).  Sequences before the first and behind the last group share nothing.
  * shared_rows  [dev] int32 [S]: the first shared_rows[s] rows of sequence s are those of the first sequence of its
- *              group too, through whose table they are read; that one's own number is the largest of the group.
- *              Any numbers, also within a page; taken as at least 0 and at most lengths[s].
+ *              group too, through whose table they are read, as far as that one's own number goes (what another shares
+ *              beyond it is read through its own table).  Any numbers, also within a page; taken as at least 0 and at
+ *              most lengths[s].
  * workspace    ck_workspace_bytes(sh, CK_WS_SHARED_ATTN, 0, 0); calls that share one must be ordered (its contents
  *              on entry do not matter).
  * CK_BF16: products as in ck_prompt_attn.  Where S times the rows that the table has room for are few (160 MB of keys and

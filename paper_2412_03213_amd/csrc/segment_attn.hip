@@ -70,6 +70,8 @@ struct Units {
   const SegmentArgs& a;
   __device__ __forceinline__ int count() const { return a.n_segments + (SHARED ? a.S : 0); }
   __device__ __forceinline__ int bound(int t) const { return t < 0 ? 0 : (t < a.n_rows ? t : a.n_rows); }
+  // rows that are read through the table of sequence s for its group
+  __device__ __forceinline__ int shared_of(int s) const { return max(0, min(a.shared[s], a.pages.clamp_length(a.lengths[s]))); }
   __device__ __forceinline__ Unit load(int i) const {
     Unit u = {0, 0, 0, 0, 0};
     if (i >= count()) return u;
@@ -79,8 +81,7 @@ struct Units {
       u.seq = i;
       if constexpr (SHARED) {
         u.seq = min(u.begin, a.S - 1);                  // the first of the group
-        const int n = min(a.shared[u.seq], a.pages.clamp_length(a.lengths[u.seq]));
-        u.end = u.tokens > 0 ? max(0, n) : 0;
+        u.end = u.tokens > 0 ? shared_of(u.seq) : 0;
       } else {
         u.end = a.pages.clamp_length(a.lengths[i]);
       }
@@ -90,7 +91,14 @@ struct Units {
       u.tokens = 1;
       u.end = a.pages.clamp_length(a.lengths[i]);
       const bool grouped = i >= a.starts[0] && i < a.starts[a.n_segments];
-      u.lo = grouped ? max(0, min(a.shared[i], u.end)) : 0;
+      int g = 0;                                        // the last group that begins at i or before
+      for (int n = a.n_segments; n > 1;) {
+        const int half = n >> 1;
+        g = a.starts[g + half] <= i ? g + half : g;
+        n -= half;
+      }
+      const int first = min(bound(a.starts[g]), a.S - 1);
+      u.lo = grouped ? min(shared_of(i), shared_of(first)) : 0;   // the rest through its own table
     }
     return u;
   }

@@ -381,3 +381,40 @@ def test_pools_beyond_32_bit_offsets():
         want, tol = attend(q[s].cpu(), k[:, 0].cpu(), v[:, 0].cpu(), np.ones((4, rows)), BF, p_step=P_STEP[BF])
         close(a[s], want, tol, f"shared {s}")
         close(b[s], want, tol, f"cross {s}")
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("lens,shares", [([64, 200, 130], [64, 90, 20]),      # the others share more than the first
+                                         ([20, 200, 130], [100, 100, 100]),   # the first is shorter than its number
+                                         ([0, 200, 7], [100, 100, 100])])     # ... and has no row at all
+def test_shared_no_further_than_the_first_goes(lens, shares, form):
+    """Rows that the first of a group does not share are read through each one's own table."""
+    n = max(0, min(shares[0], lens[0]))
+    groups, page = [0, 3], 16
+    c = shared_cache(groups, lens, [min(x, n) for x in shares], 2, page, form=form)
+    S, G = 3, 4
+    q = (torch.randn(S, 2 * G, D, generator=torch.Generator().manual_seed(4)) * 1.5).to(BF)
+    out = torch.full((S, 2 * G, D), float("nan"), dtype=BF, device=DEV)
+    ck.ck_shared_decode_attn(shape(S, 2, G), q.to(DEV), c.kv(), i32(lens), i32(groups), i32(shares), out)
+    for s, m in enumerate(lens):
+        for h in range(2):
+            want, tol = attend(q[s, h * G:(h + 1) * G], c.rows_k[s][h], c.rows_v[s][h], np.ones((G, m)), BF,
+                               p_step=P_STEP[BF])
+            close(out[s, h * G:(h + 1) * G], want, tol, f"sequence {s} head {h}")
+
+
+@pytest.mark.parametrize("S", [9, 700])
+def test_shared_groups_of_many_sizes_no_further_than_their_first(S):
+    groups, s = [1], 1
+    while s < S - 2:
+        s = min(S - 2, s + 1 + len(groups) % 4)
+        groups.append(s)
+    lens = [40 + (s * 37) % 60 for s in range(S)]
+    shares = [20 + (s * 13) % 70 for s in range(S)]
+    real = list(shares)
+    for a, b in zip(groups[:-1], groups[1:]):
+        for s in range(a, b):
+            real[s] = max(0, min(shares[s], shares[a], lens[a]))
+    real[0] = real[-1] = real[-2] = 0
+    c = shared_cache(groups, lens, real, 1, 16)
+    run_shared(groups, lens, shares, 1, 2, 16, cache=c)
