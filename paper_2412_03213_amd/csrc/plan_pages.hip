@@ -2,9 +2,9 @@
 //
 // Integers only, and few: what counts is the chain of steps that wait for each other.  One workgroup takes
 // all of them, so that a step waits for a barrier and not for a launch: pages taken over from parents, pages given back,
-// pages given out, slots.  Each step is a list of items (sequence, entry of its table); a prefix sum over the sequences
-// numbers them, and a thread finds the sequence of its item by binary search in LDS.  So a sequence with many
-// pages and many sequences with one are the same.  Free pages are those that nobody refers to: the counts are read
+// pages given out, slots.  Each step is a list of entries of tables, single ones or runs of up to 64; a prefix sum over the
+// sequences numbers them, and a thread finds the sequence of its entry or run by binary search in LDS.  So a sequence with
+// many pages and many sequences with one are the same.  Free pages are those that nobody refers to: the counts are read
 // once, 16 bytes a lane, and turned to bits in registers; the free page of rank r goes to item r.  Nothing depends
 // on the order of atomics.
 #include "paged.hpp"
@@ -15,14 +15,20 @@ namespace {
 
 // Threads of the planning workgroup.  Prefix sums are done by every wavefront for itself, over all of them: four are done
 // sooner where there are few sequences and few pages to take over or give back, for which the host has the table's size.  Tokens
-// given and taken back, two calls in a graph, four / sixteen, us: 64 sequences 11.2 / 13.6, 100 with a table of 502 entries each
-// 14.4 / 15.8, 12000 pages taken over and 16500 given back 94 / 71.
+// given and taken back, two calls in a graph, four / sixteen, us: 64 sequences 11.0 / 13.8, 100 with a table of 502 entries each
+// 13.8 / 16.0, 64 prompts of 1000 tokens 32.5 / 24.2, 12000 pages taken over and 16500 given back 118 / 61.
 constexpr int PL_FEW = 256, PL_MANY = 1024, PL_FEW_ENTRIES = 65536;
 constexpr int PL_LOADS = 32;                            // runs of 256 pages that a wavefront looks at together, at most
 // ... and the workgroup to begin with, four times as many in each turn.  A token for each of 64 sequences (5 pages of 16384)
 // and taken back, two calls in a graph: 11.2 us, 11.8 with 32 runs, 10.9 with 8; 14.0, 14.7 and 16.1 where no page is free.
 constexpr int PL_FIRST_RUNS = 16;
-constexpr int PL_ITEMS = 4;                             // of a thread at a time
+constexpr int PL_RUNS = 4;                              // of entries that a wavefront takes together (8: as fast)
+// Where many counts change, those of the first pages do in LDS, 16 bits each, and then once in memory: a compute unit takes
+// 4.5 cycles for an atomic to memory.  Two calls, us, with / without: 4000 entries given back in a pool of 16384 pages 26.0 /
+// 27.7; 12000 taken over and 16500 given back in one of 32768 49.5 / 65.7, of 131072 61.2 / 69.3.
+constexpr int PL_COUNTED = 65536, PL_COUNTED_MANY = 32768;   // pages; the smaller number where sequences need the room
+constexpr int PL_COUNTED_S = 1024;
+constexpr int PL_LEAST = 2000, PL_MOST = 32768;         // entries that are taken over, or given back, for that: [least, most)
 constexpr int PL_LIST = 2048;                           // free pages that are given out together
 // Rows whose slots the planning workgroup writes itself; more are left to a launch of their own (two calls, us: 2400 rows
 // 13.1 and 13.6, 4000 14.1 and 13.7, 16000 21.6 and 14.8).
@@ -62,6 +68,9 @@ __device__ __forceinline__ void scan_two(int& x, int& y, int& x_before, int& y_b
   x_before = all.x;
   y_before = all.y;
 }
+
+// Up to 64 entries of one sequence: read from, written to, as numbers in the table.
+struct Run { int from, to, n; };
 
 // The first i of [0, n) with upto[i] > x (n - 1 if there is none), for several x at a time; upto ascends.
 template <int N>
@@ -108,7 +117,7 @@ __device__ __forceinline__ void memory_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
-template <int THREADS>
+template <int THREADS, int COUNTED>
 __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   constexpr int WAVES = THREADS / 64;
   extern __shared__ int lds[];
@@ -118,29 +127,50 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   __shared__ int behind;                                // pages that the table has no entry for
   __shared__ int list[PL_LIST];                         // free pages
   __shared__ int free_upto[PL_LOADS * WAVES];           // free pages of a run; then before it
+  __shared__ int4 changes[COUNTED / 8];                 // of the counts of the first pages: even ones in the lower half of a word
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int ps = (int)a.size.d;
   auto after = [&](int s, int n) {                      // rows of a sequence after the call
     const int64_t x = (int64_t)rows[s] + n;
     return (int)(x < 0 ? 0 : (x < 0x7FFFFFFF ? x : 0x7FFFFFFF));
   };
-  // Items of all sequences, numbered through upto[]: get(sequence, item of it) asks for what put takes.  Several at a
-  // time: an item is a chain of look-ups, one after the other.
-  auto for_items = [&](int total, auto get, auto put) {
-    for (int r0 = tid; r0 < total; r0 += PL_ITEMS * THREADS) {
-      decltype(get(0, 0)) x[PL_ITEMS];
-      int r[PL_ITEMS], s[PL_ITEMS];
+  const int counted = min(COUNTED, a.n_pages);
+  bool in_lds = false;                                  // changes[] is in use
+  auto count_in_lds = [&](int entries) {
+    if (in_lds || entries < PL_LEAST) return;
+    for (int i = tid; i < (counted + 7) / 8; i += THREADS) changes[i] = make_int4(0, 0, 0, 0);
+    in_lds = true;
+  };
+  auto change = [&](int page, int by, bool here) {
+    if (here && page < counted)
+      atomicAdd(reinterpret_cast<int*>(changes) + (page >> 1), by * (page & 1 ? 65536 : 1));
+    else
+      atomicAdd(a.refs + page, by);
+  };
+  // Entries of all sequences, up to 64 of one of them at a time, numbered through upto[]: a lane finds one such run, of(sequence,
+  // number of its run), for its wavefront, which then takes them one after the other, an entry each lane.
+  auto for_runs = [&](int total, auto of, auto put) {
+    for (int x0 = 0; x0 < total; x0 += THREADS) {
+      const int x = min(x0 + lane * WAVES + wave, total - 1);
+      const int s = first_beyond(upto, a.S, x);
+      const Run mine = of(s, x - (s > 0 ? upto[s - 1] : 0));
+      const int runs = min((total - x0 - wave + WAVES - 1) / WAVES, WAVE);   // of this wavefront
+      for (int k = 0; k < runs; k += PL_RUNS) {
+        int to[PL_RUNS], n[PL_RUNS], page[PL_RUNS];
 #pragma unroll
-      for (int u = 0; u < PL_ITEMS; ++u) r[u] = min(r0 + u * THREADS, total - 1);   // the last one again behind the end
-      first_beyond<PL_ITEMS>(upto, a.S, r, s);
+        for (int u = 0; u < PL_RUNS; ++u) {
+          const int i = min(k + u, runs - 1);
+          const int from = __builtin_amdgcn_readlane(mine.from, i);
+          to[u] = __builtin_amdgcn_readlane(mine.to, i);
+          n[u] = k + u < runs ? __builtin_amdgcn_readlane(mine.n, i) : 0;
+          page[u] = lane < n[u] ? a.table[(uint32_t)(from + lane)] : -1;
+        }
 #pragma unroll
-      for (int u = 0; u < PL_ITEMS; ++u) x[u] = get(s[u], r[u] - (s[u] > 0 ? upto[s[u] - 1] : 0));
-#pragma unroll
-      for (int u = 0; u < PL_ITEMS; ++u)
-        if (r0 + u * THREADS < total) put(x[u]);
+        for (int u = 0; u < PL_RUNS; ++u)
+          if (lane < n[u]) put(a.table + (uint32_t)(to[u] + lane), page[u]);
+      }
     }
   };
-  struct Entry { int32_t* at; int page; };
 
   // the counts of pages p to p + 3; behind the last there are no free ones
   auto counts_of = [&](int p) {
@@ -159,10 +189,10 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
   if (tid == 0) behind = 0;
 
   // ---- sequences without rows take over whole pages of a parent, as it stands before the call ----
-  int taken = 0, unused = 0, less = 0;
+  int taken = 0, taken_entries = 0, less = 0;
   for (int s0 = 0; s0 < a.S; s0 += THREADS) {
     const int s = s0 + tid;
-    int pages = 0, zero = 0;
+    int pages = 0;
     if (s < a.S) {
       const int n = a.n_new[s], old = max(a.lengths[s], 0);
       less |= n < 0;
@@ -176,45 +206,94 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
       rows[s] = old + pages * ps;
     }
     if (a.parent) {
-      scan_two<WAVES>(pages, zero, taken, unused, tmp);
-      if (s < a.S) upto[s] = pages;
+      int runs = (pages + WAVE - 1) / WAVE;
+      scan_two<WAVES>(runs, pages, taken, taken_entries, tmp);
+      if (s < a.S) upto[s] = runs;
     }
   }
+  count_in_lds(taken_entries);
   less = __syncthreads_or(less);
   if (taken > 0) {
-    for_items(taken,
-              [&](int s, int e) -> Entry {
-                return {a.table + (uint32_t)(s * a.per_seq + e), a.table[(uint32_t)(a.parent[s] * a.per_seq + e)]};
-              },
-              [&](const Entry& x) {
-                const bool is = a.is_page(x.page);
-                *x.at = is ? x.page : -1;
-                if (is) atomicAdd(a.refs + x.page, 1);
-              });
+    const bool here = in_lds && taken_entries < PL_MOST;
+    for_runs(taken,
+             [&](int s, int k) -> Run {
+               const int e = k * WAVE;
+               return {a.parent[s] * a.per_seq + e, s * a.per_seq + e, min(a.size.quotient(rows[s]) - e, WAVE)};
+             },
+             [&](int32_t* at, int page) {
+               const bool is = a.is_page(page);
+               *at = is ? page : -1;
+               if (is) change(page, 1, here);
+             });
     memory_barrier();
   }
 
   // ---- pages that hold no row any more are given back ----
   if (less) {
-    int given = 0;
+    int given = 0, given_entries = 0;
     for (int s0 = 0; s0 < a.S; s0 += THREADS) {
       const int s = s0 + tid;
-      int n = 0, zero = 0;
+      int pages = 0;
       if (s < a.S && a.n_new[s] < 0)
-        n = max(0, min(a.pages_of(rows[s]), a.per_seq) - a.pages_of(after(s, a.n_new[s])));
-      scan_two<WAVES>(n, zero, given, unused, tmp);
+        pages = max(0, min(a.pages_of(rows[s]), a.per_seq) - a.pages_of(after(s, a.n_new[s])));
+      int n = (pages + WAVE - 1) / WAVE;
+      scan_two<WAVES>(n, pages, given, given_entries, tmp);
       if (s < a.S) upto[s] = n;
     }
+    count_in_lds(given_entries);
+    const bool here = in_lds && given_entries < PL_MOST;
     __syncthreads();
-    for_items(given,
-              [&](int s, int i) -> Entry {
-                int32_t* at = a.table + (uint32_t)(s * a.per_seq + a.pages_of(after(s, a.n_new[s])) + i);
-                return {at, *at};
-              },
-              [&](const Entry& x) {
-                *x.at = -1;
-                if (a.is_page(x.page)) atomicAdd(a.refs + x.page, -1);
-              });
+    for_runs(given,
+             [&](int s, int k) -> Run {
+               const int e = a.pages_of(after(s, a.n_new[s])) + k * WAVE, at = s * a.per_seq + e;
+               return {at, at, min(min(a.pages_of(rows[s]), a.per_seq) - e, WAVE)};
+             },
+             [&](int32_t* at, int page) {
+               *at = -1;
+               if (a.is_page(page)) change(page, -1, here);
+             });
+    memory_barrier();
+  }
+
+  // ---- what was counted in LDS, eight pages a thread; nobody else changes counts now ----
+  if (in_lds) {
+    constexpr int EACH = 2;
+    for (int i0 = tid; i0 * 8 < counted; i0 += EACH * THREADS) {
+      int4 d[EACH], c[EACH][2];
+      auto whole = [&](int i) { return i * 8 + 7 < counted; };
+      auto some = [&](int u) { return (d[u].x | d[u].y | d[u].z | d[u].w) != 0; };
+      auto add = [](int4 c, int x, int y) {
+        const int x0 = (short)x, y0 = (short)y;
+        return make_int4(c.x + x0, c.y + ((x - x0) >> 16), c.z + y0, c.w + ((y - y0) >> 16));
+      };
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) {
+        const int i = i0 + u * THREADS;
+        d[u] = i * 8 < counted ? changes[i] : make_int4(0, 0, 0, 0);
+        if (some(u) && whole(i)) {
+          const int4* at = reinterpret_cast<const int4*>(a.refs + 8 * i);
+          c[u][0] = at[0];
+          c[u][1] = at[1];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) {
+        const int i = i0 + u * THREADS;
+        if (!some(u)) continue;
+        if (whole(i)) {
+          int4* at = reinterpret_cast<int4*>(a.refs + 8 * i);
+          at[0] = add(c[u][0], d[u].x, d[u].y);
+          at[1] = add(c[u][1], d[u].z, d[u].w);
+        } else {                                        // the last pages
+          const int w[4] = {d[u].x, d[u].y, d[u].z, d[u].w};
+          for (int k = 0; k < 4; ++k) {
+            const int even = (short)w[k], odd = (w[k] - even) >> 16;
+            if (even) a.refs[8 * i + 2 * k] += even;    // there are no changes of pages that are not
+            if (odd) a.refs[8 * i + 2 * k + 1] += odd;
+          }
+        }
+      }
+    }
     memory_barrier();
   }
 
@@ -283,7 +362,7 @@ __global__ __launch_bounds__(THREADS) void k_plan_pages(const PlanArgs a) {
       for (int k = mine; k < loads; ++k) free_upto[k * WAVES + wave] = 0;
     __syncthreads();
     const bool run = tid < loads * WAVES;
-    int n = run ? free_upto[tid] : 0, zero = 0;
+    int n = run ? free_upto[tid] : 0, zero = 0, unused = 0;
     const int n_run = n, found_before = found;
     scan_two<WAVES>(n, zero, found, unused, tmp);
     if (run) free_upto[tid] = n - n_run;                // before the run
@@ -362,9 +441,11 @@ hipError_t launch_plan_pages(int S, const int32_t* n_new, int32_t* lengths, int3
   a.n_rows = (int)n_rows;
   a.size = Divider((uint32_t)page_size);
   if (S <= PL_FEW && (int64_t)S * pages_per_seq <= PL_FEW_ENTRIES && n_rows <= 4 * PL_FEW)
-    hipLaunchKernelGGL(k_plan_pages<PL_FEW>, dim3(1), dim3(PL_FEW), (size_t)S * 2 * sizeof(int), st, a);
+    hipLaunchKernelGGL((k_plan_pages<PL_FEW, PL_COUNTED>), dim3(1), dim3(PL_FEW), (size_t)S * 2 * sizeof(int), st, a);
+  else if (S <= PL_COUNTED_S)
+    hipLaunchKernelGGL((k_plan_pages<PL_MANY, PL_COUNTED>), dim3(1), dim3(PL_MANY), (size_t)S * 2 * sizeof(int), st, a);
   else
-    hipLaunchKernelGGL(k_plan_pages<PL_MANY>, dim3(1), dim3(PL_MANY), (size_t)S * 2 * sizeof(int), st, a);
+    hipLaunchKernelGGL((k_plan_pages<PL_MANY, PL_COUNTED_MANY>), dim3(1), dim3(PL_MANY), (size_t)S * 2 * sizeof(int), st, a);
   if (a.slots && n_rows > PL_OWN_ROWS)
     hipLaunchKernelGGL(k_plan_slots, dim3((unsigned)((n_rows + PL_SLOT_ROWS - 1) / PL_SLOT_ROWS)), dim3(PL_MANY),
                        (size_t)S * sizeof(int), st, a);

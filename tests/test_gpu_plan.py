@@ -389,3 +389,27 @@ def test_tensors_on_another_device_are_refused(monkeypatch):
                  lambda: ck.ck_shared_decode_attn(sh2, q, kv1, n, starts, n, q.clone())):
         with pytest.raises(ValueError, match="current"):
             call()
+
+
+@pytest.mark.parametrize("S,n_pages,width", [(130, 9003, 130), (130, 70001, 600), (1100, 40000, 20)])
+def test_plan_many_pages_of_many_at_once(S, n_pages, width):
+    """Enough entries for counts in LDS: pages at the end of what it holds and behind it, counted once for each of many."""
+    rng = np.random.default_rng(S + width)
+    far = n_pages * 15 // 16                              # free: a few pages before, all behind
+    x = Steps(S, width, n_pages, 4, held=rng.choice(far, far - far // 200, replace=False).tolist())
+    long = min(width - 4, 90) * 4 - 1
+    x.step([long, long + 1, long] + [0] * (S - 3))
+    x.step([0, 3, 0] + [int(v) for v in rng.integers(0, 9, S - 3)], parent=[s % 3 for s in range(S)], shared=[10 ** 6] * S)
+    x.step([int(v) for v in rng.integers(-long, 5, S)])
+    x.step([INT_MIN if s % 7 else 1 for s in range(S)], parent=[1] * S, shared=[long] * S)
+    x.step([INT_MIN] * S)
+    assert sum(x.b.refs) == far - far // 200
+
+
+def test_plan_more_entries_than_counts_in_lds_hold():
+    x = Steps(100, 400, 500, 1)
+    x.step([390] + [0] * 99)
+    x.step([0] * 100, parent=[0] * 100, shared=[380] * 100)   # 37620 entries of 380 pages
+    assert x.b.refs[0] == 100
+    x.step([INT_MIN] * 100)
+    assert sum(x.b.refs) == 0
