@@ -115,8 +115,8 @@ struct QueryState {
 //   my_first, my_end          tiles that some query of the wavefront sees something of lie in [my_first, my_end)
 // q_row: the lane's query, in 16-byte pieces of this lane: channels 16 sl + 8 (lane / 32) + (0..7).
 // EIGHTS: pages hold whole groups of 8 rows, so that the 8 rows that a wavefront brings of a tile are in one page: one
-// address, and page numbers looked up for eight tiles at a time.  8192 tokens 479 us, row by row 495; chunks with a
-// window 197 and 204 (timed in turn, pages of 64 and 32 rows).
+// address, and page numbers looked up for eight tiles at a time.  8192 tokens 489 us, row by row 501; chunks with a
+// window 199 and 205 (timed in turn, pages of 64 and 32 rows).
 template <bool EIGHTS, class View>
 __device__ __forceinline__ void attend_tiles(const View& view, const bf16* K, const bf16* V, const Pages& pages, int h,
                                              float scale_log2e, const bf16* q_row, bool once, TileBuffers& lds,

@@ -312,8 +312,11 @@ __global__ __launch_bounds__(THREADS) void k_segment_plan(const SegmentArgs a) {
       p.result = cut[s].y < 0 ? -1 : cut[s].y + piece * v.tokens + block * U::TOKENS;
       return p;
     };
-    // Those that take longest go first, so that what runs at the end is short.  Which of a class comes first changes no
-    // result: where each leaves its results does not depend on it.
+    // Those that take longest go first, so that what runs at the end is short.  us, longest first, shortest first and as they
+    // come: 64 sequences that share 32768 rows 107, 142, 108; 5 ragged groups 35.5, 38, 38.5; 32 members with 16384 shared and
+    // up to 4000 of their own 69, 75, 78; cross attention of 40 x 20 tokens over 600 to 6000 rows 107, 119, 135, of 24 x 220
+    // over 5000 164, 197, 178.  (16 sequences that share 131072: 103 to 108, 101, 100; 8 groups of 8 54.5, 62, 58.)
+    // Which of a class comes first changes no result: where each leaves its results does not depend on it.
     auto class_of = [&](const Piece& p) {
       const float share = (float)p.n_tiles * tile_cost(p.n_tok * G, p.flags & Piece::SEVERAL ? 2 : 1) / within;
       return max(0, min(SG_CLASSES - 1, SG_CLASSES - 1 - (int)(share * SG_CLASSES)));
