@@ -507,26 +507,42 @@ reduced:
   }
 }
 
-// Block x of the segments, all of its rows; by every wavefront for itself.
+// Block x of the segments, all of its rows; by every wavefront for itself.  Of up to 64 segments whose blocks do not fit on
+// the chip together those with the longest states come first, so that what runs at the end is short: 64 x 16 tokens over 1500 to
+// 3000 rows (512 blocks) 101 us, not 110, 40 x 60 over 750 to 1500 (320) 63, not 72.  Of more blocks many begin and
+// end together then, while memory waits: 100 x 30 over 500 to 1000 rows (800) 81, not 78.
 template <int G>
 __device__ __forceinline__ bool whole_block(const SegmentArgs& a, int x, Piece* p) {
   using U = Units<G, false>;
   const U units{a};
-  int before = 0;
+  auto last = [](int v) { return __builtin_amdgcn_readlane(v, WAVE - 1); };
   for (int i0 = 0; i0 < a.n_segments; i0 += WAVE) {
     const Unit u = units.load(i0 + (threadIdx.x & 63));
-    const int n = U::blocks(u), upto = before + wave_inclusive_scan(n);
-    const uint64_t beyond = __ballot(upto > x);
-    if (beyond) {
-      const int l = __builtin_ctzll(beyond);
-      auto get = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      const Unit v = {get(u.begin), get(u.tokens), get(u.seq), 0, get(u.end)};
-      const int block = x - (get(upto) - get(n));
-      *p = {v.begin + block * U::TOKENS, (short)min(U::TOKENS, v.tokens - block * U::TOKENS),
-            (short)(U::blocks(v) > 1 ? Piece::SEVERAL : 0), v.seq, 0, v.end, 0, v.tiles(), -1};
-      return block >= 0;
+    int n = U::blocks(u), upto = wave_inclusive_scan(n);
+    const int all = last(upto);
+    if (x >= all) {
+      x -= all;
+      continue;
     }
-    before = __builtin_amdgcn_readlane(upto, WAVE - 1);
+    if (a.n_segments <= WAVE && all * a.Hkv > SG_CUS && all * a.Hkv <= 3 * SG_CUS) {
+      // bit by bit of their numbers of tiles, the five highest that one can have: are there more than x blocks with a one?
+      const int tiles = u.tiles(), top = 31 - __builtin_clz((a.pages.rows + AT_TILE - 1) / AT_TILE);
+      for (int b = top; b >= max(0, top - 4); --b) {
+        const bool one = (tiles >> b) & 1;
+        const int ones = last(wave_inclusive_scan(one ? n : 0));
+        const bool among = x < ones;
+        x -= among ? 0 : ones;
+        n = one == among ? n : 0;                       // the others are out
+      }
+      upto = wave_inclusive_scan(n);
+    }
+    const int l = __builtin_ctzll(__ballot(upto > x));
+    auto get = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+    const Unit v = {get(u.begin), get(u.tokens), get(u.seq), 0, get(u.end)};
+    const int block = x - (get(upto) - get(n));
+    *p = {v.begin + block * U::TOKENS, (short)min(U::TOKENS, v.tokens - block * U::TOKENS),
+          (short)(U::blocks(v) > 1 ? Piece::SEVERAL : 0), v.seq, 0, v.end, 0, v.tiles(), -1};
+    return block >= 0;
   }
   return false;
 }
@@ -778,17 +794,19 @@ struct Space {
 };
 
 // Whether every block is left to one workgroup, whatever the lengths are: the plan and the join cost 8 to 9 us, which cutting
-// and sorting have to spare.  The host knows the table's width and takes it for the longest sequence, and that segments
-// are not empty.  us, direct / planned, 8 heads of G = 4, lengths of 0.1 to 1 and 0.7 to 1 of N rows:
-//   1 sequence, 64 tokens (8 blocks)      256 rows - and 12 / 19, 768 - and 24 / 20
-//   8 of 20 tokens (64)                   1024 rows 22 / 25, 1536 30 / 26
-//   16 of 20 (128)                        1536 30 / 31, 2048 38 / 35
-//   64 of 16 (512)                        4000 108 / 124; 3000 rows of 0.7 to 1 118 / 139
-//   24 of 200 (600 full blocks)           768 43 / 39, 4000 140 / 121; 3000 rows of 0.7 to 1 214 / 218
+// has to spare.  The host knows the table's width and takes it for the longest sequence, and that segments are not empty.
+// us, direct / planned, 8 heads of G = 4, lengths of 0.7 to 1 and 0.1 to 1 of N rows, tokens likewise:
+//   N                      768               1536              2500               4000
+//   1 x 64 tokens          24 / 22           41 / 26           64 / 32            96 / 41
+//   8 x 20                 20 / 22, 19 / 26  31 / 27, 31 / 28  48 / 31, 47 / 28   70 / 38, 70 / 34
+//   16 x 20                20 / 27, 19 / 26  32 / 39, 31 / 29  49 / 51, 48 / 36   71 / 56, 71 / 46
+//   16 x 100               29 / 35, 25 / 31  47 / 53, 42 / 48  73 / 78, 65 / 63   106 / 114, 97 / 87
+//   64 x 16                40 / 46, 30 / 38  66 / 75, 47 / 59  99 / 111, 70 / 78  150 / 162, 103 / 113
+//   24 x 200               70 / 77, 34 / 39  116 / 124, 48 / 57  174 / 185, 72 / 79  275 / 277, 107 / 117
+//   48 x 200               116 / 123, 63 / 66  215 / 218, 99 / 97  339 / 327, 150 / 138  514 / 516, 222 / 213
 bool goes_direct(const Dims& dm, int64_t n_rows, int64_t rows) {
-  const int64_t full = n_rows / (AT_ROWS / dm.G) * dm.Hkv, segments = (n_rows < dm.S ? n_rows : dm.S) * dm.Hkv;
-  const int64_t blocks = full > segments ? full : segments;
-  return rows <= (blocks < 64 || full >= SG_CUS ? 768 : (blocks < SG_CUS ? 1536 : 4096));
+  const int64_t blocks = (n_rows / (AT_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S)) * dm.Hkv;   // at most
+  return rows <= (blocks < 64 ? 768 : (blocks < 128 ? 1280 : (blocks < SG_CUS ? 2048 : 4096)));
 }
 
 hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv, const Space& space, void* workspace,

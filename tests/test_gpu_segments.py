@@ -418,3 +418,12 @@ def test_shared_groups_of_many_sizes_no_further_than_their_first(S):
     real[0] = real[-1] = real[-2] = 0
     c = shared_cache(groups, lens, real, 1, 16)
     run_shared(groups, lens, shares, 1, 2, 16, cache=c)
+
+
+@pytest.mark.parametrize("S,page", [(40, 16), (64, 20)])
+def test_cross_blocks_that_begin_in_the_order_of_their_lengths(S, page):
+    # more than fit on the chip, in one launch; some of equal length, some empty, some without tokens, some of several blocks
+    lens = [(s * 197) % 701 // 100 * 100 + s % 3 for s in range(S)]
+    news = [0 if s % 11 == 5 else 1 + (5 * s) % 9 for s in range(S)]
+    lens[3], news[2], news[3], lens[S - 1] = 0, 150, 4, 1300
+    run_cross(lens, news, 8, 4, page)
