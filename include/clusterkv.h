@@ -38,7 +38,8 @@
  *  - Integer outputs are bit-reproducible from run to run.  Floating-point
  *    outputs are too (no floating-point atomics are used anywhere).
  *  - Supported: d == 128; Hq / Hkv in {1, 2, 4, 8}; cluster counts up to
- *    CK_MAX_CLUSTERS per head-problem.
+ *    CK_MAX_CLUSTERS per head-problem; at most 65535 head-problems (S * Hkv) in a
+ *    call, except in ck_plan_pages.
  *  - Caches in pages have a layout of their own (ck_paged_kv, below).
  */
 #ifndef CLUSTERKV_H
@@ -661,7 +662,9 @@ int ck_copy_rows(const ck_shape* sh, const ck_paged_kv* src, const ck_paged_kv* 
  *            page; -1 for a row on no page and from q_starts[S] on.
  * lacking    [dev] int32 [1] out: pages that could not be given, as none was free (entry -1) or the table has no entry.
  *            Lengths grow all the same: rows on no page are not stored and not attended.
- * Only sh->S counts, S <= 8192; n_pages <= 2^30; the sums of new tokens and of a sequence's rows have to stay below 2^31.  A page that
+ * sh has to be a supported one, of which only S counts: S <= 8192 with any number of heads.  n_pages and a sequence's
+ * pages_per_seq * page_size are at most 2^30, S * pages_per_seq and the pool's n_pages * page_size below 2^31, n_rows at most
+ * 2^24; the sums of new tokens and of a sequence's rows have to stay below 2^31.  A page that
  * others refer to too must not get rows: share whole pages, as a parent's are, and ck_copy_rows for the rest.
  */
 int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, int32_t* page_table,

@@ -30,7 +30,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
     if ((p) && !aligned16(p)) return fail(CK_EMISALIGNED, "%s is not 16-byte aligned", #p); \
   } while (0)
 
-int check_shape(const ck_shape* sh, ck::Dims* dm, bool need_bf16) {
+// A model that the library serves, for any number of sequences.
+int check_model(const ck_shape* sh) {
   if (!sh) return fail(CK_EINVALID, "shape is NULL");
   if (sh->S < 1 || sh->Hq < 1 || sh->Hkv < 1 || sh->N_cap < 1 || sh->C_cap < 1)
     return fail(CK_EINVALID, "S, Hq, Hkv, N_cap and C_cap must be positive");
@@ -42,15 +43,21 @@ int check_shape(const ck_shape* sh, ck::Dims* dm, bool need_bf16) {
     return fail(CK_EUNSUPPORTED, "GQA group size %d (only 1, 2, 4, 8)", G);
   if (sh->dtype != CK_BF16 && sh->dtype != CK_F32)
     return fail(CK_EINVALID, "unknown dtype %d", sh->dtype);
+  if (sh->N_cap > (int64_t)0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "N_cap exceeds int32 rows");
+  return CK_OK;
+}
+
+int check_shape(const ck_shape* sh, ck::Dims* dm, bool need_bf16) {
+  const int rc = check_model(sh);
+  if (rc) return rc;
   if (need_bf16 && sh->dtype != CK_BF16)
     return fail(CK_EUNSUPPORTED, "clustering runs on bf16 keys only");
-  if (sh->N_cap > (int64_t)0x7FFFFFFF) return fail(CK_EUNSUPPORTED, "N_cap exceeds int32 rows");
   if ((int64_t)sh->S * sh->Hkv > 65535)
     return fail(CK_EUNSUPPORTED, "more than 65535 head-problems in one call");
   dm->S = sh->S;
   dm->Hq = sh->Hq;
   dm->Hkv = sh->Hkv;
-  dm->G = G;
+  dm->G = sh->Hq / sh->Hkv;
   dm->HP = sh->S * sh->Hkv;
   dm->N_cap = sh->N_cap;
   dm->C_cap = sh->C_cap;
@@ -1030,8 +1037,7 @@ int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, in
                   int32_t pages_per_seq, int32_t* page_refs, int32_t n_pages, int32_t page_size,
                   const int32_t* parent, const int32_t* shared_rows, int32_t* q_starts, int32_t* slots,
                   int64_t n_rows, int32_t* lacking, void* stream) {
-  ck::Dims dm;
-  int rc = check_shape(sh, &dm, false);
+  const int rc = check_model(sh);                       // nothing here is done for each head
   if (rc) return rc;
   if (sh->S > ck::MAX_PLANNED)
     return fail(CK_EUNSUPPORTED, "%d sequences (at most %d)", sh->S, ck::MAX_PLANNED);
