@@ -215,7 +215,7 @@ __global__ __launch_bounds__(THREADS) void k_segment_plan(const SegmentArgs a) {
   work = all_sum(work);
   const float least = fmaxf(work.x * (float)a.Hkv / SG_CUS, 6.f);
 
-  // ---- and how long it has to be given, so that the pieces fit: a wavefront tries one length ----
+  // ---- and how long it has to be given, so that the pieces fit the chip and the workspace: a wavefront tries one length ----
   float within = least * 1.25f, extra = 0.f;            // extra: pieces that are more than blocks
   int winner = 0;
   if (model) {
@@ -238,7 +238,9 @@ __global__ __launch_bounds__(THREADS) void k_segment_plan(const SegmentArgs a) {
     int uncut = -1;
 #pragma unroll
     for (int w = SG_TRIES - 1; w >= 0; --w) {
-      const bool fits = needed[w].x <= (float)SG_CUS;
+      // 144 x 2 tokens over 11759 rows, 2 heads, G = 4: two pieces each (288 more than blocks) 305 us; three fit the chip in less
+      // time, but are 576 more, and without the second condition nothing was cut then: 346 us
+      const bool fits = needed[w].x <= (float)SG_CUS && needed[w].y * (float)a.Hkv <= (float)SG_EXTRA;
       winner = fits ? w : winner;
       uncut = fits && needed[w].y == 0.f ? w : uncut;
     }
