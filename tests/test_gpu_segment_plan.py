@@ -158,3 +158,16 @@ def test_groups_just_above_the_compute_units_are_cut():
     counts = c.pieces(ws)
     assert CUS < 144 * 2 < 2 * CUS and all(k > 1 for k in counts[:144]) and c.extra(counts) <= EXTRA
     c.check(out, only=(0, 1, 143, 286, 287))
+
+
+@pytest.mark.parametrize("n,m,Hkv,G", [(3548, 405, 2, 8), (8579, 492, 1, 4), (2640, 357, 4, 1)])
+def test_even_shares_fit_the_compute_units(n, m, Hkv, G):
+    """Full blocks of 256 queries leave 20 us of results in every piece, more than the whole call should take: no cut that is
+    tried fits, and shares are even."""
+    c = Call([n] * (4 if Hkv == 4 else 1), Hkv, G, 16, width=4097 // 16 + 1)
+    out, ws = c.run([m] * len(c.lens))
+    counts = c.pieces(ws)
+    even = -(-sum(c.blocks()) * -(-n // TILE) * Hkv // CUS)          # tiles of a share, before it is made longer
+    assert 1 < counts[0] // c.blocks()[0] <= -(-n // TILE) // even + 1
+    assert sum(counts) * Hkv <= CUS and c.extra(counts) <= EXTRA
+    c.check(out)
