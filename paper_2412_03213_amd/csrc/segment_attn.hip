@@ -820,8 +820,20 @@ struct Space {
 //   64 x 16                40 / 46, 30 / 38  66 / 75, 47 / 59  99 / 111, 70 / 78  150 / 162, 103 / 113
 //   24 x 200               70 / 77, 34 / 39  116 / 124, 48 / 57  174 / 185, 72 / 79  275 / 277, 107 / 117
 //   48 x 200               116 / 123, 63 / 66  215 / 218, 99 / 97  339 / 327, 150 / 138  514 / 516, 222 / 213
+// Every workgroup walks over the segments, 64 a turn, until it has its own (0.3 us a turn); the plan does that once.  us, direct /
+// planned, tokens of G = 4 over 0.5 to 1 of 100, 700 and 2000 rows, by turns x blocks:
+//   512 x 4 tokens, 1 head         4300       16 / 27, 33 / 44, 73 / 83
+//   1024 x 4, 1 head              17000       35 / 42, 63 / 75, 137 / 154
+//   512 x 4, 8 heads              35000       106 / 100, 225 / 230, 509 / 524
+//   2048 x 4, 1 head              70000       86 / 61, 137 / 125, 269 / 280
+//   768 x 1, 8 heads              75000       147 / 125, 299 / 288, 710 / 725
+//   1024 x 4, 8 heads            139000       243 / 184, 472 / 446, 1022 / 1037
+//   4000 x 4, 8 heads           2100000       1856 / 677, 2609 / 1760
+//   60000, of which 100 have a token, 1 head  95000  253 / 249 (100 rows)
+constexpr int64_t SG_WALK = 65536;
 bool goes_direct(const Dims& dm, int64_t n_rows, int64_t rows) {
   const int64_t blocks = (n_rows / (AT_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S)) * dm.Hkv;   // at most
+  if (dm.S / WAVE * blocks >= SG_WALK) return false;
   return rows <= (blocks < 64 ? 768 : (blocks < 128 ? 1280 : (blocks < SG_CUS ? 2048 : 4096)));
 }
 

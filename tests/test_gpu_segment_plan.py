@@ -171,3 +171,22 @@ def test_even_shares_fit_the_compute_units(n, m, Hkv, G):
     assert 1 < counts[0] // c.blocks()[0] <= -(-n // TILE) // even + 1
     assert sum(counts) * Hkv <= CUS and c.extra(counts) <= EXTRA
     c.check(out)
+
+
+@pytest.mark.parametrize("S,Hkv", [(4000, 2), (8000, 8), (30000, 1)])
+def test_many_segments_are_planned(S, Hkv):
+    """In one launch every workgroup walks over all segments to find its own: for so many the plan does it once."""
+    lens = [(7 * s) % 97 for s in range(S)]
+    c = Call(lens, Hkv, 2, 16)
+    out, ws = c.run([(s % 3 > 0) + (s % 1000 == 7) for s in range(S)])
+    assert planned(ws)
+    c.pieces(ws)
+    c.check(out, only=[*range(20), *range(1000, 1010), *range(S - 20, S)])
+
+
+@pytest.mark.parametrize("S", [64, 500])
+def test_segments_of_short_states_go_in_one_launch(S):
+    c = Call([(7 * s) % 97 for s in range(S)], 2, 2, 16)
+    out, ws = c.run([s % 3 for s in range(S)])
+    assert not planned(ws)
+    c.check(out, only=[0, 1, 2, S - 1])
