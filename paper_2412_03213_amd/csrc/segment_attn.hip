@@ -820,6 +820,10 @@ struct Space {
 //   64 x 16                40 / 46, 30 / 38  66 / 75, 47 / 59  99 / 111, 70 / 78  150 / 162, 103 / 113
 //   24 x 200               70 / 77, 34 / 39  116 / 124, 48 / 57  174 / 185, 72 / 79  275 / 277, 107 / 117
 //   48 x 200               116 / 123, 63 / 66  215 / 218, 99 / 97  339 / 327, 150 / 138  514 / 516, 222 / 213
+// Just above a round of the compute units the last blocks run alone.  22 batches with bounds of 256 to 383 blocks take 0.95, 1.01,
+// 1.03 and 1.05 times as long in one launch at N = 2048, 3000, 3500 and 4000 (0.87 to 1.12 at the first, 0.95 to 1.21 at the last), 15
+// with 384 to 449 blocks 0.93, 0.97, 0.98 and 1.00.  17 x 100 tokens (0.7 to 1, 0.1 to 1): 90 / 83, 54 / 57; 124 / 111, 76 / 73;
+// 142 / 125, 87 / 81; 164 / 145, 99 / 89; 12 x 200: 93 / 102, 55 / 62; 130 / 139, 78 / 87; 149 / 157, 89 / 97; 167 / 174, 101 / 95.
 // Every workgroup walks over the segments, 64 a turn, until it has its own (0.3 us a turn); the plan does that once.  us, direct /
 // planned, tokens of G = 4 over 0.5 to 1 of 100, 700 and 2000 rows, by turns x blocks:
 //   512 x 4 tokens, 1 head         4300       16 / 27, 33 / 44, 73 / 83
@@ -834,7 +838,7 @@ constexpr int64_t SG_WALK = 65536;
 bool goes_direct(const Dims& dm, int64_t n_rows, int64_t rows) {
   const int64_t blocks = (n_rows / (AT_ROWS / dm.G) + (n_rows < dm.S ? n_rows : dm.S)) * dm.Hkv;   // at most
   if (dm.S / WAVE * blocks >= SG_WALK) return false;
-  return rows <= (blocks < 64 ? 768 : (blocks < 128 ? 1280 : (blocks < SG_CUS ? 2048 : 4096)));
+  return rows <= (blocks < 64 ? 768 : (blocks < 128 ? 1280 : (blocks < SG_CUS ? 2048 : (blocks < 384 ? 3000 : 4096))));
 }
 
 hipError_t launch_segments(const Dims& dm, SegmentArgs& a, const ck_paged_kv& kv, const Space& space, void* workspace,

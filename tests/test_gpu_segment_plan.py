@@ -190,3 +190,15 @@ def test_segments_of_short_states_go_in_one_launch(S):
     out, ws = c.run([s % 3 for s in range(S)])
     assert not planned(ws)
     c.check(out, only=[0, 1, 2, S - 1])
+
+
+@pytest.mark.parametrize("S,n,want", [(17, 3990, True), (17, 2500, False), (64, 3990, False)])
+def test_a_round_and_a_few_blocks_of_long_states_are_planned(S, n, want):
+    """272 workgroups of 8 heads: the last ones would walk over their rows alone.  512 fill two rounds."""
+    c = Call([n - 37 * s % (n // 3) for s in range(S)], 8, 4, 16)
+    out, ws = c.run([(100 if S == 17 else 16) - s % 30 * (S == 17) for s in range(S)])
+    assert CUS < sum(c.blocks()) * 8
+    assert planned(ws) == want
+    c.check(out, only=(0, 1, S - 1))
+    if want:
+        c.pieces(ws)
