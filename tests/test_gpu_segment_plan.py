@@ -202,3 +202,76 @@ def test_a_round_and_a_few_blocks_of_long_states_are_planned(S, n, want):
     c.check(out, only=(0, 1, S - 1))
     if want:
         c.pieces(ws)
+
+
+def falling(n, S, least=1):
+    """S lengths between a tenth of n and n."""
+    return [max(least, int(n * (1 - 0.9 * ((s * 0.618) % 1)))) for s in range(S)]
+
+
+def test_pieces_in_order_of_their_size_several_of_a_thread():
+    """250 segments of one head, planned by 256 threads: some 500 pieces, put in order two at a time."""
+    c = Call(falling(6000, 250), 1, 4, 16)
+    out, ws = c.run([1] * 250)
+    counts = c.pieces(ws)
+    assert len(c.units()) <= 256 < sum(counts) and max(counts) > 1
+    c.check(out)
+
+
+def test_pieces_of_groups_in_order_of_their_size_several_of_a_thread():
+    c = Call(falling(9000, 160, 64), 1, 4, 16, groups=list(range(0, 161, 2)), shares=[100] * 160)
+    out, ws = c.run()
+    counts = c.pieces(ws)
+    assert len(c.units()) <= 256 < sum(counts) and max(counts) > 1
+    c.check(out)
+
+
+@pytest.mark.parametrize("even", [False, True])
+def test_more_segments_than_threads_that_are_cut(even):
+    """Long segments among the first 1024 units and behind them; with full blocks shares are even."""
+    lens, news = [(7 * s) % 197 for s in range(1100)], [(3 * s) % 5 for s in range(1100)]
+    for s in (0, 1, 1097, 1099):
+        lens[s], news[s] = 9000, 3
+    if even:
+        lens, news = [(7 * s) % 40 for s in range(1100)], [s % 2 for s in range(1100)]
+        lens[3], news[3], lens[1090], news[1090] = 9000, 3, 8579, 492
+    c = Call(lens, 1, 4 if even else 2, 16)
+    out, ws = c.run(news)
+    counts = c.pieces(ws)
+    cut = [i for i, (k, b) in enumerate(zip(counts, c.blocks())) if k > b]
+    assert cut and cut[0] < 1024 <= cut[-1] and c.extra(counts) <= EXTRA
+    c.check(out, only=[*cut, *range(4, 40), *range(1000, 1100)])
+
+
+def test_more_groups_and_sequences_than_threads_that_are_cut():
+    S = 900
+    lens, shares = [100 + (s * 31) % 90 for s in range(S)], [90 if s % 2 == 0 else 71 for s in range(S)]
+    for s in (0, 1):
+        lens[s], shares[s] = 9100 + s, 9000
+    lens[897] = lens[899] = 8000
+    c = Call(lens, 1, 2, 16, width=161 * 10 ** 6 // (512 * S) // 16 + 1, groups=[*range(0, S, 2), S], shares=shares)
+    out, ws = c.run()
+    counts = c.pieces(ws)
+    # groups 0 to 449, then the sequences
+    assert counts[0] > 1 and counts[450 + 897] > 1 and 450 + 897 >= 1024 and c.extra(counts) <= EXTRA
+    c.check(out, only=[*range(30), *range(880, S)])
+
+
+def test_groups_of_full_blocks_in_even_shares():
+    """Four groups of 256 query rows: as in the cross attention, no cut that is tried fits."""
+    S, n = 256, 16900
+    c = Call([n] * S, 1, 4, 16, groups=[0, 64, 128, 192, 256], shares=[n] * S)
+    out, ws = c.run()
+    counts = c.pieces(ws)
+    even = -(-4 * -(-n // TILE) // CUS)
+    assert counts[:4] == [counts[0]] * 4 and 1 < counts[0] <= -(-n // TILE) // even + 1 and sum(counts) <= CUS
+    c.check(out, only=(0, 63, 64, 130, 255))
+
+
+def test_cross_more_blocks_than_compute_units_and_a_long_segment():
+    """280 workgroups without a cut, and a segment that is cut; longest first."""
+    c = Call([150, 9000, 70, 3000], 8, 1, 16)
+    out, ws = c.run([7000, 2, 900, 300])
+    counts = c.pieces(ws)
+    assert sum(c.blocks()) * 8 > CUS and counts[1] > 1
+    c.check(out)
