@@ -119,8 +119,12 @@ const char* ck_last_error_detail(void);
  *                       (budget + n_sink + recent window), c ignored.
  *   CK_WS_PAGED_ATTN:   n and c ignored: enough for every list, window and lengths.
  *   CK_WS_PROMPT_ATTN:  n = n_rows of ck_prompt_attn, c ignored; enough for fewer rows too.
- *   CK_WS_SHARED_ATTN:  n and c ignored: enough for all groups and lengths.
+ *   CK_WS_SHARED_ATTN:  n and c ignored: enough for all groups and lengths.  About 0.54 MB times
+ *                       min(S * Hq / Hkv, 256), at most 138 MB, and 1 KB for each query head of each sequence;
+ *                       not less than CK_WS_PAGED_ATTN.
  *   CK_WS_CROSS_ATTN:   n = n_rows of ck_cross_attn, c ignored; enough for fewer rows too.
+ *                       About 0.54 MB times min(n * Hq / Hkv, 256), at most 138 MB, and a list of 32 bytes for
+ *                       every 256 / (Hq / Hkv) rows; not less than CK_WS_PAGED_ATTN.
  * Returns 0 for an invalid request.
  */
 size_t ck_workspace_bytes(const ck_shape* sh, int which, int64_t n, int32_t c);
@@ -694,7 +698,8 @@ int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_st
  *              most lengths[s].
  * workspace    ck_workspace_bytes(sh, CK_WS_SHARED_ATTN, 0, 0); calls that share one must be ordered (its contents
  *              on entry do not matter).
- * CK_BF16: products as in ck_prompt_attn.  Where S times the rows that the table has room for are few (160 MB of keys and
+ * CK_BF16: products as in ck_prompt_attn; of up to 16 queries (tokens times Hq / Hkv) that see the same rows as in
+ * ck_paged_decode_attn.  Where S times the rows that the table has room for are few (160 MB of keys and
  * values) every sequence reads all of its rows through its own table, with the products of ck_paged_decode_attn; so it
  * does in CK_F32 (check mode).
  * Lengths, groups and tables are read on the device: a captured call may be replayed with others.  The order of the
@@ -711,7 +716,7 @@ int ck_shared_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* 
  * q, out    [dev] [n_rows, Hq, d], not the same buffer.
  * q_starts  [dev] int32 [S + 1], as in ck_prompt_attn, but lengths do not count the new tokens; queries that attend to the same
  *           states (beams) can be one sequence's.  NULL: n_rows == S, one token per sequence, bf16 or fp32.
- *           With q_starts CK_BF16 only, products as in ck_prompt_attn.
+ *           With q_starts CK_BF16 only, products as in ck_shared_decode_attn.
  * workspace ck_workspace_bytes(sh, CK_WS_CROSS_ATTN, n, 0) with n >= n_rows; calls that share one must be ordered (its
  *           contents on entry do not matter).
  * Captured calls and the order of sums as in ck_shared_decode_attn.
