@@ -682,7 +682,7 @@ int ck_plan_pages(const ck_shape* sh, const int32_t* n_new, int32_t* lengths, in
  *   K[p / page_size][h][p % page_size] := k[t][h],  V likewise.
  * k, v, k_stride, v_stride  as in ck_rope_append.
  * slots     [dev] int32 [n_rows], as ck_plan_pages writes them; two rows must not have one slot.
- * Of kv the pool counts, the table does not.
+ * Of kv the pool counts; the table has to be there, but is not read.  At most 2^24 rows, and 2^26 rows of heads (n_rows * Hkv).
  */
 int ck_store_rows(const ck_shape* sh, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
                   int64_t n_rows, const int32_t* slots, const ck_paged_kv* kv, void* stream);
@@ -713,7 +713,7 @@ int ck_shared_decode_attn(const ck_shape* sh, const void* q, const ck_paged_kv* 
 /*
  * Cross attention: GQA attention of tokens to all rows [0, lengths[s]) of a cache of another length, an encoder's
  * states, without a causal order.  No row at all gives zeros.
- * q, out    [dev] [n_rows, Hq, d], not the same buffer.
+ * q, out    [dev] [n_rows, Hq, d], not the same buffer; n_rows at most 2^24, n_rows * Hq at most 2^30.
  * q_starts  [dev] int32 [S + 1], as in ck_prompt_attn, but lengths do not count the new tokens; queries that attend to the same
  *           states (beams) can be one sequence's.  NULL: n_rows == S, one token per sequence, bf16 or fp32.
  *           With q_starts CK_BF16 only, products as in ck_shared_decode_attn.
